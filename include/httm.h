@@ -415,6 +415,119 @@ HTTM_API int httm_unmerge_filtered(const httm_plan_t* plan, const void* o_m, con
  * head).  Waits for the stream; for tests and diagnostics. */
 HTTM_API int httm_outlier_stats(const httm_plan_t* plan, float* tau, int32_t* counts, void* stream);
 
+/* ---- around the layer: rows of a QKV projection, a paged cache, attention with a shared prefix --------
+ *
+ * The layer takes q, k, v as [H, N, d_head]; what a QKV projection leaves are rows of tokens, without the norms of queries
+ * and keys and without the position rotation (the host model applies both in front of its attention).
+ * httm_qk_norm_rope makes the one from the other.  A scene that is watched further - new frames, several viewers, tokens
+ * that are drawn one by one - keeps its merged keys and values (stage 2's k_m, v_m) as a prefix that every sequence of
+ * a batch shares, and what is new in pages: httm_cache_append writes them, httm_attention_cached reads both.
+ *
+ * For these calls:
+ *   - d_head must be 64, at most HTTM_MAX_HEADS heads.  H_q query heads share H_kv key heads, H_q a multiple of H_kv:
+ *     query head h reads key head h / (H_q / H_kv).
+ *   - Data in device memory (offsets, lengths, tables, positions) is not seen by the argument checks.  The kernels bound
+ *     every address they make from it: see the calls for what becomes of values out of range.
+ *   - No call keeps anything between calls; with a workspace of its own each, calls may overlap freely. */
+
+/* Element type of a tensor whose type the caller chooses */
+enum { HTTM_BF16 = 0, HTTM_FP16 = 1, HTTM_FP32 = 2 };
+
+enum {
+  HTTM_NORM_NONE = 0,
+  HTTM_NORM_RMS = 1,    /* x / sqrt(mean(x^2) + eps) * weight + bias */
+  HTTM_NORM_LAYER = 2   /* (x - mean(x)) / sqrt(var(x) + eps) * weight + bias, var without Bessel's correction */
+};
+enum {
+  HTTM_ROPE_HALVES = 0,     /* channel i of an axis rotates with channel i + w / 2 */
+  HTTM_ROPE_NEIGHBOURS = 1  /* channels 2 i and 2 i + 1 of an axis */
+};
+
+/* Norm over the d_head channels of every row of q and of k, then the rotation of their first rot_dim channels by the
+ * token's position.  These are split evenly among the `axes` coordinates of a position (row and column of the patch
+ * grid: 2; place in a text: 1): axis a has the w = rot_dim / axes channels from a * w on, in w / 2 pairs, and pair i turns by
+ * t = position[a] * base^(-2 i / w): (x, y) -> (x cos t - y sin t, y cos t + x sin t).  Computed in fp32, the angle
+ * modulo a turn in 64-bit fixed point, so that it is exact at any position. */
+typedef struct httm_norm_rope {
+  int32_t norm;         /* HTTM_NORM_* */
+  int32_t axes;         /* position coordinates, 0 (no rotation) to 3 */
+  int32_t rot_dim;      /* channels that rotate: a multiple of 16 * axes, at most d_head; ignored without axes */
+  int32_t pairing;      /* HTTM_ROPE_* */
+  double base;          /* 1 to 1e12 */
+  float eps;            /* finite, not negative */
+  float k_scale;        /* finite factor on the keys in fp32, behind the rotation: 1, or log2(e) / 8 for a plan with log2 keys */
+  const float* q_weight;    /* [d_head] fp32 (device, 16-byte aligned) or NULL: ones / zeros; ignored without norm */
+  const float* q_bias;
+  const float* k_weight;
+  const float* k_bias;
+} httm_norm_rope_t;
+
+/* Rows of tokens: channel c of head h of token t is element t * token_stride + h * head_stride + c.  Strides in
+ * elements, not negative, multiples of 8. */
+typedef struct httm_rows {
+  const void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} httm_rows_t;
+
+/* q_out[h][t], k_out[h][t] = rotated norm of q[t][h], k[t][h];  v_out[h][t] = v[t][h].
+ * q: N x H_q rows, k, v: N x H_kv rows, all of type `dtype` (HTTM_BF16, _FP16, _FP32).  Any of the three may have data
+ * NULL and is left out then, with its output; k and v need not come together.
+ * pos: [N][axes] int32 (device); may be NULL without axes.
+ * q_out: [H_q, N, d_head], k_out, v_out: [H_kv, N, d_head] bf16.  N < 2^25. */
+HTTM_API int httm_qk_norm_rope(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v,
+                               int dtype, const int32_t* pos, int64_t N, int H_q, int H_kv, int d_head, void* q_out,
+                               void* k_out, void* v_out, void* stream);
+
+/* Keys and values of n_seqs sequences in pages of page_size rows: row p of sequence b and key head h is
+ * pages[page_table[b * table_stride + p / page_size]][h][p % page_size].
+ * A page may belong to several sequences (a beginning that they share) as long as none appends to it.  An entry of the
+ * table outside 0 .. n_pages - 1 is no page: what would be written there is left out, and so are keys that would be
+ * read.  A sequence has at most table_stride * page_size rows; a greater length counts as that, a negative one as 0. */
+typedef struct httm_paged {
+  void* k_pages;                /* [n_pages, H_kv, page_size, d_head] bf16 */
+  void* v_pages;
+  const int32_t* page_table;    /* [n_seqs, table_stride] int32 (device) */
+  int64_t n_pages;              /* 1 .. 2^31 - 1 */
+  int32_t n_seqs;               /* 1 .. HTTM_MAX_SEQS */
+  int32_t table_stride;
+  int32_t page_size;            /* a power of two, 16 .. 4096 */
+  int32_t H_kv;
+} httm_paged_t;
+#define HTTM_MAX_SEQS 4096
+
+/* Appends new tokens to the cache and puts their queries into q_out, norm and rotation as httm_qk_norm_rope.
+ * The tokens of the batch lie one sequence behind the other: sequence b has the tokens [offsets[b], offsets[b + 1]), which
+ * become its last rows: with them it has seq_lens[b].  offsets: [n_seqs + 1] int32 (device), not decreasing; tokens in
+ * front of offsets[0] and from offsets[n_seqs] on are padding, for which nothing is written.  A token whose row
+ * would be negative is not written to the cache.
+ * q: n_tokens x H_q rows, k, v: n_tokens x H_kv rows of type `dtype`.  q may have data NULL, and q_out be NULL then.
+ * pos: [n_tokens][axes] int32 (device), or NULL with one axis: then a token's position is first_pos + its row.
+ * q_out: [n_tokens, H_q, d_head] bf16.  n_tokens < 2^25; 0 tokens are no error. */
+HTTM_API int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v,
+                               int dtype, const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head,
+                               const httm_paged_t* cache, const int32_t* offsets, const int32_t* seq_lens, void* q_out,
+                               void* stream);
+
+/* Attention of the tokens of a batch (offsets, seq_lens as above, after the append) to a prefix that all sequences share
+ * and to their own cache:
+ *   o[t][h] = sum_j e^(scale * q.k_j) v_j / sum_j e^(scale * q.k_j)
+ * over the P rows of the prefix and the rows of the token's sequence: all of them, or with `causal` the rows up to the token's
+ * own.  Weights and sums in fp32, weights rounded to bf16 for the product with v.  A token that sees no key gets
+ * zeros; padding is left as it was.  What stands in rows and pages that a token does not see has no effect on it, NaN
+ * and infinities included.
+ * q: n_tokens x H_q rows, bf16.  k_prefix, v_prefix: [H_kv, P, d_head] bf16, P < 2^24; may be NULL with P = 0.
+ * cache: may have no rows in it (all lengths 0: attention to the prefix alone).
+ * scale: positive, finite (1/8 = 1/sqrt(d_head); ln 2 for keys with log2(e) / 8 in them: HTTM_FLAG_LOG2_KEYS).
+ * o: [n_tokens, H_q * d_head] bf16.  n_tokens < 2^21; 0 tokens are no error.
+ * workspace: device, 256-byte aligned, httm_attention_cached_workspace(...) bytes; its contents before and after the call are
+ * meaningless.  Results do not depend on it and are run-to-run identical. */
+HTTM_API int64_t httm_attention_cached_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P);
+HTTM_API int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P,
+                                   const httm_paged_t* cache, const int32_t* offsets, const int32_t* seq_lens, int64_t n_tokens,
+                                   int H_q, int d_head, float scale, int causal, void* o, void* workspace,
+                                   int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

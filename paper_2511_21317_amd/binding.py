@@ -41,6 +41,21 @@ class WorkspaceLayout(C.Structure):
                                          "q_out", "o_out", "attn_split", "total")]
 
 
+class NormRopeStruct(C.Structure):
+    _fields_ = [("norm", C.c_int32), ("axes", C.c_int32), ("rot_dim", C.c_int32), ("pairing", C.c_int32), ("base", C.c_double),
+                ("eps", C.c_float), ("k_scale", C.c_float), ("q_weight", C.c_void_p), ("q_bias", C.c_void_p),
+                ("k_weight", C.c_void_p), ("k_bias", C.c_void_p)]
+
+
+class RowsStruct(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class PagedStruct(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p), ("n_pages", C.c_int64),
+                ("n_seqs", C.c_int32), ("table_stride", C.c_int32), ("page_size", C.c_int32), ("H_kv", C.c_int32)]
+
+
 _lib = None
 
 
@@ -86,7 +101,13 @@ def lib() -> C.CDLL:
     L.httm_unmerge_filtered.argtypes = [vp, vp, vp, i32p, vp, vp]
     L.httm_outlier_stats.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_int32), vp]
     L.httm_global_match.argtypes = [vp, C.c_int64, C.c_int, C.c_int, C.c_double, i32p, f32p, vp]
-    for name in ("httm_geom_sizes", "httm_workspace_layout", "httm_geom_tables", "httm_geom_block_forms", "httm_plan_create", "httm_plan_clone",
+    i64, rows, norm_rope, paged = C.c_int64, C.POINTER(RowsStruct), C.POINTER(NormRopeStruct), C.POINTER(PagedStruct)
+    L.httm_qk_norm_rope.argtypes = [norm_rope, rows, rows, rows, C.c_int, vp, i64, C.c_int, C.c_int, C.c_int, vp, vp, vp, vp]
+    L.httm_cache_append.argtypes = [norm_rope, rows, rows, rows, C.c_int, vp, i64, i64, C.c_int, C.c_int, paged, vp, vp, vp, vp]
+    L.httm_attention_cached_workspace.argtypes = [i64, C.c_int, C.c_int, C.c_int, i64]
+    L.httm_attention_cached_workspace.restype = i64
+    L.httm_attention_cached.argtypes = [rows, vp, vp, i64, paged, vp, vp, i64, C.c_int, C.c_int, C.c_float, C.c_int, vp, vp, i64, vp]
+    for name in ("httm_qk_norm_rope", "httm_cache_append", "httm_attention_cached", "httm_geom_sizes", "httm_workspace_layout", "httm_geom_tables", "httm_geom_block_forms", "httm_plan_create", "httm_plan_clone",
                  "httm_plan_destroy", "httm_plan_query", "httm_reorder", "httm_match_merge",
                  "httm_reorder_match_merge",
                  "httm_attention", "httm_attention_scratch", "httm_attention_log2", "httm_attention_log2_scratch", "httm_attention_log2_static", "httm_attention_split_plan", "httm_attention_route", "httm_attention_wide_plan", "httm_unmerge", "httm_layer_forward",
@@ -467,3 +488,159 @@ def global_match(x, dst_frac: float, best_dst, sim=None):
 
 def alloc_workspace(plan: Plan) -> torch.Tensor:
     return torch.empty(int(plan.sizes.workspace_bytes), dtype=torch.uint8, device="cuda")
+
+
+# ---- rows of a projection, paged cache, attention with a shared prefix ---------------------------------------
+
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+PAIRINGS = {"halves": 0, "neighbours": 1}
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+MAX_SEQS = 4096
+
+
+def _same_device(*tensors):
+    """All on the GPU that is current: a launch goes there, and its stream is asked for there."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise HttmError(f"tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def _rows(t, H, dtype):
+    """A [N, H, 64] view whose channels are dense, as the C side takes it."""
+    if t is None:
+        return RowsStruct(None, 0, 0)
+    if not t.is_cuda:
+        raise HttmError("tensor must live on the GPU")
+    if t.dtype != dtype:
+        raise HttmError(f"expected dtype {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[1] != H or t.shape[2] != 64:
+        raise HttmError(f"expected shape [N, {H}, 64], got {tuple(t.shape)}")
+    token, head, channel = t.stride()
+    if channel != 1:
+        raise HttmError("the 64 channels of a row must be contiguous")
+    # (a stride along an axis of length 1 means nothing)
+    return RowsStruct(t.data_ptr(), token if t.shape[0] > 1 else 0, head if H > 1 else 0)
+
+
+class NormRope:
+    """Norms of queries and keys and the rotation by position (httm_norm_rope_t).
+
+    norm: "none", "rms" or "layer"; weights and biases: [64] fp32 tensors or None.
+    axes: coordinates of a position, 0 (no rotation) to 3; rot_dim: channels that rotate, a multiple of 16 * axes;
+    pairing: "halves" or "neighbours"; k_scale: factor on the keys (LOG2_KEY_SCALE for log2 keys)."""
+
+    def __init__(self, norm="layer", eps=1e-6, axes=2, rot_dim=64, pairing="halves", base=100.0, q_weight=None, q_bias=None,
+                 k_weight=None, k_bias=None, k_scale=1.0):
+        self.affine = (q_weight, q_bias, k_weight, k_bias)      # kept alive
+        self.axes = int(axes)
+        self.struct = NormRopeStruct(NORMS[norm], self.axes, int(rot_dim), PAIRINGS[pairing], float(base), float(eps), float(k_scale),
+                                     *(None if t is None else _dev(t, torch.float32, (64,)) for t in self.affine))
+
+
+class PagedCache:
+    """Keys and values in pages (httm_paged_t): k_pages, v_pages [n_pages, H_kv, page_size, 64] bf16, page_table
+    [n_seqs, pages of a sequence] int32."""
+
+    def __init__(self, k_pages, v_pages, page_table):
+        if k_pages.dim() != 4 or page_table.dim() != 2:
+            raise HttmError("expected k_pages [n_pages, H_kv, page_size, 64] and page_table [n_seqs, pages]")
+        n_pages, H_kv, page_size, d = k_pages.shape
+        shape = (n_pages, H_kv, page_size, 64)
+        _same_device(k_pages, v_pages, page_table) if k_pages.is_cuda else None
+        self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
+        self.n_seqs, self.H_kv, self.page_size = int(page_table.shape[0]), int(H_kv), int(page_size)
+        self.struct = PagedStruct(_dev(k_pages, torch.bfloat16, shape), _dev(v_pages, torch.bfloat16, shape),
+                                  _dev(page_table, torch.int32), n_pages, self.n_seqs, page_table.shape[1], page_size, H_kv)
+
+
+def _projection_type(*tensors):
+    dtype = next((t.dtype for t in tensors if t is not None), None)
+    if dtype not in _DTYPES:
+        raise HttmError(f"rows must be bf16, fp16 or fp32, got {dtype}")
+    return dtype
+
+
+def qk_norm_rope(nr: NormRope, q, k, v, pos, q_out, k_out, v_out):
+    """Rows of a projection -> the layer's tensors: q [N, H_q, 64], k, v [N, H_kv, 64] (any token and head strides, bf16, fp16 or
+    fp32) -> q_out [H_q, N, 64], k_out, v_out [H_kv, N, 64] bf16.  pos: [N, axes] int32 (None without axes).
+    Any of q, k, v may be None, with its output."""
+    given = [t for t in (q, k, v) if t is not None]
+    dtype = _projection_type(*given)
+    N = int(given[0].shape[0])
+    kv = k if k is not None else v
+    H_kv = int(kv.shape[1]) if kv is not None else 1
+    H_q = int(q.shape[1]) if q is not None else H_kv
+    rows = [_rows(q, H_q, dtype), _rows(k, H_kv, dtype), _rows(v, H_kv, dtype)]
+    outs = []
+    for t, out, H in ((q, q_out, H_q), (k, k_out, H_kv), (v, v_out, H_kv)):
+        if t is not None and t.shape[0] != N:
+            raise HttmError(f"expected {N} tokens, got {int(t.shape[0])}")
+        if (t is None) != (out is None):
+            raise HttmError("every tensor needs its output, and every output its tensor")
+        outs.append(_dev(out, torch.bfloat16, (H, N, 64)) if out is not None else None)
+    turning = nr.axes > 0 and (q is not None or k is not None)
+    if turning and pos is None:
+        raise HttmError("positions are needed for a rotation")
+    p = _dev(pos, torch.int32, (N, nr.axes)) if turning else None
+    _same_device(q, k, v, pos if turning else None, q_out, k_out, v_out, *nr.affine)
+    _check(lib().httm_qk_norm_rope(C.byref(nr.struct), C.byref(rows[0]), C.byref(rows[1]), C.byref(rows[2]), _DTYPES[dtype], p,
+                                   N, H_q, H_kv, 64, *outs, _stream()), "httm_qk_norm_rope")
+    return q_out, k_out, v_out
+
+
+def cache_append(nr: NormRope, q, k, v, pos, cache: PagedCache, offsets, seq_lens, q_out, first_pos: int = 0):
+    """New tokens of the sequences of a batch into the cache: q [n, H_q, 64] (or None, with q_out), k, v [n, H_kv, 64]; offsets
+    [n_seqs + 1], seq_lens [n_seqs] (with the new tokens) int32 on the GPU; q_out [n, H_q, 64] bf16.
+    pos: [n, axes] int32, or None with one axis: first_pos + a token's row in its sequence."""
+    dtype = _projection_type(k)
+    n = int(k.shape[0])
+    H_q = int(q.shape[1]) if q is not None else cache.H_kv
+    if v is None or v.shape[0] != n or (q is not None and q.shape[0] != n):
+        raise HttmError(f"expected {n} tokens in q, k and v")
+    if (q is None) != (q_out is None):
+        raise HttmError("q needs q_out, and q_out needs q")
+    rows = [_rows(q, H_q, dtype), _rows(k, cache.H_kv, dtype), _rows(v, cache.H_kv, dtype)]
+    out = _dev(q_out, torch.bfloat16, (n, H_q, 64)) if q_out is not None else None
+    p = _dev(pos, torch.int32, (n, nr.axes)) if pos is not None and nr.axes > 0 else None
+    off, lens = _dev(offsets, torch.int32, (cache.n_seqs + 1,)), _dev(seq_lens, torch.int32, (cache.n_seqs,))
+    _same_device(q, k, v, pos, cache.k_pages, offsets, seq_lens, q_out, *nr.affine)
+    _check(lib().httm_cache_append(C.byref(nr.struct), C.byref(rows[0]), C.byref(rows[1]), C.byref(rows[2]), _DTYPES[dtype], p,
+                                   int(first_pos), n, H_q, 64, C.byref(cache.struct), off, lens, out, _stream()), "httm_cache_append")
+    return q_out
+
+
+def attention_cached_workspace(n_tokens: int, n_seqs: int, H_q: int, H_kv: int, P: int) -> int:
+    """Bytes of workspace of attention_cached()."""
+    n = int(lib().httm_attention_cached_workspace(int(n_tokens), int(n_seqs), int(H_q), int(H_kv), int(P)))
+    if n < 0:
+        _check(n, "httm_attention_cached_workspace")
+    return n
+
+
+def attention_cached(q, k_prefix, v_prefix, cache: PagedCache, offsets, seq_lens, out, scale: float = 0.125, causal: bool = False,
+                     workspace=None):
+    """Attention of a batch's tokens q [n, H_q, 64] (any strides) to the prefix [H_kv, P, 64] (or None) that all sequences
+    share and to their own rows in the cache.  offsets, seq_lens as for cache_append; out [n, H_q * 64] bf16.
+    workspace: a uint8 tensor of at least attention_cached_workspace(...) bytes."""
+    bf = torch.bfloat16
+    if q.dim() != 3:
+        raise HttmError(f"expected q [n, H_q, 64], got {tuple(q.shape)}")
+    n, H_q, P = int(q.shape[0]), int(q.shape[1]), 0
+    rows = _rows(q, H_q, bf)
+    if (k_prefix is None) != (v_prefix is None):
+        raise HttmError("a prefix has keys and values")
+    if k_prefix is not None:
+        if k_prefix.dim() != 3:
+            raise HttmError(f"expected a prefix [{cache.H_kv}, P, 64], got {tuple(k_prefix.shape)}")
+        P = int(k_prefix.shape[1])
+    kp = _dev(k_prefix, bf, (cache.H_kv, P, 64)) if P else None
+    vp = _dev(v_prefix, bf, (cache.H_kv, P, 64)) if P else None
+    off, lens = _dev(offsets, torch.int32, (cache.n_seqs + 1,)), _dev(seq_lens, torch.int32, (cache.n_seqs,))
+    if workspace is None:
+        raise HttmError("a workspace of attention_cached_workspace() bytes is needed")
+    _same_device(q, k_prefix, v_prefix, cache.k_pages, offsets, seq_lens, out, workspace)
+    _check(lib().httm_attention_cached(C.byref(rows), kp, vp, P, C.byref(cache.struct), off, lens, n, H_q, 64, float(scale),
+                                       1 if causal else 0, _dev(out, bf, (n, H_q * 64)), _dev(workspace, torch.uint8),
+                                       workspace.numel(), _stream()), "httm_attention_cached")
+    return out

@@ -17,7 +17,7 @@ PROBE_LIB_PATH = os.path.join(PKG_DIR, "libhttm_probe.so")   # measurement helpe
 PROBE_SOURCES = ["mfma_probe.hip"]
 
 SOURCES = ["api.hip", "geometry.cpp", "reorder_unmerge.hip", "match_merge.hip", "match_merge_big.hip", "outlier_filter.hip",
-           "attention.hip"]
+           "attention.hip", "token_rows.hip", "attention_cached.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -2,6 +2,7 @@
 // httm_layer_forward.  See include/httm.h for the contract of every entry point.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstring>
 #include <memory>
 #include <new>
@@ -687,6 +688,164 @@ int httm_outlier_stats(const httm_plan_t* p, float* tau, int32_t* counts, void* 
   int32_t off[HTTM_MAX_HEADS + 1];
   HTTM_HIP(hipMemcpy(off, p->ob.offsets, (size_t)(p->geom.H + 1) * 4, hipMemcpyDeviceToHost));
   for (int h = 0; h < p->geom.H; ++h) counts[h] = off[h + 1] - off[h];
+  return HTTM_OK;
+}
+
+}  // extern "C"
+
+// ---- rows of a projection, paged cache, attention with a shared prefix ----------------------------------------
+
+namespace {
+
+// What all rows of a call must be: 16-byte aligned 8-channel chunks, addresses within 62 bits
+int check_rows(const httm_rows_t* r, TokenRows* out) {
+  *out = {nullptr, 0, 0};
+  if (!r || !r->data) return HTTM_OK;
+  constexpr int64_t kMost = (int64_t)1 << 31;
+  if (!aligned16(r->data) || r->token_stride < 0 || r->head_stride < 0 || r->token_stride % 8 || r->head_stride % 8 ||
+      r->token_stride >= kMost || r->head_stride >= kMost * 64)
+    return HTTM_E_INVALID_ARG;
+  *out = {(const char*)r->data, r->token_stride, r->head_stride};
+  return HTTM_OK;
+}
+
+int check_cache(const httm_paged_t* c, int H_q, PagedArgs* out) {
+  if (!c || !c->k_pages || !c->v_pages || !c->page_table || c->n_pages < 1 || c->n_seqs < 1 || c->table_stride < 1 ||
+      c->page_size < 1 || c->H_kv < 1 || H_q < 1 || H_q % c->H_kv)
+    return HTTM_E_INVALID_ARG;
+  if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || (reinterpret_cast<uintptr_t>(c->page_table) & 3u)) return HTTM_E_INVALID_ARG;
+  if (H_q > HTTM_MAX_HEADS || c->n_seqs > HTTM_MAX_SEQS || c->page_size < 16 || c->page_size > 4096 ||
+      (c->page_size & (c->page_size - 1)) || c->n_pages > INT32_MAX ||
+      (int64_t)c->table_stride * c->page_size > ((int64_t)1 << 30))
+    return HTTM_E_UNSUPPORTED;
+  *out = {(char*)c->k_pages, (char*)c->v_pages, c->page_table, c->n_pages, c->n_seqs, c->table_stride, __builtin_ctz(c->page_size), c->H_kv};
+  return HTTM_OK;
+}
+
+// Norm, rotation and sources of a launch
+int fill_norm_rope(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype, int64_t N,
+                   int H_q, int H_kv, int d_head, NormRopeArgs* a) {
+  std::memset(a, 0, sizeof(*a));
+  if (!nr || N < 0 || H_q < 1 || H_kv < 1) return HTTM_E_INVALID_ARG;
+  if (dtype != HTTM_BF16 && dtype != HTTM_FP16 && dtype != HTTM_FP32) return HTTM_E_INVALID_ARG;
+  if (nr->norm != HTTM_NORM_NONE && nr->norm != HTTM_NORM_RMS && nr->norm != HTTM_NORM_LAYER) return HTTM_E_INVALID_ARG;
+  if (nr->pairing != HTTM_ROPE_HALVES && nr->pairing != HTTM_ROPE_NEIGHBOURS) return HTTM_E_INVALID_ARG;
+  if (!std::isfinite(nr->eps) || nr->eps < 0.f || !std::isfinite(nr->k_scale)) return HTTM_E_INVALID_ARG;
+  if (nr->axes < 0 || nr->axes > 3) return HTTM_E_INVALID_ARG;
+  if (d_head != 64 || H_q > HTTM_MAX_HEADS || H_kv > HTTM_MAX_HEADS || N >= ((int64_t)1 << 25)) return HTTM_E_UNSUPPORTED;
+  if (nr->axes > 0) {
+    if (nr->rot_dim < 1 || nr->rot_dim > d_head || nr->rot_dim % (16 * nr->axes)) return HTTM_E_INVALID_ARG;
+    if (!(nr->base >= 1.0 && nr->base <= 1e12)) return HTTM_E_INVALID_ARG;
+    const int width = nr->rot_dim / nr->axes;
+    a->axis_chunks = width / 8;
+    // 2^64 / 2 pi; the product keeps 64 bits, and base >= 1 keeps it below 2^62
+    constexpr long double kTurn = 18446744073709551616.0L / 6.28318530717958647692528676655900577L;
+    for (int i = 0; i < width / 2; ++i) a->turn[i] = (uint64_t)(kTurn * std::pow((long double)nr->base, -2.0L * i / width) + 0.5L);
+  }
+  if (nr->norm != HTTM_NORM_NONE) {
+    const float* affine[] = {nr->q_weight, nr->k_weight, nr->q_bias, nr->k_bias};
+    for (int i = 0; i < 4; ++i) {
+      if (!aligned16(affine[i])) return HTTM_E_INVALID_ARG;
+      (i < 2 ? a->weight[i] : a->bias[i - 2]) = affine[i];
+    }
+  }
+  const httm_rows_t* src[] = {q, k, v};
+  for (int i = 0; i < 3; ++i) {
+    const int rc = check_rows(src[i], &a->src[i]);
+    if (rc != HTTM_OK) return rc;
+    a->H[i] = a->src[i].data ? (i == 0 ? H_q : H_kv) : 0;
+  }
+  a->N = N;
+  a->axes = nr->axes;
+  a->norm = nr->norm;
+  a->pairing = nr->pairing;
+  a->eps = nr->eps;
+  a->k_scale = nr->k_scale;
+  return HTTM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int httm_qk_norm_rope(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype,
+                      const int32_t* pos, int64_t N, int H_q, int H_kv, int d_head, void* q_out, void* k_out, void* v_out,
+                      void* stream) {
+  NormRopeArgs a;
+  const int rc = fill_norm_rope(nr, q, k, v, dtype, N, H_q, H_kv, d_head, &a);
+  if (rc != HTTM_OK) return rc;
+  if (N == 0) return HTTM_OK;
+  void* out[] = {q_out, k_out, v_out};
+  for (int i = 0; i < 3; ++i) {
+    if ((a.src[i].data == nullptr) != (out[i] == nullptr) || !aligned16(out[i])) return HTTM_E_INVALID_ARG;
+    a.out[i] = (char*)out[i];
+  }
+  if (a.H[0] + a.H[1] + a.H[2] == 0) return HTTM_E_INVALID_ARG;
+  if (a.axes > 0 && a.H[0] + a.H[1] > 0 && (!pos || (reinterpret_cast<uintptr_t>(pos) & 3u))) return HTTM_E_INVALID_ARG;
+  a.pos = pos;
+  HTTM_HIP(launch_norm_rope(a, dtype, false, (hipStream_t)stream));
+  return HTTM_OK;
+}
+
+int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype,
+                      const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head, const httm_paged_t* cache,
+                      const int32_t* offsets, const int32_t* seq_lens, void* q_out, void* stream) {
+  NormRopeArgs a;
+  PagedArgs paged;
+  int rc = check_cache(cache, H_q, &paged);
+  if (rc != HTTM_OK) return rc;
+  rc = fill_norm_rope(nr, q, k, v, dtype, n_tokens, H_q, cache->H_kv, d_head, &a);
+  if (rc != HTTM_OK) return rc;
+  if (first_pos < 0 || first_pos > INT32_MAX) return HTTM_E_INVALID_ARG;
+  if (!offsets || !seq_lens || ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(seq_lens)) & 3u)) return HTTM_E_INVALID_ARG;
+  if (n_tokens == 0) return HTTM_OK;
+  if (!a.src[1].data || !a.src[2].data || (a.src[0].data == nullptr) != (q_out == nullptr) || !aligned16(q_out)) return HTTM_E_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(pos) & 3u) return HTTM_E_INVALID_ARG;
+  if (!pos && a.axes > 1) return HTTM_E_INVALID_ARG;
+  a.pos = pos;
+  a.first_pos = first_pos;
+  a.cache = paged;
+  a.offsets = offsets;
+  a.seq_lens = seq_lens;
+  a.out[0] = (char*)q_out;
+  HTTM_HIP(launch_norm_rope(a, dtype, true, (hipStream_t)stream));
+  return HTTM_OK;
+}
+
+int64_t httm_attention_cached_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
+  if (n_tokens < 0 || n_seqs < 1 || H_kv < 1 || H_q < 1 || H_q % H_kv || P < 0) return HTTM_E_INVALID_ARG;
+  if (n_seqs > HTTM_MAX_SEQS || H_q > HTTM_MAX_HEADS || n_tokens >= ((int64_t)1 << 21) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
+  return cached_attention_workspace(n_tokens, n_seqs, H_q, H_kv, P);
+}
+
+int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P, const httm_paged_t* cache,
+                          const int32_t* offsets, const int32_t* seq_lens, int64_t n_tokens, int H_q, int d_head, float scale,
+                          int causal, void* o, void* workspace, int64_t workspace_bytes, void* stream) {
+  CachedAttnArgs a;
+  std::memset(&a, 0, sizeof(a));
+  int rc = check_cache(cache, H_q, &a.cache);
+  if (rc != HTTM_OK) return rc;
+  if (n_tokens < 0 || P < 0 || !std::isfinite(scale) || !std::isnormal(scale) || scale < 0.f) return HTTM_E_INVALID_ARG;
+  if (d_head != 64 || n_tokens >= ((int64_t)1 << 21) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
+  if (P > 0 && (!k_prefix || !v_prefix || !aligned16(k_prefix) || !aligned16(v_prefix))) return HTTM_E_INVALID_ARG;
+  if (!offsets || !seq_lens || ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(seq_lens)) & 3u)) return HTTM_E_INVALID_ARG;
+  if (n_tokens == 0) return HTTM_OK;
+  if (!q || !q->data || !o || !aligned16(o) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HTTM_E_INVALID_ARG;
+  rc = check_rows(q, &a.q);
+  if (rc != HTTM_OK) return rc;
+  if (workspace_bytes < cached_attention_workspace(n_tokens, cache->n_seqs, H_q, cache->H_kv, P)) return HTTM_E_WORKSPACE_TOO_SMALL;
+  a.k_prefix = (const char*)k_prefix;
+  a.v_prefix = (const char*)v_prefix;
+  a.P = P;
+  a.offsets = offsets;
+  a.seq_lens = seq_lens;
+  a.n_tokens = n_tokens;
+  a.group = H_q / cache->H_kv;
+  a.causal = causal != 0;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.o = o;
+  a.workspace = (char*)workspace;
+  HTTM_HIP(launch_cached_attention(a, (hipStream_t)stream));
   return HTTM_OK;
 }
 

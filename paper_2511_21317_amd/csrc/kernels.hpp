@@ -194,4 +194,63 @@ hipError_t launch_unmerge(const void* o_m, const int32_t* assign, const int32_t*
                           int H, int64_t N, int64_t M_q, int fused, hipStream_t stream,
                           const void* o_out = nullptr);
 
+// ---- rows of a projection, paged cache -------------------------------------------------------------
+constexpr int kMaxPairs = 64 / 2;     // pairs of channels an axis can have
+struct TokenRows {
+  const char* data;         // nullptr: left out
+  int64_t token_stride;     // elements
+  int64_t head_stride;
+};
+struct PagedArgs {
+  char* k_pages;
+  char* v_pages;
+  const int32_t* table;
+  int64_t n_pages;
+  int32_t n_seqs;
+  int32_t table_stride;
+  int32_t page_shift;       // log2 of the rows of a page
+  int32_t H_kv;
+};
+struct NormRopeArgs {
+  TokenRows src[3];         // q, k, v
+  const int32_t* pos;       // [N][axes] or nullptr
+  int64_t first_pos;        // nullptr: a token's position is first_pos + its row in the cache
+  int64_t N;
+  int32_t H[3];             // heads of q, k, v; 0 where src is left out
+  int32_t axes;
+  int32_t norm;
+  int32_t pairing;
+  int32_t axis_chunks;      // 8-channel chunks of an axis
+  float eps;
+  float k_scale;
+  const float* weight[2];   // q, k; or nullptr
+  const float* bias[2];
+  char* out[3];             // q_out, k_out, v_out; with a cache only q_out, [N][H_q][64]
+  PagedArgs cache;          // appending only
+  const int32_t* offsets;
+  const int32_t* seq_lens;
+  uint64_t turn[kMaxPairs]; // turns per position step of every pair of an axis, as a fraction of 2^64
+};
+// dtype: HTTM_BF16 / _FP16 / _FP32 of the sources; append: into a.cache instead of [H, N, 64] tensors.
+hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, bool append, hipStream_t stream);
+
+// ---- attention of a batch with a shared prefix and a paged cache --------------------------------------
+struct CachedAttnArgs {
+  TokenRows q;
+  const char* k_prefix;
+  const char* v_prefix;
+  int64_t P;
+  PagedArgs cache;
+  const int32_t* offsets;
+  const int32_t* seq_lens;
+  int64_t n_tokens;
+  int32_t group;            // query heads per key head
+  int32_t causal;
+  float scale_log2;         // scale * log2(e)
+  void* o;                  // [n_tokens][H_kv * group * 64] bf16
+  char* workspace;
+};
+int64_t cached_attention_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P);
+hipError_t launch_cached_attention(const CachedAttnArgs& a, hipStream_t stream);
+
 }  // namespace httm

@@ -1,0 +1,267 @@
+// The rows that a QKV projection leaves, on their way into the layer or into a paged cache: norms of queries and keys
+// over their 64 channels and the rotation of channel pairs by the token's position, in one pass.
+//
+//   layer norm  (x - mean) / sqrt(mean((x - mean)^2) + eps) * w + b,   RMS norm  x / sqrt(mean(x^2) + eps) * w + b
+//   rotation    (x, y) -> (x cos t - y sin t, y cos t + x sin t),   t = position * base^(-2 i / axis width)
+//
+// The kernel moves 128 bytes in and 128 out per row (256 in from fp32) and does some ten operations per element: it is bound
+// by memory, or by one launch where there are few rows.
+//
+// Layout.  Eight lanes hold a row, 8 channels (16 bytes of bf16) each, so a wave has the same head of eight
+// consecutive tokens: eight 128-byte lines in, and out to [H, N, 64] 1 KB in a piece.  The sums of a norm are sums in
+// a lane and three exchanges.  A wave walks over several heads of its tokens: the angles depend on the token alone, and
+// their 16 sines and cosines per lane cost as much issue time as a row's memory time, so they are made once.
+//
+// Angles.  In units of turns and modulo 1, which is all that sine and cosine see: position times a 64-bit fraction
+// of a turn per step, wrapped by the integer product itself.  The fraction is off by at most 2^-65, the angle at position
+// 2^31 by 2^-34 turns; fp32 holds the wrapped angle to 2^-25.  v_sin_f32 and v_cos_f32 take turns.
+#include <algorithm>
+
+#include "dev_common.hpp"
+#include "kernels.hpp"
+
+namespace httm {
+
+namespace {
+
+constexpr int kWaves = 4;          // per workgroup
+constexpr int kTokens = 8;         // per wave
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// 8 channels of a row as they lie in memory, and as numbers
+template <int DT>
+struct RawChunk {
+  u32x4 w[DT == HTTM_FP32 ? 2 : 1];
+};
+template <int DT>
+__device__ __forceinline__ RawChunk<DT> load_chunk(const char* row, int chunk) {
+  RawChunk<DT> r;
+#pragma unroll
+  for (int i = 0; i < (DT == HTTM_FP32 ? 2 : 1); ++i) r.w[i] = ((const u32x4*)row)[DT == HTTM_FP32 ? 2 * chunk + i : chunk];
+  return r;
+}
+template <int DT>
+__device__ __forceinline__ void to_f32(const RawChunk<DT>& r, float (&x)[8]) {
+  if constexpr (DT == HTTM_FP32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(r.w[e >> 2][e & 3]);
+  } else if constexpr (DT == HTTM_FP16) {
+    const f32x8 y = __builtin_convertvector(__builtin_bit_cast(f16x8, r.w[0]), f32x8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = y[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = e & 1 ? bf16_hi(r.w[0][e >> 1]) : bf16_lo(r.w[0][e >> 1]);
+  }
+}
+__device__ __forceinline__ u32x4 pack_chunk(const float (&x)[8]) {
+  return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+}
+
+// Sum over the eight lanes of a row
+__device__ __forceinline__ float row_sum(float x) {
+  x += __shfl_xor(x, 1);
+  x += __shfl_xor(x, 2);
+  return x + __shfl_xor(x, 4);
+}
+
+// What a lane knows of its eight channels for all heads of its token
+struct LaneRope {
+  float cos[8], sin[8];   // sin carries the sign that the channel's partner enters with
+  int partner;            // lane that holds the other channel of the pairs (halves)
+  bool rotates;           // these channels are among the first rot_dim
+};
+
+__device__ __forceinline__ void make_rope(LaneRope& r, const NormRopeArgs& a, int64_t p, int lane, bool rotates, int in_axis) {
+  r.rotates = rotates;
+  const int half = a.axis_chunks >> 1;
+  const bool halves = a.pairing == HTTM_ROPE_HALVES;
+  const bool second = halves && in_axis >= half;
+  r.partner = !rotates || !halves ? lane : (second ? lane - half : lane + half);
+  const int first_pair = halves ? (second ? in_axis - half : in_axis) * 8 : in_axis * 4;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int pair = halves ? first_pair + e : first_pair + (e >> 1);
+    const uint64_t frac = (uint64_t)p * a.turn[rotates ? pair & (kMaxPairs - 1) : 0];
+    const float t = (float)(int32_t)(frac >> 32) * 2.3283064365386963e-10f;    // 2^-32
+    const float c = __builtin_amdgcn_cosf(t), s = __builtin_amdgcn_sinf(t);
+    const bool minus = halves ? !second : (e & 1) == 0;
+    r.cos[e] = c;
+    r.sin[e] = minus ? -s : s;
+  }
+}
+
+__device__ __forceinline__ void rotate(float (&x)[8], const LaneRope& r, bool halves) {
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = halves ? __shfl(x[e], r.partner) : x[e ^ 1];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = r.rotates ? fmaf(x[e], r.cos[e], y[e] * r.sin[e]) : x[e];
+}
+
+__device__ __forceinline__ void normalise(float (&x)[8], int norm, float eps, const float (&w)[8], const float (&b)[8]) {
+  if (norm == HTTM_NORM_LAYER) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += x[e];
+    const float mean = row_sum(s) * (1.f / kDHead);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] -= mean;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
+  const float scale = 1.f / sqrtf(row_sum(s) * (1.f / kDHead) + eps);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e] * scale, w[e], b[e]);
+}
+
+// Where a token of the batch belongs in the cache
+struct CachePlace {
+  bool real;          // of a sequence, not padding
+  bool in_cache;      // its row exists and has a page
+  int64_t row;        // in its sequence
+  int64_t page_row;   // page * H_kv * page_size + row in the page: add head * page_size
+};
+__device__ __forceinline__ CachePlace find_place(const NormRopeArgs& a, int64_t t, int lane) {
+  CachePlace c = {false, false, 0, 0};
+  // how many offsets are not above t: 64 at a time, one load for the whole wave
+  int below = 0;
+  const int n_off = a.cache.n_seqs + 1, mine = lane >> 3;
+  for (int i = 0; i < n_off; i += 64) {
+    const int off = i + lane < n_off ? a.offsets[i + lane] : INT32_MAX;
+#pragma unroll
+    for (int j = 0; j < kTokens; ++j) {
+      const int64_t tj = __shfl((int)t, 8 * j);
+      const int n = __popcll(__ballot(off <= tj));
+      below += mine == j ? n : 0;
+    }
+  }
+  const int b = below - 1;
+  if (t >= a.N || b < 0 || b >= a.cache.n_seqs) return c;
+  c.real = true;
+  const int64_t most = (int64_t)a.cache.table_stride << a.cache.page_shift;
+  const int64_t len = std::clamp<int64_t>(a.seq_lens[b], 0, most);
+  c.row = len - a.offsets[b + 1] + t;
+  if (c.row < 0 || c.row >= most) return c;
+  const int64_t page = a.cache.table[(int64_t)b * a.cache.table_stride + (c.row >> a.cache.page_shift)];
+  if (page < 0 || page >= a.cache.n_pages) return c;
+  c.in_cache = true;
+  c.page_row = ((page * a.cache.H_kv) << a.cache.page_shift) + (c.row & ((1 << a.cache.page_shift) - 1));
+  return c;
+}
+
+template <int DT, bool APPEND>
+__global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeArgs a, int slots_per_wave) {
+  const int lane = threadIdx.x & 63, chunk = lane & 7;
+  const int64_t t = (int64_t)blockIdx.x * kTokens + (lane >> 3);
+  const int n_slots = a.H[0] + a.H[1] + a.H[2];
+  const int s0 = (blockIdx.y * kWaves + (threadIdx.x >> 6)) * slots_per_wave;
+  const int s1 = s0 + slots_per_wave < n_slots ? s0 + slots_per_wave : n_slots;
+  if (s0 >= s1) return;
+  constexpr int kBytes = DT == HTTM_FP32 ? 4 : 2;
+  const int64_t tt = t < a.N ? t : a.N - 1;     // lanes of no token read the last one and write nothing
+
+  auto which = [&](int s, int& head) {
+    const int part = s < a.H[0] ? 0 : (s < a.H[0] + a.H[1] ? 1 : 2);
+    head = s - (part > 0 ? a.H[0] : 0) - (part > 1 ? a.H[1] : 0);
+    return part;
+  };
+  auto source = [&](int s) {
+    int head;
+    const TokenRows& r = a.src[which(s, head)];
+    return r.data + (tt * r.token_stride + head * r.head_stride) * kBytes;
+  };
+  RawChunk<DT> next = load_chunk<DT>(source(s0), chunk);
+
+  CachePlace place = {true, false, 0, 0};
+  if constexpr (APPEND) place = find_place(a, t, lane);
+  const bool write = t < a.N && place.real;
+
+  LaneRope rope = {};
+  const bool turns = a.axes > 0 && s0 < a.H[0] + a.H[1];
+  const bool halves = a.pairing == HTTM_ROPE_HALVES;
+  if (turns) {
+    int axis = 0, in_axis = chunk;
+    while (axis < a.axes && in_axis >= a.axis_chunks) in_axis -= a.axis_chunks, ++axis;
+    const bool rotates = axis < a.axes;
+    int64_t p = 0;
+    if (rotates) p = a.pos ? (int64_t)a.pos[tt * a.axes + axis] : a.first_pos + place.row;
+    make_rope(rope, a, p, lane, rotates, rotates ? in_axis : 0);
+  }
+  float w[8], b[8];
+  int have = -1;
+  for (int s = s0; s < s1; ++s) {
+    const RawChunk<DT> raw = next;
+    if (s + 1 < s1) next = load_chunk<DT>(source(s + 1), chunk);
+    int head;
+    const int part = which(s, head);
+    u32x4 packed;
+    if (part == 2 && DT == HTTM_BF16) {
+      packed = raw.w[0];
+    } else {
+      float x[8];
+      to_f32<DT>(raw, x);
+      if (part < 2) {
+        if (a.norm != HTTM_NORM_NONE) {
+          if (have != part) {
+            have = part;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              w[e] = a.weight[part] ? a.weight[part][chunk * 8 + e] : 1.f;
+              b[e] = a.bias[part] ? a.bias[part][chunk * 8 + e] : 0.f;
+            }
+          }
+          normalise(x, a.norm, a.eps, w, b);
+        }
+        if (turns) rotate(x, rope, halves);
+        if (part == 1) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= a.k_scale;
+        }
+      }
+      packed = pack_chunk(x);
+    }
+    if (!write) continue;
+    if constexpr (APPEND) {
+      if (part == 0) {
+        ((u32x4*)(a.out[0] + (t * a.H[0] + head) * kRowBytes))[chunk] = packed;
+      } else if (place.in_cache) {
+        char* pages = part == 1 ? a.cache.k_pages : a.cache.v_pages;
+        ((u32x4*)(pages + (place.page_row + ((int64_t)head << a.cache.page_shift)) * kRowBytes))[chunk] = packed;
+      }
+    } else {
+      ((u32x4*)(a.out[part] + ((int64_t)head * a.N + t) * kRowBytes))[chunk] = packed;
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, bool append, hipStream_t stream) {
+  const int n_slots = a.H[0] + a.H[1] + a.H[2];
+  if (a.N == 0 || n_slots == 0) return hipSuccess;
+  const int64_t groups = (a.N + kTokens - 1) / kTokens;
+  // Heads a wave takes one after the other: as many as leave 8 waves for every SIMD, at most a workgroup's share of all
+  const int64_t most = (n_slots + kWaves - 1) / kWaves;
+  const int64_t per = std::max<int64_t>(1, std::min(most, groups * n_slots / 8192));
+  const dim3 grid((unsigned)groups, (unsigned)((n_slots + kWaves * per - 1) / (kWaves * per)));
+#define HTTM_ROWS(DT)                                                                             \
+  if (append)                                                                                     \
+    hipLaunchKernelGGL((norm_rope_kernel<DT, true>), grid, dim3(64 * kWaves), 0, stream, a, (int)per); \
+  else                                                                                            \
+    hipLaunchKernelGGL((norm_rope_kernel<DT, false>), grid, dim3(64 * kWaves), 0, stream, a, (int)per)
+  if (dtype == HTTM_BF16) {
+    HTTM_ROWS(HTTM_BF16);
+  } else if (dtype == HTTM_FP16) {
+    HTTM_ROWS(HTTM_FP16);
+  } else {
+    HTTM_ROWS(HTTM_FP32);
+  }
+#undef HTTM_ROWS
+  return hipGetLastError();
+}
+
+}  // namespace httm

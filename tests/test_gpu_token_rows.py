@@ -1,0 +1,263 @@
+"""qk_norm_rope and cache_append against the formulas in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2511_21317_amd as httm
+
+pytestmark = pytest.mark.gpu
+
+D = 64
+DTYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+def formula(x, norm, w, b, eps, axes, rot_dim, pairing, base, pos, k_scale=1.0):
+    """What a row becomes, in 64 bits, and how far fp32 arithmetic with one rounding to bf16 may be off."""
+    x = x.double()
+    peak = x.abs().amax(-1, keepdim=True)
+    slip = torch.zeros_like(peak)
+    if norm != "none":
+        if norm == "layer":
+            x = x - x.mean(-1, keepdim=True)
+        r = torch.rsqrt((x * x).mean(-1, keepdim=True) + eps)
+        x = x * r
+        # sums of 64 terms and their products: 64 roundings of 2^-24, relative to the largest term
+        slip = 64 * 2.0 ** -24 * (peak * r + x.abs().amax(-1, keepdim=True))
+        if w is not None:
+            x, slip = x * w.double(), slip * w.abs().max().double()
+        if b is not None:
+            x = x + b.double()
+    y = x.clone()
+    size = x.abs()
+    if axes:
+        width = rot_dim // axes
+        for a in range(axes):
+            i = torch.arange(width // 2, device=x.device)
+            t = pos[:, a].double()[:, None, None] * base ** (-2.0 * i.double() / width)
+            first, second = (i, i + width // 2) if pairing == "halves" else (2 * i, 2 * i + 1)
+            u, v = x[..., a * width + first], x[..., a * width + second]
+            y[..., a * width + first] = u * torch.cos(t) - v * torch.sin(t)
+            y[..., a * width + second] = v * torch.cos(t) + u * torch.sin(t)
+            for idx in (first, second):
+                size[..., a * width + idx] = u.abs() + v.abs()
+    # rounding to bf16: half a step, 2^-8 of the value; sine and cosine to 2^-18, and 2^-21 for the angle's own fp32
+    tol = (2.0 ** -8 * y.abs() + 2.0 ** -17 * size + 2 * slip) * abs(k_scale)
+    return y * k_scale, tol + 1e-30
+
+
+def check(got, ref, tol, what):
+    bad = (got.double() - ref).abs() > tol
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst {((got.double() - ref).abs() / tol).max():.2f} times"
+
+
+def affine(norm, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    kw = {}
+    if norm != "none":
+        kw = {n: 1 + 0.3 * torch.randn(D, generator=g, device="cuda") for n in ("q_weight", "k_weight")}
+    if norm == "layer":
+        kw |= {n: 0.2 * torch.randn(D, generator=g, device="cuda") for n in ("q_bias", "k_bias")}
+    return kw
+
+
+def positions(N, axes, far, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    p = torch.randint(-far, far, (N, max(1, axes)), generator=g, device="cuda", dtype=torch.int64)
+    p[0] = 0
+    if far > 1 << 20:
+        p[-1] = 2**31 - 1
+    return p.to(torch.int32)[:, :axes].contiguous() if axes else None
+
+
+@pytest.mark.parametrize("norm,axes,rot_dim,pairing,base", [
+    ("layer", 2, 64, "halves", 100.0), ("rms", 1, 64, "halves", 10000.0), ("rms", 1, 48, "neighbours", 500000.0),
+    ("none", 3, 48, "halves", 10000.0), ("layer", 3, 48, "neighbours", 100.0), ("rms", 1, 16, "halves", 10000.0), ("none", 2, 32, "neighbours", 100.0),
+    ("layer", 0, 64, "halves", 100.0), ("none", 0, 0, "halves", 1.0)])
+@pytest.mark.parametrize("N,H_q,H_kv,dtype,far", [(1, 1, 1, "bf16", 40), (13, 6, 2, "fp32", 2**31 - 1), (261, 16, 16, "bf16", 5000),
+                                                  (1003, 5, 3, "fp16", 2**31 - 1)])
+def test_norm_rope(norm, axes, rot_dim, pairing, base, N, H_q, H_kv, dtype, far):
+    torch.manual_seed(N + H_q)
+    x = (torch.randn(N, H_q + 2 * H_kv, D, device="cuda") * 1.7 + 0.8).to(DTYPES[dtype])
+    q, k, v = x[:, :H_q], x[:, H_q:H_q + H_kv], x[:, H_q + H_kv:]
+    kw = affine(norm, 5)
+    nr = httm.NormRope(norm=norm, eps=1e-5, axes=axes, rot_dim=rot_dim, pairing=pairing, base=base, k_scale=0.18, **kw)
+    pos = positions(N, axes, far, 9)
+    out = [torch.full((H, N, D), float("nan"), dtype=torch.bfloat16, device="cuda") for H in (H_q, H_kv, H_kv)]
+    httm.qk_norm_rope(nr, q, k, v, pos, *out)
+    for name, t, got, scale in (("q", q, out[0], 1.0), ("k", k, out[1], float(torch.tensor(0.18, dtype=torch.float32)))):
+        ref, tol = formula(t, norm, kw.get(name + "_weight"), kw.get(name + "_bias"), 1e-5, axes, rot_dim, pairing, base, pos, scale)
+        check(got.transpose(0, 1), ref, tol, name)
+    assert torch.equal(out[2].transpose(0, 1), v.to(torch.bfloat16))
+
+
+def test_norm_rope_takes_any_strides_and_parts():
+    torch.manual_seed(3)
+    N, H = 77, 4
+    nr = httm.NormRope(norm="rms", axes=1, base=10000.0)
+    pos = positions(N, 1, 3000, 2)
+    want = [torch.empty(H, N, D, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    q, k, v = (torch.randn(N, H, D, device="cuda").bfloat16() for _ in range(3))
+    httm.qk_norm_rope(nr, q, k, v, pos, *want)
+    # head-major sources, rows with room between them, a head that is broadcast
+    wide = torch.randn(N, 2 * H, 2 * D, device="cuda").bfloat16()
+    wide[:, ::2, :D] = q
+    headwise = k.transpose(0, 1).contiguous().transpose(0, 1)
+    one = v[:, :1].expand(N, H, D)
+    got = [torch.empty_like(t) for t in want]
+    httm.qk_norm_rope(nr, wide[:, ::2, :D], headwise, one, pos, *got)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(got[2], want[2][:1].expand_as(got[2]))
+    alone = torch.empty_like(want[1])
+    httm.qk_norm_rope(nr, None, k, None, pos, None, alone, None)
+    assert torch.equal(alone, want[1])
+    httm.qk_norm_rope(nr, None, None, v, None, None, None, alone)
+    assert torch.equal(alone, want[2])
+    with pytest.raises(httm.HttmError):
+        httm.qk_norm_rope(nr, q, k, v, None, *got)
+    with pytest.raises(httm.HttmError):
+        httm.qk_norm_rope(nr, q, k, v, pos[:-1], *got)
+    with pytest.raises(httm.HttmError):
+        httm.qk_norm_rope(nr, q, k[:-1], v, pos, *got)
+    with pytest.raises(httm.HttmError):
+        httm.qk_norm_rope(nr, q.transpose(1, 2).contiguous().transpose(1, 2), k, v, pos, *got)
+
+
+def test_norm_rope_feeds_the_layer():
+    """Rows of a projection through norm, rotation and the layer, as a scene goes: the same as the layer on tensors in which norm
+    and rotation were taken apart."""
+    from perf.cases import _geom, _layer
+    case = _layer("x", S=3, Hp=9, Wp=11, b=4, T=2, rho_q=0.5, rho_kv=0.5, H=4)
+    plan = httm.Plan(_geom(case))
+    torch.manual_seed(1)
+    qkv = torch.randn(plan.N, 3, 4, D, device="cuda").bfloat16()
+    kw = affine("layer", 7)
+    nr = httm.NormRope(norm="layer", axes=2, base=100.0, **kw)
+    slot = torch.arange(plan.N, device="cuda") % (9 * 11 + 5) - 5
+    pos = torch.stack([torch.where(slot < 0, 0, slot // 11 + 1), torch.where(slot < 0, 0, slot % 11 + 1)], 1).to(torch.int32).contiguous()
+    q, k, v = (torch.empty(4, plan.N, D, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    httm.qk_norm_rope(nr, qkv[:, 0], qkv[:, 1], qkv[:, 2], pos, q, k, v)
+    for name, i, got in (("q", 0, q), ("k", 1, k)):
+        ref, tol = formula(qkv[:, i], "layer", kw[name + "_weight"], kw[name + "_bias"], 1e-6, 2, 64, "halves", 100.0, pos)
+        check(got.transpose(0, 1), ref, tol, name)
+    out = torch.empty(plan.N, 4 * D, dtype=torch.bfloat16, device="cuda")
+    httm.layer_forward(plan, q, k, v, out, httm.alloc_workspace(plan))
+    apart = [t.transpose(0, 1).contiguous().transpose(0, 1).contiguous() for t in (q, k, v)]
+    again = torch.empty_like(out)
+    httm.layer_forward(plan, *apart, again, httm.alloc_workspace(plan))
+    assert torch.equal(out, again) and torch.isfinite(out.float()).all()
+
+
+def make_cache(lens, page, H_kv, seed, spare=3, extra=1):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    need = [-(-n // page) for n in lens]
+    order = torch.randperm(sum(need) + spare, generator=g, device="cuda").to(torch.int32)
+    table = torch.full((len(lens), max(need + [0]) + extra), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    k, v = (torch.randn(order.numel(), H_kv, page, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    return httm.PagedCache(k, v, table)
+
+
+@pytest.mark.parametrize("new,lens,page,H_q,H_kv,dtype", [
+    ([1], [1], 16, 1, 1, "bf16"), ([1] * 9, [1, 17, 16, 15, 32, 33, 64, 300, 2], 16, 8, 2, "bf16"), ([5, 0, 40, 1, 200], [5, 7, 100, 65, 231], 64, 6, 3, "fp32"),
+    ([130, 3], [130, 131], 32, 4, 4, "fp16"), ([3] * 70, [9 + 5 * i for i in range(70)], 128, 2, 1, "bf16")])
+@pytest.mark.parametrize("given_pos", [True, False])
+def test_append(new, lens, page, H_q, H_kv, dtype, given_pos):
+    pad_front, pad = 2, 11
+    n = pad_front + sum(new) + pad
+    torch.manual_seed(n)
+    x = torch.randn(n, H_q + 2 * H_kv, D, device="cuda").to(DTYPES[dtype])
+    q, k, v = x[:, :H_q], x[:, H_q:H_q + H_kv], x[:, H_q + H_kv:]
+    kw = affine("rms", 3)
+    nr = httm.NormRope(norm="rms", axes=1, rot_dim=64, base=10000.0, **kw)
+    cache = make_cache(lens, page, H_kv, 1)
+    want_k, want_v = cache.k_pages.double(), cache.v_pages.double()
+    off = [pad_front]
+    for a in new:
+        off.append(off[-1] + a)
+    offsets = torch.tensor(off, dtype=torch.int32, device="cuda")
+    seq_lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    first = 100000
+    row = torch.zeros(n, dtype=torch.int64, device="cuda")
+    seq = torch.full((n,), -1, dtype=torch.int64)
+    for b, a in enumerate(new):
+        row[off[b]:off[b + 1]] = torch.arange(lens[b] - a, lens[b], device="cuda")
+        seq[off[b]:off[b + 1]] = b
+    pos = positions(n, 1, 2**31 - 1, 4) if given_pos else (first + row)[:, None].to(torch.int32)
+    q_out = torch.full((n, H_q, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    httm.cache_append(nr, q, k, v, pos if given_pos else None, cache, offsets, seq_lens, q_out, first_pos=first)
+    ref_q, tol_q = formula(q, "rms", kw["q_weight"], None, 1e-6, 1, 64, "halves", 10000.0, pos)
+    ref_k, tol_k = formula(k, "rms", kw["k_weight"], None, 1e-6, 1, 64, "halves", 10000.0, pos)
+    real = slice(pad_front, n - pad)
+    check(q_out[real], ref_q[real], tol_q[real], "q")
+    assert (q_out[:pad_front] == 7).all() and (q_out[n - pad:] == 7).all()
+    tol = torch.zeros_like(want_k)
+    table = cache.page_table.cpu()
+    for t in range(pad_front, n - pad):
+        r = int(row[t])
+        p = int(table[seq[t], r // page])
+        want_k[p, :, r % page], tol[p, :, r % page] = ref_k[t], tol_k[t]
+        want_v[p, :, r % page] = v[t].to(torch.bfloat16).double()
+    check(cache.k_pages, want_k, tol, "k pages")          # tolerance 0 where nothing was to be written
+    assert torch.equal(cache.v_pages.double(), want_v)
+
+
+def test_append_leaves_what_has_no_place():
+    """Rows before the first, pages that are none, lengths beyond the table: the queries still come, the cache keeps."""
+    H, page = 2, 16
+    cache = make_cache([40, 16, 20], page, H, 8, extra=0)
+    cache.page_table[0, 1] = -1
+    cache.page_table[2, 0] = cache.k_pages.shape[0]
+    before = cache.k_pages.clone()
+    # 20 new tokens of length 12: eight have no row; a length of 1000 counts as the table's 48 rows
+    offsets = torch.tensor([0, 20, 40, 45], dtype=torch.int32, device="cuda")
+    seq_lens = torch.tensor([1000, 12, 20], dtype=torch.int32, device="cuda")
+    x = torch.randn(45, H, D, device="cuda").bfloat16()
+    nr = httm.NormRope(norm="none", axes=0)
+    q_out = torch.zeros_like(x)
+    httm.cache_append(nr, x, x, x, None, cache, offsets, seq_lens, q_out)
+    assert torch.equal(q_out, x)
+    want = before.clone()
+    for t in range(45):
+        b = 0 if t < 20 else 1 if t < 40 else 2
+        r = [48, 12, 20][b] - [20, 40, 45][b] + t
+        if r < 0 or not 0 <= int(cache.page_table[b, r // page]) < want.shape[0]:
+            continue
+        want[int(cache.page_table[b, r // page]), :, r % page] = x[t]
+    assert torch.equal(cache.k_pages, want) and not torch.equal(want, before)
+
+
+def test_append_on_another_stream_and_in_a_graph():
+    """A captured append follows the lengths on the device: replays after the first write where the sequences have got to."""
+    H, page, B = 3, 16, 5
+    cache = make_cache([60] * B, page, H, 2)
+    eager = httm.PagedCache(cache.k_pages.clone(), cache.v_pages.clone(), cache.page_table)
+    nr = httm.NormRope(norm="rms", axes=1, base=10000.0)
+    offsets = torch.arange(B + 1, dtype=torch.int32, device="cuda")
+    seq_lens = torch.tensor([1, 16, 17, 30, 40], dtype=torch.int32, device="cuda")
+    x = torch.randn(B, 3 * H, D, device="cuda").bfloat16()
+    q_out = torch.empty(B, H, D, dtype=torch.bfloat16, device="cuda")
+    args = (x[:, :H], x[:, H:2 * H], x[:, 2 * H:], None)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        httm.cache_append(nr, *args, cache, offsets, seq_lens, q_out)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            httm.cache_append(nr, *args, cache, offsets, seq_lens, q_out)
+    torch.cuda.synchronize()
+    want = torch.empty_like(q_out)
+    httm.cache_append(nr, *args, eager, offsets, seq_lens, want)
+    for step in range(4):
+        x.copy_(torch.randn_like(x))
+        graph.replay()
+        httm.cache_append(nr, *args, eager, offsets, seq_lens, want)
+        torch.cuda.synchronize()
+        assert torch.equal(q_out, want) and torch.equal(cache.k_pages, eager.k_pages) and torch.equal(cache.v_pages, eager.v_pages)
+        seq_lens += 1
