@@ -100,22 +100,44 @@ struct Seq {
   int units;       // of a tile, at least one: rows without keys are written too
 };
 template <int R>
-__device__ __forceinline__ Seq sequence(const LineArgs& a, int b) {
-  const CachedAttnArgs& c = a.c;
-  Seq s;
-  const int T = (int)c.n_tokens;
-  const int o0 = c.offsets[b], o1 = c.offsets[a.stacked ? c.cache.n_seqs : b + 1];
-  s.first = std::clamp(o0, 0, T);
-  s.n = std::clamp(o1, s.first, T) - s.first;
-  s.len = 0;
-  if (a.with_own) {
-    const int64_t most = (int64_t)c.cache.table_stride << c.cache.page_shift;
-    s.len = (int)std::clamp<int64_t>(c.seq_lens[b], 0, most);
-  }
-  const int keys = (a.with_prefix ? ((int)c.P + kUnit - 1) / kUnit : 0) + (int)(((int64_t)s.len + kUnit - 1) / kUnit);
-  s.tiles = (int)(((int64_t)s.n * c.group + R - 1) / R);
+__device__ __forceinline__ void count(const LineArgs& a, Seq& s) {
+  const int keys = (a.with_prefix ? ((int)a.c.P + kUnit - 1) / kUnit : 0) + (s.len + kUnit - 1) / kUnit;
+  s.tiles = (s.n * a.c.group + R - 1) / R;
   s.units = keys > 1 ? keys : 1;
+}
+// 64 sequences from `base` on, one per lane; those behind the last have no tokens
+template <int R>
+__device__ __forceinline__ Seq load_window(const LineArgs& a, int base, int lane) {
+  const CachedAttnArgs& c = a.c;
+  const int n_seq = a.stacked ? 1 : c.cache.n_seqs, b = base + lane, T = (int)c.n_tokens;
+  Seq s = {};
+  if (b < n_seq) {
+    const int o0 = c.offsets[b], o1 = c.offsets[a.stacked ? c.cache.n_seqs : b + 1];
+    const int len = a.with_own ? c.seq_lens[b] : 0;
+    s.first = std::clamp(o0, 0, T);
+    s.n = std::clamp(o1, s.first, T) - s.first;
+    s.len = std::clamp(len, 0, c.cache.table_stride << c.cache.page_shift);
+  }
+  count<R>(a, s);
   return s;
+}
+template <int R>
+__device__ __forceinline__ Seq of_lane(const LineArgs& a, const Seq& window, int l) {
+  Seq s;
+  s.first = __builtin_amdgcn_readlane(window.first, l);
+  s.n = __builtin_amdgcn_readlane(window.n, l);
+  s.len = __builtin_amdgcn_readlane(window.len, l);
+  count<R>(a, s);
+  return s;
+}
+
+// floor(x / y) for 0 <= x, 0 < y, both below 2^52: the compiler's 64-bit division takes some 200 instructions, in front of
+// everything else that a workgroup does
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  int64_t q = (int64_t)((double)x / (double)y);
+  const int64_t r = x - q * y;
+  q += r < 0 ? -1 : (r >= y ? 1 : 0);
+  return uniform64(q);
 }
 
 // Where a share starts
@@ -123,72 +145,71 @@ struct Place {
   int h, b, tile, unit;
   int tile_id;      // of (h, b, tile) in the line
   int64_t at, end;  // units of the share, as positions on the line
-  int64_t total, shares;
   int64_t per_share, longer;    // units of a share; the first `longer` shares have one more
   int share;
+  int base;         // first sequence of the window
   // the share that has unit x of the line
   __device__ __forceinline__ int share_of(int64_t x) const {
     const int64_t split = longer * (per_share + 1);
-    return (int)(x < split ? x / (per_share + 1) : longer + (x - split) / per_share);
+    return (int)(x < split ? quotient(x, per_share + 1) : longer + quotient(x - split, per_share));
   }
 };
 template <int R>
-__device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p) {
+__device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p, Seq& window) {
   const int n_seq = a.stacked ? 1 : a.c.cache.n_seqs;
-  int64_t sum = 0;
-  int tiles = 0;
-  for (int i = lane; i < n_seq; i += 64) {
-    const Seq s = sequence<R>(a, i);
+  const int lanes = n_seq < 64 ? n_seq : 64;
+  window = load_window<R>(a, 0, lane);
+  int64_t sum = (int64_t)window.tiles * window.units;
+  int tiles = window.tiles;
+  for (int i = 64; i < n_seq; i += 64) {
+    const Seq s = load_window<R>(a, i, lane);
     sum += (int64_t)s.tiles * s.units;
     tiles += s.tiles;
   }
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) {
+  for (int i = 1; i < lanes; i <<= 1) {
     sum += __shfl_xor(sum, i);
     tiles += __shfl_xor(tiles, i);
   }
   const int64_t per_head = uniform64(sum);
   const int tiles_per_head = uniform(tiles);
   if (per_head == 0) return false;
-  p.total = per_head * a.c.cache.H_kv;
-  p.shares = std::clamp<int64_t>(p.total / a.min_units, 1, gridDim.x);
+  const int64_t total = per_head * a.c.cache.H_kv;
+  const int shares = (int)std::clamp<int64_t>(quotient(total, a.min_units), 1, gridDim.x);
   // workgroups go to the 8 XCDs in turn: shares next to each other, which read the same keys, go to one of them
-  const int per_xcd = (int)((p.shares + 7) / 8);
+  const int per_xcd = (shares + 7) / 8;
   p.share = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_xcd || p.share >= p.shares) return false;
-  p.per_share = p.total / p.shares;
-  p.longer = p.total % p.shares;
+  if ((int)(blockIdx.x >> 3) >= per_xcd || p.share >= shares) return false;
+  p.per_share = quotient(total, shares);
+  p.longer = total - p.per_share * shares;
   p.at = p.share * p.per_share + std::min<int64_t>(p.share, p.longer);
   p.end = p.at + p.per_share + (p.share < p.longer ? 1 : 0);
-  p.h = (int)(p.at / per_head);
+  p.h = (int)quotient(p.at, per_head);
   int64_t rest = p.at - p.h * per_head;
   int before = 0;
-  for (int i = 0;; i += 64) {
-    Seq s = {};
-    if (i + lane < n_seq) s = sequence<R>(a, i + lane);
-    int64_t scan = (int64_t)s.tiles * s.units;
-    int tscan = s.tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
+  for (p.base = 0;; p.base += 64) {
+    if (p.base > 0) window = load_window<R>(a, p.base, lane);
+    int64_t scan = (int64_t)window.tiles * window.units;
+    int tscan = window.tiles;
+    for (int d = 1; d < lanes; d <<= 1) {
       const int64_t v = __shfl_up(scan, d);
       const int tv = __shfl_up(tscan, d);
       scan += lane >= d ? v : 0;
       tscan += lane >= d ? tv : 0;
     }
-    const uint64_t in = __ballot(rest < scan);
-    if (in == 0 && i + 64 < n_seq) {
+    const uint64_t in = __ballot(lane < lanes && rest < scan);
+    if (in == 0) {
+      if (p.base + 64 >= n_seq) return false;
       rest -= uniform64(__shfl(scan, 63));
       before += uniform(__shfl(tscan, 63));
       continue;
     }
-    if (in == 0) return false;
     const int l = __builtin_ctzll(in);
-    const int units = uniform(__shfl(s.units, l)), n_tiles = uniform(__shfl(s.tiles, l));
-    rest -= uniform64(__shfl(scan, l)) - (int64_t)n_tiles * units;
-    p.b = i + l;
-    p.tile = (int)(rest / units);
-    p.unit = (int)(rest - (int64_t)p.tile * units);
-    p.tile_id = p.h * tiles_per_head + before + uniform(__shfl(tscan, l)) - n_tiles + p.tile;
+    const Seq s = of_lane<R>(a, window, l);
+    rest -= uniform64(__shfl(scan, l)) - (int64_t)s.tiles * s.units;
+    p.b = p.base + l;
+    p.tile = (int)quotient(rest, s.units);
+    p.unit = (int)(rest - (int64_t)p.tile * s.units);
+    p.tile_id = p.h * tiles_per_head + before + uniform(__shfl(tscan, l)) - s.tiles + p.tile;
     return true;
   }
 }
@@ -215,28 +236,37 @@ struct WaveState {
   bf16x8 qf[NQ][2];     // Q^T, 32 channels each
   f32x4 o[4][NQ];       // O^T, 16 channels each
   float m[NQ], l[NQ];   // shift in log2 units, sum over the lane's keys
-  int limit[NQ];        // own keys that the lane's row sees
+  int limit[NQ];        // causal: own keys that the lane's row sees
 };
 
-// One unit of keys on its way: where its two halves of 16 rows are
-struct UnitRows {
-  const char* k[2];
-  const char* v[2];
-  int last[2];      // last row of the half that may be read
-  int row0, end;    // first key, and how many there are in all
-  bool own;
-  int ok;           // bit per half: it has a page
-};
+// One unit of keys on its way to a wave
 struct UnitData {
   u32x4 k[4];       // [key half * 2 + channel half]: the A operands
   u32x4 v[4];       // 8 rows each
 };
 
+// Rows of K or V: 16 from `at` on, of which the first `n` are there; the others are read as zeros, wherever they would be
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_rows(const char* at, int n) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, n * kRowBytes, kRawBufferWord3);
+}
+__device__ __forceinline__ u32x4 load_row(__amdgpu_buffer_rsrc_t rows, int offset) {
+  return __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 0, 0);
+}
+
+// Whether some value of a lane's V rows is an infinity or NaN
+__device__ __forceinline__ bool not_finite(const u32x4 (&v)[4]) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= (v[i][e] & 0x7F80u) == 0x7F80u || (v[i][e] & 0x7F800000u) == 0x7F800000u;
+  return bad;
+}
 // Weights times V where a row must not see a key whose V is not finite: 0 * inf would reach it.  Key by key, each
 // added where it is seen.
 template <int NQ>
 __device__ __forceinline__ void add_seen(f32x4 (&o)[4][NQ], const bf16x8 (&av)[4], const bf16x8 (&p)[NQ], const int (&limit)[NQ], int row0,
-                                                   int lane) {
+                                         int lane) {
   const int grp = lane >> 4;
 #pragma unroll 1
   for (int j = 0; j < kUnit; ++j) {
@@ -259,25 +289,14 @@ __device__ __forceinline__ void add_seen(f32x4 (&o)[4][NQ], const bf16x8 (&av)[4
   }
 }
 
-template <int NQ>
-__device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitRows& u, UnitData& d, bf16_t* sv, float c, int least, bool causal,
+// Scores, statistics and product of a unit.  row0: its first key; end: keys from there on are masked in all rows (causal
+// own keys: in some); ok: bit per half of 16 keys, whether it has a page.
+template <int NQ, bool CAUSAL>
+__device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, bf16_t* sv, float c, int row0, int end, int ok, bool own,
                                           int lane) {
   const int l16 = lane & 15, grp = lane >> 4;
-  const bool masked = u.ok != 3 || u.row0 + kUnit > (u.own ? least : u.end);
-  bool wild = false;
-  if (masked) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (u.row0 + 8 * i + (lane >> 3) >= u.end || !((u.ok >> (i >> 1)) & 1)) d.v[i] = u32x4{0, 0, 0, 0};
-    if (u.own && causal) {
-      bool bad = false;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= (d.v[i][e] & 0x7F80u) == 0x7F80u || (d.v[i][e] & 0x7F800000u) == 0x7F800000u;
-      wild = __ballot(bad) != 0;
-    }
-  }
+  const bool masked = ok != 3 || row0 + kUnit > end;
+  const bool wild = CAUSAL && masked && own && __ballot(not_finite(d.v)) != 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = 8 * i + (lane >> 3);
@@ -294,12 +313,12 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitRows& u, U
   if (masked) {
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
-      const int limit = u.own ? w.limit[qt] : u.end;
+      const int limit = (CAUSAL && own ? w.limit[qt] : end) - row0 - 4 * grp;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (u.row0 + 16 * kt + 4 * grp + r >= limit || !((u.ok >> kt) & 1)) s[kt][qt][r] = -__builtin_inff();
+          if (16 * kt + r >= limit || !((ok >> kt) & 1)) s[kt][qt][r] = -__builtin_inff();
     }
   }
   float top[NQ];
@@ -337,8 +356,8 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitRows& u, U
   bf16x8 av[4];
   load_v_operands(av, sv, l16, grp);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (__builtin_expect(wild, 0)) {
-    add_seen<NQ>(w.o, av, p, w.limit, u.row0, lane);
+  if (CAUSAL && __builtin_expect(wild, 0)) {
+    add_seen<NQ>(w.o, av, p, w.limit, row0, lane);
   } else {
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct)
@@ -347,9 +366,13 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitRows& u, U
   }
 }
 
-template <int NQ, int KS>
-__global__ __launch_bounds__(64 * KS) void attention_cached_kernel(const LineArgs a) {
+constexpr int waves_per_simd(int nq) { return nq == 1 ? 3 : 2; }
+
+template <int NQ, int KS, bool CAUSAL>
+__global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_per_simd(NQ), waves_per_simd(NQ)))) void attention_cached_kernel(
+    const LineArgs a) {
   constexpr int R = 16 * NQ;
+  constexpr int DEPTH = 1;     // units of a wave on their way besides the one in work
   __shared__ __attribute__((aligned(16))) char s_mem[KS * kUnitBytes];
   __shared__ float2 s_ml[KS > 1 ? KS : 1][R];
   const CachedAttnArgs& c = a.c;
@@ -357,69 +380,74 @@ __global__ __launch_bounds__(64 * KS) void attention_cached_kernel(const LineArg
   const int l16 = lane & 15, grp = lane >> 4;
   bf16_t* sv = (bf16_t*)(s_mem + wave * kUnitBytes);
   Place p;
-  if (!find_share<R>(a, lane, p)) return;
-  Seq s = sequence<R>(a, p.b);
+  Seq window;
+  if (!find_share<R>(a, lane, p, window)) return;
+  Seq s = of_lane<R>(a, window, p.b - p.base);
   const int prefix_units = a.with_prefix ? ((int)c.P + kUnit - 1) / kUnit : 0;
   const int64_t share_start = p.at;
+  const int k_offset = l16 * kRowBytes + grp * 16, v_offset = lane * 16;
 
   while (p.at < p.end) {
     const int u0 = p.unit;
     const int u1 = (int)std::min<int64_t>(s.units, p.unit + (p.end - p.at));
     const int n_rows = s.n * c.group, r0 = p.tile * R;
-    const int32_t* table = c.cache.table + (int64_t)p.b * c.cache.table_stride;
+    // (constant memory: scalar loads, which are waited for apart from those of the keys)
+    const auto* table = (const __attribute__((address_space(4))) int32_t*)(c.cache.table + (int64_t)p.b * c.cache.table_stride);
 
-    auto locate = [&](int unit) {
-      UnitRows u;
-      u.own = unit >= prefix_units;
-      u.ok = 3;
-      u.row0 = (u.own ? unit - prefix_units : unit) * kUnit;
-      if (!u.own) {
-        u.end = (int)c.P;
+    // Pages of a unit's two halves, asked for well before its rows; a prefix needs none
+    struct Pages {
+      int page[2];
+    };
+    auto look_up = [&](int unit) {
+      Pages g = {{0, 0}};
+      if (unit >= prefix_units) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int first = std::min(u.row0 + 16 * i, u.end - 1);
-          const int64_t at = (p.h * c.P + first) * kRowBytes;
-          u.k[i] = c.k_prefix + at;
-          u.v[i] = c.v_prefix + at;
-          u.last[i] = std::min(15, u.end - 1 - first);
-        }
-      } else {
-        u.end = s.len;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int row = u.row0 + 16 * i;
-          const int index = row >> c.cache.page_shift;
-          int64_t page = index < c.cache.table_stride ? table[index] : -1;
-          if (page < 0 || page >= c.cache.n_pages) {
-            page = 0;
-            u.ok &= ~(1 << i);
-          }
-          const int64_t at = (((page * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
-          u.k[i] = c.cache.k_pages + at;
-          u.v[i] = c.cache.v_pages + at;
-          u.last[i] = 15;
+          const int index = ((unit - prefix_units) * kUnit + 16 * i) >> c.cache.page_shift;
+          g.page[i] = index < c.cache.table_stride ? table[index] : -1;
         }
       }
-      return u;
+      return g;
     };
-    auto fetch = [&](const UnitRows& u, UnitData& d) {
+    // Requests a unit's rows; returns its ok bits
+    auto fetch = [&](int unit, const Pages& g, UnitData& d) {
+      int ok = 3;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int i = 0; i < 2; ++i) {
+        const char *k, *v;
+        int n;
+        if (unit < prefix_units) {
+          const int row = unit * kUnit + 16 * i;
+          const int64_t at = (p.h * c.P + row) * kRowBytes;
+          k = c.k_prefix + at;
+          v = c.v_prefix + at;
+          n = (int)c.P - row;
+        } else {
+          const int row = (unit - prefix_units) * kUnit + 16 * i;
+          const bool there = g.page[i] >= 0 && g.page[i] < c.cache.n_pages;
+          const int64_t at = ((((int64_t)g.page[i] * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
+          k = c.cache.k_pages + at;
+          v = c.cache.v_pages + at;
+          n = there ? s.len - row : 0;
+          ok &= there ? 3 : ~(1 << i);
+        }
+        n = std::clamp(n, 0, 16);
+        const __amdgpu_buffer_rsrc_t kr = half_rows(k, n), vr = half_rows(v, n);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-          d.k[kt * 2 + ks] = *(const u32x4*)(u.k[kt] + (uint32_t)(std::min(l16, u.last[kt]) * kRowBytes + (ks * 4 + grp) * 16));
+        for (int ks = 0; ks < 2; ++ks) d.k[2 * i + ks] = load_row(kr, k_offset + ks * 64);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        d.v[i] = *(const u32x4*)(u.v[i >> 1] + (uint32_t)(std::min(8 * (i & 1) + (lane >> 3), u.last[i >> 1]) * kRowBytes + (lane & 7) * 16));
+        for (int e = 0; e < 2; ++e) d.v[2 * i + e] = load_row(vr, v_offset + e * 1024);
+      }
+      return ok;
     };
 
     WaveState<NQ> w;
-    auto row_of = [&](int r, int& token) {     // element of q's head dimension too
+    auto row_of = [&](int r, int& token) {     // the head of q, and the token
       const int i = r / c.group;
       token = s.first + i;
       return p.h * c.group + (r - i * c.group);
     };
-    auto seen_by = [&](int r) { return c.causal ? std::clamp(s.len - s.n + r / c.group + 1, 0, s.len) : s.len; };
+    auto seen_by = [&](int r) { return CAUSAL ? std::clamp(s.len - s.n + r / c.group + 1, 0, s.len) : s.len; };
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
       const int r = std::min(r0 + 16 * qt + l16, n_rows - 1);
@@ -428,34 +456,36 @@ __global__ __launch_bounds__(64 * KS) void attention_cached_kernel(const LineArg
       const char* q = c.q.data + (token * c.q.token_stride + head * c.q.head_stride) * 2;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) w.qf[qt][ks] = *(const bf16x8*)(q + (ks * 4 + grp) * 16);
-      w.limit[qt] = seen_by(r);
+      if (CAUSAL) w.limit[qt] = seen_by(r);
       w.m[qt] = kLowest;
       w.l[qt] = 0.f;
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int least = seen_by(r0), most = seen_by(std::min(r0 + R, n_rows) - 1);
+    const int least = uniform(seen_by(r0)), most = uniform(seen_by(std::min(r0 + R, n_rows) - 1));
     // keys behind the last one that a row of the tile sees are not read
     const int stop = std::min(u1, prefix_units + (most + kUnit - 1) / kUnit);
-
+    // DEPTH units are on their way, the pages of the next one are asked for.  (The data moves through registers: two copies
+    // of the step in the loop need more scalar registers than there are.)
     int unit = u0 + wave;
-    if (unit < stop) {
-      UnitRows u = locate(unit);
-      UnitData d;
-      fetch(u, d);
-      while (true) {
-        const int next = unit + KS;
-        UnitRows un = u;
-        UnitData dn = d;
-        if (next < stop) {
-          un = locate(next);
-          fetch(un, dn);
-        }
-        unit_step<NQ>(w, u, d, sv, c.scale_log2, least, c.causal, lane);
-        if (next >= stop) break;
-        unit = next;
-        u = un;
-        d = dn;
+    UnitData d[DEPTH + 1];
+    int ok[DEPTH + 1];
+    Pages g = look_up(unit);
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      if (unit + i * KS < stop) ok[i] = fetch(unit + i * KS, g, d[i]);
+      g = look_up(unit + (i + 1) * KS);
+    }
+#pragma unroll 1
+    for (; unit < stop; unit += KS) {
+      if (unit + DEPTH * KS < stop) ok[DEPTH] = fetch(unit + DEPTH * KS, g, d[DEPTH]);
+      g = look_up(unit + (DEPTH + 1) * KS);
+      const bool own = unit >= prefix_units;
+      unit_step<NQ, CAUSAL>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : (int)c.P, ok[0], own, lane);
+#pragma unroll
+      for (int i = 0; i < DEPTH; ++i) {
+        d[i] = d[i + 1];
+        ok[i] = ok[i + 1];
       }
     }
 
@@ -552,7 +582,11 @@ __global__ __launch_bounds__(64 * KS) void attention_cached_kernel(const LineArg
           p.b = 0;
           if (++p.h == c.cache.H_kv) return;
         }
-        s = sequence<R>(a, p.b);
+        if (p.b < p.base || p.b >= p.base + 64) {
+          p.base = p.b;
+          window = load_window<R>(a, p.b, lane);
+        }
+        s = of_lane<R>(a, window, p.b - p.base);
       } while (s.tiles == 0);
     }
   }
@@ -670,7 +704,10 @@ int64_t slot_bytes(const Launch& l) { return align256(l.slots * 16 * l.nq * 8) +
 
 template <int NQ, int KS>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
-  hipLaunchKernelGGL((attention_cached_kernel<NQ, KS>), dim3(shares), dim3(64 * KS), 0, stream, a);
+  if (a.c.causal && a.with_own)
+    hipLaunchKernelGGL((attention_cached_kernel<NQ, KS, true>), dim3(shares), dim3(64 * KS), 0, stream, a);
+  else
+    hipLaunchKernelGGL((attention_cached_kernel<NQ, KS, false>), dim3(shares), dim3(64 * KS), 0, stream, a);
 }
 
 }  // namespace
@@ -703,7 +740,7 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
     a.with_prefix = l.with_prefix;
     a.with_own = l.with_own;
     a.finish = ch.finish;
-    a.min_units = 4 * l.ks;
+    a.min_units = l.ks;
     a.max_slots = (int32_t)l.slots;
     const int R = 16 * l.nq;
     a.rows = (RowPieces*)at;
