@@ -26,6 +26,7 @@
 // after the first unit is rare, and a comparison per score pays for it.
 #include <algorithm>
 
+#include "attention_common.hpp"
 #include "dev_common.hpp"
 #include "kernels.hpp"
 
@@ -37,8 +38,6 @@ constexpr int kUnit = 32;                       // keys
 constexpr int kUnitBytes = kUnit * kRowBytes;
 constexpr float kSlack = 10.f;
 constexpr float kLowest = -3.402823466e38f;     // a finite shift for sums without a key
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // Where the pieces of a row of q are, as rows of the workspace: the first in `first`, the i-th in base + i * stride
 struct RowPieces {
@@ -58,34 +57,21 @@ struct LineArgs {
   float* slot_o;          // [max_slots][R][64]
 };
 
-struct Pair {
-  float a, b;
-};
-__device__ __forceinline__ Pair swap16(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const uint32_t lo = r[0], hi = r[1];
-  return {__uint_as_float(lo), __uint_as_float(hi)};
-}
-__device__ __forceinline__ Pair swap32(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  const uint32_t lo = r[0], hi = r[1];
-  return {__uint_as_float(lo), __uint_as_float(hi)};
-}
 // over the four lane groups that share a row
 __device__ __forceinline__ float groups_max(float x) {
-  Pair p = swap16(x);
+  LanePair p = swap16(x);
   p = swap32(fmaxf(p.a, p.b));
   return fmaxf(p.a, p.b);
 }
 __device__ __forceinline__ float groups_sum(float x) {
-  Pair p = swap16(x);
+  LanePair p = swap16(x);
   p = swap32(p.a + p.b);
   return p.a + p.b;
 }
-__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+// (the IEEE 754-2019 maximum: fmaxf() would quiet every operand with an instruction of its own first)
+__device__ __forceinline__ float max8(const f32x4& a, const f32x4& b) {
+  auto max3 = [](float x, float y, float z) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z); };
+  return max3(max3(a[0], a[1], a[2]), max3(a[3], b[0], b[1]), __builtin_elementwise_maximum(b[2], b[3]));
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform64(int64_t x) {
@@ -99,14 +85,14 @@ struct Seq {
   int tiles;       // of R rows
   int units;       // of a tile, at least one: rows without keys are written too
 };
-template <int R>
+template <int R, int UNIT>
 __device__ __forceinline__ void count(const LineArgs& a, Seq& s) {
-  const int keys = (a.with_prefix ? ((int)a.c.P + kUnit - 1) / kUnit : 0) + (s.len + kUnit - 1) / kUnit;
+  const int keys = (a.with_prefix ? ((int)a.c.P + UNIT - 1) / UNIT : 0) + (s.len + UNIT - 1) / UNIT;
   s.tiles = (s.n * a.c.group + R - 1) / R;
   s.units = keys > 1 ? keys : 1;
 }
 // 64 sequences from `base` on, one per lane; those behind the last have no tokens
-template <int R>
+template <int R, int UNIT>
 __device__ __forceinline__ Seq load_window(const LineArgs& a, int base, int lane) {
   const CachedAttnArgs& c = a.c;
   const int n_seq = a.stacked ? 1 : c.cache.n_seqs, b = base + lane, T = (int)c.n_tokens;
@@ -118,16 +104,16 @@ __device__ __forceinline__ Seq load_window(const LineArgs& a, int base, int lane
     s.n = std::clamp(o1, s.first, T) - s.first;
     s.len = std::clamp(len, 0, c.cache.table_stride << c.cache.page_shift);
   }
-  count<R>(a, s);
+  count<R, UNIT>(a, s);
   return s;
 }
-template <int R>
+template <int R, int UNIT>
 __device__ __forceinline__ Seq of_lane(const LineArgs& a, const Seq& window, int l) {
   Seq s;
   s.first = __builtin_amdgcn_readlane(window.first, l);
   s.n = __builtin_amdgcn_readlane(window.n, l);
   s.len = __builtin_amdgcn_readlane(window.len, l);
-  count<R>(a, s);
+  count<R, UNIT>(a, s);
   return s;
 }
 
@@ -154,15 +140,15 @@ struct Place {
     return (int)(x < split ? quotient(x, per_share + 1) : longer + quotient(x - split, per_share));
   }
 };
-template <int R>
+template <int R, int UNIT>
 __device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p, Seq& window) {
   const int n_seq = a.stacked ? 1 : a.c.cache.n_seqs;
   const int lanes = n_seq < 64 ? n_seq : 64;
-  window = load_window<R>(a, 0, lane);
+  window = load_window<R, UNIT>(a, 0, lane);
   int64_t sum = (int64_t)window.tiles * window.units;
   int tiles = window.tiles;
   for (int i = 64; i < n_seq; i += 64) {
-    const Seq s = load_window<R>(a, i, lane);
+    const Seq s = load_window<R, UNIT>(a, i, lane);
     sum += (int64_t)s.tiles * s.units;
     tiles += s.tiles;
   }
@@ -187,7 +173,7 @@ __device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p
   int64_t rest = p.at - p.h * per_head;
   int before = 0;
   for (p.base = 0;; p.base += 64) {
-    if (p.base > 0) window = load_window<R>(a, p.base, lane);
+    if (p.base > 0) window = load_window<R, UNIT>(a, p.base, lane);
     int64_t scan = (int64_t)window.tiles * window.units;
     int tscan = window.tiles;
     for (int d = 1; d < lanes; d <<= 1) {
@@ -204,7 +190,7 @@ __device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p
       continue;
     }
     const int l = __builtin_ctzll(in);
-    const Seq s = of_lane<R>(a, window, l);
+    const Seq s = of_lane<R, UNIT>(a, window, l);
     rest -= uniform64(__shfl(scan, l)) - (int64_t)s.tiles * s.units;
     p.b = p.base + l;
     p.tile = (int)quotient(rest, s.units);
@@ -214,9 +200,91 @@ __device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p
   }
 }
 
-// V rows in LDS: chunk c of row r sits at position c ^ v_swizzle(r), so that the transposing reads find their rows in
-// different banks.
-__device__ __forceinline__ int v_swizzle(int row) { return ((row >> 1) & 3) << 1; }
+// On to the next tile, behind a piece of `done` units; false at the end of the share
+template <int R, int UNIT>
+__device__ __forceinline__ bool next_tile(const LineArgs& a, Place& p, Seq& window, Seq& s, int done, int lane) {
+  p.at += done;
+  p.unit = 0;
+  ++p.tile_id;
+  if (p.at >= p.end) return false;
+  if (++p.tile < s.tiles) return true;
+  p.tile = 0;
+  do {
+    if (++p.b == (a.stacked ? 1 : a.c.cache.n_seqs)) {
+      p.b = 0;
+      if (++p.h == a.c.cache.H_kv) return false;
+    }
+    if (p.b < p.base || p.b >= p.base + 64) {
+      p.base = p.b;
+      window = load_window<R, UNIT>(a, p.b, lane);
+    }
+    s = of_lane<R, UNIT>(a, window, p.b - p.base);
+  } while (s.tiles == 0);
+  return true;
+}
+
+// A row of a tile as q and o have it
+struct Row {
+  int token, head;
+};
+__device__ __forceinline__ Row row_of(const LineArgs& a, const Place& p, const Seq& s, int r) {
+  const int i = r / a.c.group;
+  return {s.first + i, p.h * a.c.group + (r - i * a.c.group)};
+}
+__device__ __forceinline__ const char* q_row(const LineArgs& a, const Row& r) {
+  return a.c.q.data + (r.token * a.c.q.token_stride + r.head * a.c.q.head_stride) * 2;
+}
+// Own keys that row r sees
+template <bool CAUSAL>
+__device__ __forceinline__ int seen_by(const LineArgs& a, const Seq& s, int r) {
+  return CAUSAL ? std::clamp(s.len - s.n + r / a.c.group + 1, 0, s.len) : s.len;
+}
+
+// Where a piece of units [u0, u1) goes: to o, or to a slot
+struct Target {
+  bool finish;
+  int slot;
+};
+// (by one wave: `threads` of them from `thread` on) The piece that has a tile's first unit says where the others are.
+template <int R>
+__device__ __forceinline__ Target place_piece(const LineArgs& a, const Place& p, const Seq& s, int64_t share_start, int u0, int u1, int thread,
+                                              int threads) {
+  Target t = {a.finish && u0 == 0 && u1 == s.units, 0};
+  if (!t.finish) t.slot = a.finish ? 2 * p.share + (p.at == share_start ? 0 : 1) : p.share + p.tile_id;
+  if (u0 == 0 && thread < threads) {
+    const int r0 = p.tile * R, n_rows = s.n * a.c.group;
+    RowPieces rp = {0, 0, 0, 0};
+    if (!t.finish) {
+      rp.n = p.share_of(p.at + s.units - 1) - p.share + 1;
+      rp.first = t.slot * R;
+      rp.base = (a.finish ? 2 * p.share : t.slot) * R;
+      rp.stride = a.finish ? 2 * R : R;
+    }
+    for (int i = thread; i < R; i += threads)
+      if (r0 + i < n_rows) {
+        const Row r = row_of(a, p, s, r0 + i);
+        a.rows[(int64_t)r.token * a.H_q + r.head] = {rp.first + i, rp.base + i, rp.stride, rp.n};
+      }
+  }
+  return t;
+}
+// Four channels of a row of the tile; l: the row's sum
+template <int R>
+__device__ __forceinline__ void put(const LineArgs& a, const Place& p, const Seq& s, const Target& t, int r, int channel, const f32x4& o, float l) {
+  if (p.tile * R + r >= s.n * a.c.group) return;
+  if (t.finish) {
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    const Row row = row_of(a, p, s, p.tile * R + r);
+    *(u32x2*)((char*)a.c.o + (((int64_t)row.token * a.H_q + row.head) * kDHead + channel) * 2) =
+        u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
+  } else if (t.slot < a.max_slots) {
+    *(f32x4*)(a.slot_o + ((int64_t)t.slot * R + r) * kDHead + channel) = o;
+  }
+}
+template <int R>
+__device__ __forceinline__ void put_sums(const LineArgs& a, const Place& p, const Seq& s, const Target& t, int r, float m, float l) {
+  if (!t.finish && t.slot < a.max_slots && p.tile * R + r < s.n * a.c.group) a.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
+}
 
 // V^T operands: 16 channels x 32 keys in the order of the weights (see the top)
 __device__ __forceinline__ void load_v_operands(bf16x8 (&av)[4], const bf16_t* sv, int l16, int grp) {
@@ -325,8 +393,7 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, b
   bool above = false;
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
-    const f32x4 &s0 = s[0][qt], &s1 = s[1][qt];
-    top[qt] = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+    top[qt] = max8(s[0][qt], s[1][qt]);
     above = above || fmaf(top[qt], c, -w.m[qt]) > kSlack;
   }
   if (__ballot(above)) {
@@ -381,8 +448,8 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
   bf16_t* sv = (bf16_t*)(s_mem + wave * kUnitBytes);
   Place p;
   Seq window;
-  if (!find_share<R>(a, lane, p, window)) return;
-  Seq s = of_lane<R>(a, window, p.b - p.base);
+  if (!find_share<R, kUnit>(a, lane, p, window)) return;
+  Seq s = of_lane<R, kUnit>(a, window, p.b - p.base);
   const int prefix_units = a.with_prefix ? ((int)c.P + kUnit - 1) / kUnit : 0;
   const int64_t share_start = p.at;
   const int k_offset = l16 * kRowBytes + grp * 16, v_offset = lane * 16;
@@ -442,27 +509,19 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
     };
 
     WaveState<NQ> w;
-    auto row_of = [&](int r, int& token) {     // the head of q, and the token
-      const int i = r / c.group;
-      token = s.first + i;
-      return p.h * c.group + (r - i * c.group);
-    };
-    auto seen_by = [&](int r) { return CAUSAL ? std::clamp(s.len - s.n + r / c.group + 1, 0, s.len) : s.len; };
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
       const int r = std::min(r0 + 16 * qt + l16, n_rows - 1);
-      int token;
-      const int head = row_of(r, token);
-      const char* q = c.q.data + (token * c.q.token_stride + head * c.q.head_stride) * 2;
+      const char* q = q_row(a, row_of(a, p, s, r));
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) w.qf[qt][ks] = *(const bf16x8*)(q + (ks * 4 + grp) * 16);
-      if (CAUSAL) w.limit[qt] = seen_by(r);
+      if (CAUSAL) w.limit[qt] = seen_by<CAUSAL>(a, s, r);
       w.m[qt] = kLowest;
       w.l[qt] = 0.f;
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int least = uniform(seen_by(r0)), most = uniform(seen_by(std::min(r0 + R, n_rows) - 1));
+    const int least = uniform(seen_by<CAUSAL>(a, s, r0)), most = uniform(seen_by<CAUSAL>(a, s, std::min(r0 + R, n_rows) - 1));
     // keys behind the last one that a row of the tile sees are not read
     const int stop = std::min(u1, prefix_units + (most + kUnit - 1) / kUnit);
     // DEPTH units are on their way, the pages of the next one are asked for.  (The data moves through registers: two copies
@@ -490,50 +549,15 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
     }
 
     // ---- the piece's end ---------------------------------------------------------------------------------
-    const bool whole = u0 == 0 && u1 == s.units;
-    const bool finish = a.finish && whole;
-    int slot = -1;
-    if (!finish) slot = a.finish ? 2 * p.share + (p.at == share_start ? 0 : 1) : p.share + p.tile_id;
-    if (u0 == 0 && wave == 0) {
-      RowPieces rp = {0, 0, 0, 0};
-      if (!finish) {
-        rp.n = p.share_of(p.at + s.units - 1) - p.share + 1;
-        rp.first = slot * R;
-        rp.base = (a.finish ? 2 * p.share : slot) * R;
-        rp.stride = a.finish ? 2 * R : R;
-      }
-#pragma unroll
-      for (int i = 0; i < (R + 63) / 64; ++i) {
-        const int r = r0 + i * 64 + lane;
-        if (i * 64 + lane < R && r < n_rows) {
-          int token;
-          const int head = row_of(r, token);
-          const int in_tile = i * 64 + lane;
-          a.rows[(int64_t)token * a.H_q + head] = {rp.first + in_tile, rp.base + in_tile, rp.stride, rp.n};
-        }
-      }
-    }
-    const bool store = finish || slot < a.max_slots;
-    auto put = [&](int r, int channel, f32x4 o, float l) {    // r: row in the tile
-      if (r0 + r >= n_rows || !store) return;
-      if (finish) {
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        int token;
-        const int head = row_of(r0 + r, token);
-        uint32_t* to = (uint32_t*)((char*)c.o + (((int64_t)token * a.H_q + head) * kDHead + channel) * 2);
-        *(u32x2*)to = u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
-      } else {
-        *(f32x4*)(a.slot_o + ((int64_t)slot * R + r) * kDHead + channel) = o;
-      }
-    };
+    const Target to = place_piece<R>(a, p, s, share_start, u0, u1, threadIdx.x, 64);
     if constexpr (KS == 1) {
 #pragma unroll
       for (int qt = 0; qt < NQ; ++qt) {
         const float l = groups_sum(w.l[qt]);
         const int r = 16 * qt + l16;
-        if (!finish && store && grp == 0 && r0 + r < n_rows) a.slot_ml[(int64_t)slot * R + r] = float2{w.m[qt], l};
+        if (grp == 0) put_sums<R>(a, p, s, to, r, w.m[qt], l);
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct) put(r, 16 * ct + 4 * grp, w.o[ct][qt], l);
+        for (int ct = 0; ct < 4; ++ct) put<R>(a, p, s, to, r, 16 * ct + 4 * grp, w.o[ct][qt], l);
       }
     } else {
       float f[NQ];
@@ -564,31 +588,348 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
 #pragma unroll
           for (int k = 1; k < KS; ++k) o += so[k * R * 4 + i];
           const float2 ml = joined(i >> 2);
-          if (ct == 0 && (i & 3) == 0 && !finish && store && r0 + (i >> 2) < n_rows) a.slot_ml[(int64_t)slot * R + (i >> 2)] = ml;
-          put(i >> 2, 16 * ct + 4 * (i & 3), o, ml.y);
+          if (ct == 0 && (i & 3) == 0) put_sums<R>(a, p, s, to, i >> 2, ml.x, ml.y);
+          put<R>(a, p, s, to, i >> 2, 16 * ct + 4 * (i & 3), o, ml.y);
         }
         __syncthreads();
       }
     }
 
-    // ---- the next tile --------------------------------------------------------------------------------------
-    p.at += u1 - u0;
-    p.unit = 0;
-    ++p.tile_id;
-    if (p.at < p.end && ++p.tile == s.tiles) {
-      p.tile = 0;
-      do {
-        if (++p.b == (a.stacked ? 1 : c.cache.n_seqs)) {
-          p.b = 0;
-          if (++p.h == c.cache.H_kv) return;
-        }
-        if (p.b < p.base || p.b >= p.base + 64) {
-          p.base = p.b;
-          window = load_window<R>(a, p.b, lane);
-        }
-        s = of_lane<R>(a, window, p.b - p.base);
-      } while (s.tiles == 0);
+    if (!next_tile<R, kUnit>(a, p, window, s, u1 - u0, lane)) return;
+  }
+}
+
+// ---- many rows -------------------------------------------------------------------------------------------------
+//
+// Tiles of 256 rows, 64 for each of four waves, which share the keys: units of 64 go through registers into LDS, two of
+// them there at a time.  Bound by the matrix cores and, close behind, by the vector instructions of the softmax, so a wave's
+// step of 32 keys has the products of the step before and of the step behind in one block with the weights of its
+// own, which depend on neither: the order of issue mixes them.  (V therefore runs a unit behind K.)  Whether a shift has to
+// follow is looked at before the block, on scores that the step before has left.
+
+constexpr int kWideUnit = 64;
+constexpr int kWideWaves = 4;
+constexpr int kWideQ = 4;
+constexpr int kWideRows = 16 * kWideQ * kWideWaves;
+
+// The state of a wave of 64 rows
+struct WideState {
+  bf16x8 qf[kWideQ][2];     // Q^T, 32 channels each
+  f32x4 o[4][kWideQ];       // O^T, 16 channels each
+  f32x4 cur[2][kWideQ];     // scores of the step in work
+  bf16x8 p[kWideQ];         // weights of the step before
+  float l[kWideQ];          // sums over the lane's keys
+  float m[kWideQ];          // minus the shift, in log2 units
+};
+// The shift follows the scores of the step in work, and all that is relative to it
+__device__ __forceinline__ void raise_shift(WideState& w, const float (&top)[kWideQ], float c) {
+#pragma unroll
+  for (int qt = 0; qt < kWideQ; ++qt) {
+    const float m = fminf(w.m[qt], -(groups_max(top[qt]) * c));
+    const float f = __builtin_amdgcn_exp2f(m - w.m[qt]);
+    w.m[qt] = m;
+    w.l[qt] *= f;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] *= f;
+    // the weights that wait for their product follow too; f is 1 or below 2^-kSlack, where a second rounding is nothing
+    u32x4 x = __builtin_bit_cast(u32x4, w.p[qt]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = pack_bf16x2(bf16_lo(x[e]) * f, bf16_hi(x[e]) * f);
+    w.p[qt] = __builtin_bit_cast(bf16x8, x);
+  }
+}
+
+template <bool CAUSAL>
+__global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_cached_wide_kernel(const LineArgs a) {
+  constexpr int NQ = kWideQ, R = kWideRows, UNIT = kWideUnit;
+  // K of two units, V of two.  All that reads or writes them goes by offsets that change sides once a unit.
+  constexpr int kSide = UNIT * kRowBytes, kHalf = kSide / 2;
+  __shared__ __attribute__((aligned(4 * kSide))) char s_mem[4 * kSide];
+  const CachedAttnArgs& c = a.c;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int l16 = lane & 15, grp = lane >> 4;
+  Place p;
+  Seq window;
+  if (!find_share<R, UNIT>(a, lane, p, window)) return;
+  Seq s = of_lane<R, UNIT>(a, window, p.b - p.base);
+  const int prefix_units = a.with_prefix ? ((int)c.P + UNIT - 1) / UNIT : 0;
+  const int64_t share_start = p.at;
+  // lanes' offsets: K operands (channel halves), V operands (channel quarters), the rows that a wave brings (K, V)
+  int k_at[2], v_at[4], to_k, to_v;
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) k_at[ks] = l16 * kRowBytes + ((ks * 4 + grp) ^ k_swizzle(l16)) * 16;
+  {
+    const int row = 4 * grp + (l16 >> 2);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) v_at[ct] = 2 * kSide + row * kRowBytes + ((2 * ct + ((l16 & 3) >> 1)) ^ v_swizzle(row)) * 16 + 8 * (l16 & 1);
+    const int in = 16 * wave + (lane >> 3);      // and the row 8 further, whose place among the chunks is the same one
+    to_k = in * kRowBytes + ((lane & 7) ^ k_swizzle(in)) * 16;
+    to_v = 2 * kSide + in * kRowBytes + ((lane & 7) ^ v_swizzle(in)) * 16;
+  }
+  auto change_sides = [&] {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) k_at[i] ^= kSide;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v_at[i] ^= kSide;
+    to_k ^= kSide;
+    to_v ^= kSide;
+  };
+  auto barrier = [] {      // LDS only: rows on their way from memory stay so
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  while (true) {
+    const int u0 = p.unit;
+    const int u1 = (int)std::min<int64_t>(s.units, p.unit + (p.end - p.at));
+    const int n_rows = s.n * c.group, r0 = p.tile * R, wr0 = r0 + wave * 16 * NQ;
+    const auto* table = (const __attribute__((address_space(4))) int32_t*)(c.cache.table + (int64_t)p.b * c.cache.table_stride);
+    const bool active = uniform(wr0 < n_rows) != 0;
+    const int least = uniform(seen_by<CAUSAL>(a, s, std::min(wr0, n_rows - 1)));
+    const int most = uniform(seen_by<CAUSAL>(a, s, std::min(r0 + R, n_rows) - 1));
+    const int stop = std::min(u1, prefix_units + (most + UNIT - 1) / UNIT);
+
+    WideState w;
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) {
+      const char* q = q_row(a, row_of(a, p, s, std::min(wr0 + 16 * qt + l16, n_rows - 1)));
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) w.qf[qt][ks] = *(const bf16x8*)(q + (ks * 4 + grp) * 16);
+      w.m[qt] = -kLowest;
+      w.l[qt] = 0.f;
+      w.p[qt] = bf16x8{};
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+
+    auto page_of = [&](int unit, int quarter) {
+      const int index = ((unit - prefix_units) * UNIT + 16 * quarter) >> c.cache.page_shift;
+      return index < c.cache.table_stride ? table[index] : -1;
+    };
+    auto there = [&](int page) { return page >= 0 && page < (int)c.cache.n_pages; };
+    // A wave brings the unit's rows 16 * wave .. + 15, of K and, a unit later, of V
+    struct RowsAt {
+      int64_t offset;     // from k_prefix or k_pages, and from v_prefix or v_pages
+      int n;
+      bool own;
+    };
+    auto rows_at = [&](int unit) {
+      RowsAt r = {0, 0, unit >= prefix_units};
+      const int row = (r.own ? unit - prefix_units : unit) * UNIT + 16 * wave;
+      if (unit >= stop) {
+      } else if (!r.own) {
+        r.offset = (p.h * c.P + row) * kRowBytes;
+        r.n = std::clamp((int)c.P - row, 0, 16);
+      } else {
+        const int page = page_of(unit, wave);
+        r.offset = ((((int64_t)page * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
+        r.n = there(page) ? std::clamp(s.len - row, 0, 16) : 0;
+      }
+      return r;
+    };
+    auto k_rows = [&](const RowsAt& r) { return half_rows((r.own ? c.cache.k_pages : c.k_prefix) + r.offset, r.n); };
+    auto v_rows = [&](const RowsAt& r) { return half_rows((r.own ? c.cache.v_pages : c.v_prefix) + r.offset, r.n); };
+    u32x4 in_k[2], in_v[2];
+    auto request = [&](u32x4 (&in)[2], const __amdgpu_buffer_rsrc_t rows) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) in[i] = load_row(rows, lane * 16 + i * 1024);
+    };
+    auto store_k = [&](int to, const u32x4 (&in)[2]) {
+      *(u32x4*)(s_mem + to) = in[0];
+      *(u32x4*)(s_mem + (to ^ 64) + 8 * kRowBytes) = in[1];      // (k_swizzle() of the row 8 further: 4 more)
+    };
+    auto store_v = [&](int to, const u32x4 (&in)[2]) {
+      *(u32x4*)(s_mem + to) = in[0];
+      *(u32x4*)(s_mem + to + 8 * kRowBytes) = in[1];
+    };
+    // 4 bits for a unit, whether its quarters have pages: looked at only where some entry of the tile's is none
+    bool hole = false;
+    for (int i = lane; i < (most + (1 << c.cache.page_shift) - 1) >> c.cache.page_shift; i += 64) hole |= !there(table[i]);
+    const bool holes = __ballot(hole) != 0;
+    auto ok_of = [&](int unit) {
+      uint32_t ok = 15;
+      if (holes && unit >= prefix_units) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ok &= there(page_of(unit, i)) ? 15u : ~(1u << i);
+      }
+      return ok;
+    };
+
+    auto load_k = [&](bf16x8 (&ak)[4], int half) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) ak[kt * 2 + ks] = *(const bf16x8*)(s_mem + k_at[ks] + half + kt * 16 * kRowBytes);
+    };
+    auto score = [&](const bf16x8 (&ak)[4], int qt) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) w.cur[kt][qt] = mfma16(ak[kt * 2], w.qf[qt][0], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) w.cur[kt][qt] = mfma16(ak[kt * 2 + 1], w.qf[qt][1], w.cur[kt][qt]);
+    };
+    const bf16x2 ones = __builtin_bit_cast(bf16x2, local(0x3F803F80u));   // (a literal is not taken as two bf16 halves)
+    auto limit_of = [&](int qt) { return seen_by<CAUSAL>(a, s, std::min(wr0 + 16 * qt + l16, n_rows - 1)); };
+    // V operands for the weights of the step before.  Where a row must not see one of its keys, whose V is not finite: key by
+    // key, and zeros are left
+    int old_row0 = -1;      // the first key of the step before, if some rows do not see all of it
+    auto load_v = [&](bf16x8 (&av)[4], int half) {
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct) {
+        const char* at = s_mem + v_at[ct] + half;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 16 * kRowBytes));
+        av[ct] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+      if (CAUSAL && __builtin_expect(old_row0 >= 0, 0)) {
+        bool bad = false;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = __builtin_bit_cast(u32x4, av[ct])[e];
+            bad |= (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
+          }
+        if (__ballot(bad)) {
+          int limit[NQ];
+#pragma unroll
+          for (int qt = 0; qt < NQ; ++qt) limit[qt] = limit_of(qt);
+          add_seen<NQ>(w.o, av, w.p, limit, old_row0, lane);
+#pragma unroll
+          for (int ct = 0; ct < 4; ++ct) av[ct] = bf16x8{};
+        }
+      }
+    };
+    // A step of 32 keys from row0 on.  half: where the K rows of the step behind it and the V rows of the step before are in their
+    // sides; end, ok, own as in unit_step()
+    auto step = [&](int half, int row0, int end, uint32_t ok, bool own) {
+      bf16x8 ak[4], av[4];
+      load_v(av, half);
+      const bool partial = row0 + 32 > end;
+      if (__builtin_expect(partial || ok != 3, 0)) {
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) {
+          const int limit = (CAUSAL && own ? limit_of(qt) : end) - row0 - 4 * grp;
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (16 * kt + r >= limit || !((ok >> kt) & 1)) w.cur[kt][qt][r] = -__builtin_inff();
+        }
+      }
+      if (CAUSAL) old_row0 = partial && own ? row0 : -1;
+      float top[NQ], over[NQ];
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        top[qt] = max8(w.cur[0][qt], w.cur[1][qt]);
+        over[qt] = fmaf(top[qt], c.scale_log2, w.m[qt]);
+      }
+      if (__ballot(max8(f32x4{over[0], over[1], over[2], over[3]}, f32x4{over[0], over[0], over[0], over[0]}) > kSlack)) raise_shift(w, top, c.scale_log2);
+      load_k(ak, half);
+      __builtin_amdgcn_sched_barrier(0);
+      // (a wave inside this block goes first: the other one of its SIMD fills what it leaves.  16 heads x 8192 tokens x 16384 keys 620 -> 578 us)
+      __builtin_amdgcn_s_setprio(1);
+      // query tile qt: its weights next to its product with V and the scores of the tile before
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = mfma16(av[ct], w.p[qt], w.o[ct][qt]);
+        u32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4& y = w.cur[e >> 1][qt];
+          const float x0 = __builtin_amdgcn_exp2f(fmaf(y[2 * (e & 1)], c.scale_log2, w.m[qt]));
+          const float x1 = __builtin_amdgcn_exp2f(fmaf(y[2 * (e & 1) + 1], c.scale_log2, w.m[qt]));
+          uint32_t pair = pack_bf16x2(x0, x1);
+          asm("" : "+v"(pair));     // (else the compiler takes the same element of x for all four sums: seen in its assembly)
+          x[e] = pair;
+          w.l[qt] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, w.l[qt], false);
+        }
+        if (qt > 0) score(ak, qt - 1);
+        // order of issue: a product, then an exp2 or two, then others
+        if (qt > 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        w.p[qt] = __builtin_bit_cast(bf16x8, x);
+      }
+      score(ak, NQ - 1);
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    if (u0 < stop) {
+      // K units u0 and u0 + 1 and V unit u0 are there before the first step; zeros for the V unit in front of it
+      RowsAt v_next = rows_at(u0), k_next = rows_at(u0 + 1);
+      {
+        u32x4 k1[2];
+        request(in_k, k_rows(v_next));
+        request(in_v, v_rows(v_next));
+        request(k1, k_rows(k_next));
+        store_k(to_k, in_k);
+        store_k(to_k ^ kSide, k1);
+        store_v(to_v ^ kSide, in_v);
+        *(u32x4*)(s_mem + (v_at[0] & ~(kSide - 1)) + kHalf + threadIdx.x * 16) = u32x4{0, 0, 0, 0};
+      }
+      v_next = k_next;
+      k_next = rows_at(u0 + 2);
+      request(in_k, k_rows(k_next));
+      request(in_v, v_rows(v_next));
+      barrier();
+      if (active) {
+        bf16x8 ak[4];
+        load_k(ak, 0);
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) score(ak, qt);
+      }
+      for (int unit = u0; unit < stop; ++unit) {
+        const bool own = unit >= prefix_units;
+        const int row0 = (own ? unit - prefix_units : unit) * UNIT, end = own ? least : (int)c.P;
+        const uint32_t ok = ok_of(unit);
+        if (active) step(kHalf, row0, end, ok & 3, own);
+        barrier();      // K of this unit and V of the one before have been read by everybody
+        store_k(to_k, in_k);
+        store_v(to_v, in_v);
+        v_next = k_next;
+        k_next = rows_at(unit + 3);
+        request(in_k, k_rows(k_next));
+        request(in_v, v_rows(v_next));
+        change_sides();
+        if (active) step(0, row0 + 32, end, ok >> 2, own);
+      }
+      if (active) {
+        bf16x8 av[4];
+        load_v(av, kHalf);
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+          for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = mfma16(av[ct], w.p[qt], w.o[ct][qt]);
+      }
+    }
+
+    const Target to = place_piece<R>(a, p, s, share_start, u0, u1, threadIdx.x, 64);
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) {
+      const float l = groups_sum(w.l[qt]);
+      const int r = wave * 16 * NQ + 16 * qt + l16;
+      if (grp == 0) put_sums<R>(a, p, s, to, r, -w.m[qt], l);
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct) put<R>(a, p, s, to, r, 16 * ct + 4 * grp, w.o[ct][qt], l);
+    }
+    if (!next_tile<R, UNIT>(a, p, window, s, u1 - u0, lane)) return;
+    barrier();      // the buffers are free
   }
 }
 
@@ -663,7 +1004,8 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
 // ---- what runs -----------------------------------------------------------------------------------------------
 
 struct Launch {
-  int nq, ks;             // 16 * nq rows in a tile, ks waves
+  int rows;               // of a tile
+  int nq, ks;             // 16 * nq rows, ks waves that share out the keys; nq = 0: the wide kernel
   bool stacked, with_prefix, with_own;
   int shares;
   int64_t slots;
@@ -686,21 +1028,22 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   c.rows_bytes = align256(n_tokens * H_q * (int64_t)sizeof(RowPieces));
   auto add = [&](int nq, int ks, bool stacked, bool prefix, bool own) {
     Launch& l = c.run[c.n++];
-    l = {nq, ks, stacked, prefix, own, 0, 0};
+    l = {nq ? 16 * nq : kWideRows, nq, ks, stacked, prefix, own, 0, 0};
     l.shares = ks == 1 ? 2048 : 512;
-    const int64_t R = 16 * nq;
-    const int64_t tiles = H_kv * (stacked ? (rows + R - 1) / R : rows / R + n_seqs);
+    const int64_t tiles = H_kv * (stacked ? (rows + l.rows - 1) / l.rows : rows / l.rows + n_seqs);
     l.slots = c.finish ? 2 * l.shares : l.shares + tiles;
   };
+  // tiles of 256 rows for more than 64: below, their waves would have no rows
+  auto rows_for = [&](int64_t n) { return few(n) ? 1 : n <= 64 ? 4 : 0; };
   if (stack) {
-    add(few(rows) ? 1 : 4, 4, true, true, false);
+    add(rows_for(rows), 4, true, true, false);
     add(few(mean) ? 1 : 4, few(mean) ? 1 : 4, false, false, true);
   } else {
-    add(few(mean) ? 1 : 4, 4, false, P > 0, true);
+    add(rows_for(mean), 4, false, P > 0, true);
   }
   return c;
 }
-int64_t slot_bytes(const Launch& l) { return align256(l.slots * 16 * l.nq * 8) + align256(l.slots * 16 * l.nq * kDHead * 4); }
+int64_t slot_bytes(const Launch& l) { return align256(l.slots * l.rows * 8) + align256(l.slots * l.rows * kDHead * 4); }
 
 template <int NQ, int KS>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
@@ -740,9 +1083,9 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
     a.with_prefix = l.with_prefix;
     a.with_own = l.with_own;
     a.finish = ch.finish;
-    a.min_units = l.ks;
+    a.min_units = l.nq ? l.ks : 2;
     a.max_slots = (int32_t)l.slots;
-    const int R = 16 * l.nq;
+    const int R = l.rows;
     a.rows = (RowPieces*)at;
     a.slot_ml = (float2*)(at + ch.rows_bytes);
     a.slot_o = (float*)(at + ch.rows_bytes + align256(l.slots * R * 8));
@@ -752,8 +1095,12 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
       start<1, 1>(a, l.shares, stream);
     else if (l.nq == 1)
       start<1, 4>(a, l.shares, stream);
-    else
+    else if (l.nq == 4)
       start<4, 4>(a, l.shares, stream);
+    else if (a.c.causal && a.with_own)
+      hipLaunchKernelGGL(attention_cached_wide_kernel<true>, dim3(l.shares), dim3(64 * kWideWaves), 0, stream, a);
+    else
+      hipLaunchKernelGGL(attention_cached_wide_kernel<false>, dim3(l.shares), dim3(64 * kWideWaves), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
