@@ -192,6 +192,10 @@ def _stream() -> int:
     return _raw_stream(torch.cuda.current_device())
 
 
+def _stream_of(device: int) -> int:
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
 def _dev(t: torch.Tensor, dtype, shape=None) -> int:
     if t.is_cuda and t.dtype == dtype and t.is_contiguous() and (shape is None or t.shape == shape):
         return t.data_ptr()
@@ -498,29 +502,50 @@ _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 MAX_SEQS = 4096
 
 
-def _same_device(*tensors):
-    """All on the GPU that is current: a launch goes there, and its stream is asked for there."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise HttmError(f"tensor is on {t.device}, the current device is cuda:{here}")
+_device = getattr(torch._C, "_cuda_getDevice", None)      # (torch.cuda.current_device() without its checks: 0.8 us less)
 
 
-def _rows(t, H, dtype):
-    """A [N, H, 64] view whose channels are dense, as the C side takes it."""
-    if t is None:
-        return RowsStruct(None, 0, 0)
+def _here(t: torch.Tensor) -> int:
+    """The current device, which a launch goes to; `t` must be there."""
     if not t.is_cuda:
         raise HttmError("tensor must live on the GPU")
-    if t.dtype != dtype:
-        raise HttmError(f"expected dtype {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[1] != H or t.shape[2] != 64:
-        raise HttmError(f"expected shape [N, {H}, 64], got {tuple(t.shape)}")
-    token, head, channel = t.stride()
-    if channel != 1:
+    here = _device()
+    if t.get_device() != here:
+        _refuse(t, here)
+    return here
+
+
+def _refuse(t, here, dtype=None, shape=None):
+    if t.is_cuda and t.get_device() != here:
+        raise HttmError(f"tensor is on {t.device}, the current device is cuda:{here}")
+    _dev(t, dtype, shape)
+
+
+def _at(t: torch.Tensor, here: int, dtype, shape=None) -> int:
+    """As _dev(), for a tensor on the current device."""
+    if t.get_device() == here and t.dtype is dtype and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
+    _refuse(t, here, dtype, shape)
+
+
+_NO_ROWS = RowsStruct(None, 0, 0)
+
+
+def _rows(t, here, H, dtype):
+    """A [N, H, 64] view whose channels are dense, as the C side takes it."""
+    if t is None:
+        return _NO_ROWS
+    shape, stride = t.shape, t.stride()
+    if t.get_device() != here or t.dtype is not dtype or len(shape) != 3 or shape[1] != H or shape[2] != 64 or stride[2] != 1:
+        if t.get_device() != here:
+            _refuse(t, here, dtype)
+        if t.dtype != dtype:
+            raise HttmError(f"expected dtype {dtype}, got {t.dtype}")
+        if len(shape) != 3 or shape[1] != H or shape[2] != 64:
+            raise HttmError(f"expected shape [N, {H}, 64], got {tuple(shape)}")
         raise HttmError("the 64 channels of a row must be contiguous")
     # (a stride along an axis of length 1 means nothing)
-    return RowsStruct(t.data_ptr(), token if t.shape[0] > 1 else 0, head if H > 1 else 0)
+    return RowsStruct(t.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if H > 1 else 0)
 
 
 class NormRope:
@@ -533,9 +558,19 @@ class NormRope:
     def __init__(self, norm="layer", eps=1e-6, axes=2, rot_dim=64, pairing="halves", base=100.0, q_weight=None, q_bias=None,
                  k_weight=None, k_bias=None, k_scale=1.0):
         self.affine = (q_weight, q_bias, k_weight, k_bias)      # kept alive
+        self.device = None
+        pointers = [None] * 4
+        for i, t in enumerate(self.affine):
+            if t is not None:
+                if self.device is None:
+                    self.device = _here(t)
+                pointers[i] = _at(t, self.device, torch.float32, (64,))
         self.axes = int(axes)
-        self.struct = NormRopeStruct(NORMS[norm], self.axes, int(rot_dim), PAIRINGS[pairing], float(base), float(eps), float(k_scale),
-                                     *(None if t is None else _dev(t, torch.float32, (64,)) for t in self.affine))
+        self.struct = NormRopeStruct(NORMS[norm], self.axes, rot_dim, PAIRINGS[pairing], base, eps, k_scale, *pointers)
+
+    def check_device(self, here):
+        if self.device is not None and self.device != here:
+            raise HttmError(f"weights are on cuda:{self.device}, the current device is cuda:{here}")
 
 
 class PagedCache:
@@ -543,49 +578,57 @@ class PagedCache:
     [n_seqs, pages of a sequence] int32."""
 
     def __init__(self, k_pages, v_pages, page_table):
-        if k_pages.dim() != 4 or page_table.dim() != 2:
+        shape, table_shape = k_pages.shape, page_table.shape
+        if len(shape) != 4 or shape[3] != 64 or len(table_shape) != 2:
             raise HttmError("expected k_pages [n_pages, H_kv, page_size, 64] and page_table [n_seqs, pages]")
-        n_pages, H_kv, page_size, d = k_pages.shape
-        shape = (n_pages, H_kv, page_size, 64)
-        _same_device(k_pages, v_pages, page_table) if k_pages.is_cuda else None
+        here = _here(k_pages)
+        self.device = here
         self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
-        self.n_seqs, self.H_kv, self.page_size = int(page_table.shape[0]), int(H_kv), int(page_size)
-        self.struct = PagedStruct(_dev(k_pages, torch.bfloat16, shape), _dev(v_pages, torch.bfloat16, shape),
-                                  _dev(page_table, torch.int32), n_pages, self.n_seqs, page_table.shape[1], page_size, H_kv)
+        self.n_seqs, self.H_kv, self.page_size = table_shape[0], shape[1], shape[2]
+        self.struct = PagedStruct(_at(k_pages, here, torch.bfloat16), _at(v_pages, here, torch.bfloat16, shape),
+                                  _at(page_table, here, torch.int32), shape[0], table_shape[0], table_shape[1], shape[2], shape[1])
+
+    def check_device(self, here):
+        if self.device != here:
+            raise HttmError(f"the cache is on cuda:{self.device}, the current device is cuda:{here}")
 
 
-def _projection_type(*tensors):
-    dtype = next((t.dtype for t in tensors if t is not None), None)
-    if dtype not in _DTYPES:
-        raise HttmError(f"rows must be bf16, fp16 or fp32, got {dtype}")
-    return dtype
+def _rows_type(t) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise HttmError(f"rows must be bf16, fp16 or fp32, got {t.dtype}")
+    return code
 
 
 def qk_norm_rope(nr: NormRope, q, k, v, pos, q_out, k_out, v_out):
     """Rows of a projection -> the layer's tensors: q [N, H_q, 64], k, v [N, H_kv, 64] (any token and head strides, bf16, fp16 or
     fp32) -> q_out [H_q, N, 64], k_out, v_out [H_kv, N, 64] bf16.  pos: [N, axes] int32 (None without axes).
     Any of q, k, v may be None, with its output."""
-    given = [t for t in (q, k, v) if t is not None]
-    dtype = _projection_type(*given)
-    N = int(given[0].shape[0])
+    first = q if q is not None else k if k is not None else v
+    if first is None or first.dim() != 3:
+        raise HttmError("expected q [N, H_q, 64], k or v [N, H_kv, 64]")
+    code, dtype, here = _rows_type(first), first.dtype, _here(first)
+    N = first.shape[0]
     kv = k if k is not None else v
-    H_kv = int(kv.shape[1]) if kv is not None else 1
-    H_q = int(q.shape[1]) if q is not None else H_kv
-    rows = [_rows(q, H_q, dtype), _rows(k, H_kv, dtype), _rows(v, H_kv, dtype)]
-    outs = []
+    H_kv = kv.shape[1] if kv is not None else 1
+    H_q = q.shape[1] if q is not None else H_kv
+    rows, outs = [], []
     for t, out, H in ((q, q_out, H_q), (k, k_out, H_kv), (v, v_out, H_kv)):
-        if t is not None and t.shape[0] != N:
-            raise HttmError(f"expected {N} tokens, got {int(t.shape[0])}")
         if (t is None) != (out is None):
             raise HttmError("every tensor needs its output, and every output its tensor")
-        outs.append(_dev(out, torch.bfloat16, (H, N, 64)) if out is not None else None)
-    turning = nr.axes > 0 and (q is not None or k is not None)
-    if turning and pos is None:
-        raise HttmError("positions are needed for a rotation")
-    p = _dev(pos, torch.int32, (N, nr.axes)) if turning else None
-    _same_device(q, k, v, pos if turning else None, q_out, k_out, v_out, *nr.affine)
-    _check(lib().httm_qk_norm_rope(C.byref(nr.struct), C.byref(rows[0]), C.byref(rows[1]), C.byref(rows[2]), _DTYPES[dtype], p,
-                                   N, H_q, H_kv, 64, *outs, _stream()), "httm_qk_norm_rope")
+        rows.append(C.byref(_rows(t, here, H, dtype)))
+        outs.append(None if out is None else _at(out, here, torch.bfloat16, (H, N, 64)))
+        if t is not None and t.shape[0] != N:
+            raise HttmError(f"expected {N} tokens, got {t.shape[0]}")
+    p = None
+    if nr.axes > 0 and (q is not None or k is not None):
+        if pos is None:
+            raise HttmError("positions are needed for a rotation")
+        p = _at(pos, here, torch.int32, (N, nr.axes))
+    nr.check_device(here)
+    rc = lib().httm_qk_norm_rope(C.byref(nr.struct), *rows, code, p, N, H_q, H_kv, 64, *outs, _stream_of(here))
+    if rc:
+        _check(rc, "httm_qk_norm_rope")
     return q_out, k_out, v_out
 
 
@@ -593,20 +636,23 @@ def cache_append(nr: NormRope, q, k, v, pos, cache: PagedCache, offsets, seq_len
     """New tokens of the sequences of a batch into the cache: q [n, H_q, 64] (or None, with q_out), k, v [n, H_kv, 64]; offsets
     [n_seqs + 1], seq_lens [n_seqs] (with the new tokens) int32 on the GPU; q_out [n, H_q, 64] bf16.
     pos: [n, axes] int32, or None with one axis: first_pos + a token's row in its sequence."""
-    dtype = _projection_type(k)
-    n = int(k.shape[0])
-    H_q = int(q.shape[1]) if q is not None else cache.H_kv
+    code, dtype, here = _rows_type(k), k.dtype, _here(k)
+    n, H_kv = k.shape[0], cache.H_kv
+    H_q = q.shape[1] if q is not None else H_kv
     if v is None or v.shape[0] != n or (q is not None and q.shape[0] != n):
         raise HttmError(f"expected {n} tokens in q, k and v")
     if (q is None) != (q_out is None):
         raise HttmError("q needs q_out, and q_out needs q")
-    rows = [_rows(q, H_q, dtype), _rows(k, cache.H_kv, dtype), _rows(v, cache.H_kv, dtype)]
-    out = _dev(q_out, torch.bfloat16, (n, H_q, 64)) if q_out is not None else None
-    p = _dev(pos, torch.int32, (n, nr.axes)) if pos is not None and nr.axes > 0 else None
-    off, lens = _dev(offsets, torch.int32, (cache.n_seqs + 1,)), _dev(seq_lens, torch.int32, (cache.n_seqs,))
-    _same_device(q, k, v, pos, cache.k_pages, offsets, seq_lens, q_out, *nr.affine)
-    _check(lib().httm_cache_append(C.byref(nr.struct), C.byref(rows[0]), C.byref(rows[1]), C.byref(rows[2]), _DTYPES[dtype], p,
-                                   int(first_pos), n, H_q, 64, C.byref(cache.struct), off, lens, out, _stream()), "httm_cache_append")
+    rows = [C.byref(_rows(q, here, H_q, dtype)), C.byref(_rows(k, here, H_kv, dtype)), C.byref(_rows(v, here, H_kv, dtype))]
+    out = None if q_out is None else _at(q_out, here, torch.bfloat16, (n, H_q, 64))
+    p = _at(pos, here, torch.int32, (n, nr.axes)) if pos is not None and nr.axes > 0 else None
+    nr.check_device(here)
+    cache.check_device(here)
+    rc = lib().httm_cache_append(C.byref(nr.struct), *rows, code, p, first_pos, n, H_q, 64, C.byref(cache.struct),
+                                 _at(offsets, here, torch.int32, (cache.n_seqs + 1,)), _at(seq_lens, here, torch.int32, (cache.n_seqs,)),
+                                 out, _stream_of(here))
+    if rc:
+        _check(rc, "httm_cache_append")
     return q_out
 
 
@@ -626,21 +672,24 @@ def attention_cached(q, k_prefix, v_prefix, cache: PagedCache, offsets, seq_lens
     bf = torch.bfloat16
     if q.dim() != 3:
         raise HttmError(f"expected q [n, H_q, 64], got {tuple(q.shape)}")
-    n, H_q, P = int(q.shape[0]), int(q.shape[1]), 0
-    rows = _rows(q, H_q, bf)
+    here = _here(q)
+    n, H_q, _ = q.shape
+    P, kp, vp = 0, None, None
     if (k_prefix is None) != (v_prefix is None):
         raise HttmError("a prefix has keys and values")
     if k_prefix is not None:
         if k_prefix.dim() != 3:
             raise HttmError(f"expected a prefix [{cache.H_kv}, P, 64], got {tuple(k_prefix.shape)}")
-        P = int(k_prefix.shape[1])
-    kp = _dev(k_prefix, bf, (cache.H_kv, P, 64)) if P else None
-    vp = _dev(v_prefix, bf, (cache.H_kv, P, 64)) if P else None
-    off, lens = _dev(offsets, torch.int32, (cache.n_seqs + 1,)), _dev(seq_lens, torch.int32, (cache.n_seqs,))
+        P = k_prefix.shape[1]
+        shape = (cache.H_kv, P, 64)
+        kp, vp = _at(k_prefix, here, bf, shape), _at(v_prefix, here, bf, shape)
     if workspace is None:
         raise HttmError("a workspace of attention_cached_workspace() bytes is needed")
-    _same_device(q, k_prefix, v_prefix, cache.k_pages, offsets, seq_lens, out, workspace)
-    _check(lib().httm_attention_cached(C.byref(rows), kp, vp, P, C.byref(cache.struct), off, lens, n, H_q, 64, float(scale),
-                                       1 if causal else 0, _dev(out, bf, (n, H_q * 64)), _dev(workspace, torch.uint8),
-                                       workspace.numel(), _stream()), "httm_attention_cached")
+    cache.check_device(here)
+    rc = lib().httm_attention_cached(C.byref(_rows(q, here, H_q, bf)), kp, vp, P, C.byref(cache.struct),
+                                     _at(offsets, here, torch.int32, (cache.n_seqs + 1,)), _at(seq_lens, here, torch.int32, (cache.n_seqs,)),
+                                     n, H_q, 64, scale, 1 if causal else 0, _at(out, here, bf, (n, H_q * 64)),
+                                     _at(workspace, here, torch.uint8), workspace.numel(), _stream_of(here))
+    if rc:
+        _check(rc, "httm_attention_cached")
     return out
