@@ -4,17 +4,17 @@
 // Rows.  The query heads that share a key head and the tokens of a sequence are rows of one matrix: row r of sequence b and
 // key head h is token offsets[b] + r / group, query head h * group + r % group.  A tile is R of these rows.
 //
-// The line.  The work of a launch is one line of units: for every key head, every sequence, every tile of its rows, the
-// units of kUnit keys that the tile attends to, prefix first.  It is cut into equal shares, one per workgroup, wherever the
-// cuts fall; lengths are read on the device, so a captured call follows the sequences as they grow.  A workgroup finds
-// the start of its share by a scan over the sequences, and walks.  What a share holds of a tile is a piece; a piece that is
-// not its whole tile leaves its maximum, sum and un-normalised product in the workspace, and combine_kernel adds
-// the pieces of every row up, in the order of the keys: results are run-to-run identical.
+// The line.  The work of a launch is one line: for every key head, every sequence, every tile of its rows, the keys
+// that the tile attends to, prefix first.  It is cut into equal shares, one per workgroup, wherever the cuts fall
+// (in the tile at the next unit of keys); lengths are read on the device, so a captured call follows the sequences as
+// they grow.  A workgroup finds the start of its share by a scan over the sequences, and walks.  What a share holds of a tile
+// is a piece; a piece that is not its whole tile leaves its maximum, sum and un-normalised product in the workspace, and
+// combine_kernel adds the pieces of every row up, in the order of the keys: results are run-to-run identical.
 //
-// Prefix, computed once.  Where sequences have few rows each, the prefix is a launch of its own whose tiles are cut from the
-// rows of all sequences together, so that its keys are read once per tile of the whole batch and not per
-// sequence; combine_kernel joins it with the own keys.  Where a sequence fills tiles by itself, that would save nothing:
-// there its tiles run over prefix and own keys in one go.
+// Prefix, computed once.  Where sequences have few rows each, the line has two parts: the prefix against tiles that are cut
+// from the rows of all sequences together, so that its keys are read once per tile of the whole batch and not per
+// sequence, and behind it every sequence's own keys; combine_kernel joins the two.  Where a sequence fills tiles by
+// itself, that would save nothing: there its tiles run over prefix and own keys in one go.
 //
 // A wave.  S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (A = 16 keys x 32 channels, B = 32 channels x 16 rows): a lane has
 // one row's scores of 4 of 16 keys, so that statistics are sums in a lane and two exchanges.  The weights go from the
@@ -44,17 +44,21 @@ struct RowPieces {
   int32_t first, base, stride, n;   // n = 0: the row is written already
 };
 
-struct LineArgs {
-  CachedAttnArgs c;
-  int32_t H_q;
+// A part of the line
+struct Part {
   int32_t stacked;        // one sequence that has the tokens of all of them
   int32_t with_prefix, with_own;
-  int32_t finish;         // whole tiles are written to o; else every piece is left in its slot
-  int32_t min_units;      // a share has at least so many
   int32_t max_slots;
   RowPieces* rows;        // [n_tokens * H_q]
   float2* slot_ml;        // [max_slots][R] shift (log2 units) and sum
   float* slot_o;          // [max_slots][R][64]
+};
+struct LineArgs {
+  CachedAttnArgs c;
+  int32_t H_q;
+  int32_t finish;         // (one part) whole tiles are written to o; else every piece is left in its slot
+  int32_t min_length;     // positions that a share has at least
+  Part part[2];
 };
 
 // over the four lane groups that share a row
@@ -78,45 +82,6 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
 }
 
-// A sequence as the line sees it
-struct Seq {
-  int first, n;    // tokens
-  int len;         // own keys
-  int tiles;       // of R rows
-  int units;       // of a tile, at least one: rows without keys are written too
-};
-template <int R, int UNIT>
-__device__ __forceinline__ void count(const LineArgs& a, Seq& s) {
-  const int keys = (a.with_prefix ? ((int)a.c.P + UNIT - 1) / UNIT : 0) + (s.len + UNIT - 1) / UNIT;
-  s.tiles = (s.n * a.c.group + R - 1) / R;
-  s.units = keys > 1 ? keys : 1;
-}
-// 64 sequences from `base` on, one per lane; those behind the last have no tokens
-template <int R, int UNIT>
-__device__ __forceinline__ Seq load_window(const LineArgs& a, int base, int lane) {
-  const CachedAttnArgs& c = a.c;
-  const int n_seq = a.stacked ? 1 : c.cache.n_seqs, b = base + lane, T = (int)c.n_tokens;
-  Seq s = {};
-  if (b < n_seq) {
-    const int o0 = c.offsets[b], o1 = c.offsets[a.stacked ? c.cache.n_seqs : b + 1];
-    const int len = a.with_own ? c.seq_lens[b] : 0;
-    s.first = std::clamp(o0, 0, T);
-    s.n = std::clamp(o1, s.first, T) - s.first;
-    s.len = std::clamp(len, 0, c.cache.table_stride << c.cache.page_shift);
-  }
-  count<R, UNIT>(a, s);
-  return s;
-}
-template <int R, int UNIT>
-__device__ __forceinline__ Seq of_lane(const LineArgs& a, const Seq& window, int l) {
-  Seq s;
-  s.first = __builtin_amdgcn_readlane(window.first, l);
-  s.n = __builtin_amdgcn_readlane(window.n, l);
-  s.len = __builtin_amdgcn_readlane(window.len, l);
-  count<R, UNIT>(a, s);
-  return s;
-}
-
 // floor(x / y) for 0 <= x, 0 < y, both below 2^52: the compiler's 64-bit division takes some 200 instructions, in front of
 // everything else that a workgroup does
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
@@ -126,55 +91,142 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
   return uniform64(q);
 }
 
-// Where a share starts
-struct Place {
-  int h, b, tile, unit;
-  int tile_id;      // of (h, b, tile) in the line
-  int64_t at, end;  // units of the share, as positions on the line
-  int64_t per_share, longer;    // units of a share; the first `longer` shares have one more
-  int share;
-  int base;         // first sequence of the window
-  // the share that has unit x of the line
-  __device__ __forceinline__ int share_of(int64_t x) const {
-    const int64_t split = longer * (per_share + 1);
-    return (int)(x < split ? quotient(x, per_share + 1) : longer + quotient(x - split, per_share));
+// What a tile costs besides its keys - rows in, statistics and product joined and out - in keys
+constexpr int kTileCost = 256;
+
+// A sequence as the line sees it.  Positions on the line are units of kUnit keys, or single keys where tiles are large (FINE).  A
+// tile is as long as the keys that its last row sees, behind kTileCost; with `causal` and FINE those grow by `grow` from tile to
+// tile (rounded down, the last tile apart: lengths on the line only share out the work).
+struct Seq {
+  int first, n;    // tokens
+  int len;         // own keys
+  int tiles;       // of R rows
+  int last;        // length of the last tile
+  int base, grow;  // of tile j before the last: base + grow * (j + 1)
+  __device__ __forceinline__ int64_t before(int j) const { return (int64_t)j * base + (int64_t)grow * j * (j + 1) / 2; }
+  __device__ __forceinline__ int length(int j) const { return j == tiles - 1 ? last : base + grow * (j + 1); }
+  __device__ __forceinline__ int64_t total() const { return tiles ? before(tiles - 1) + last : 0; }
+  // the tile that has position x of the sequence
+  __device__ __forceinline__ int tile_at(int64_t x) const {
+    if (tiles == 1) return 0;
+    int64_t j;
+    if (grow == 0) {
+      j = quotient(x, base);
+    } else {
+      const double b = 2.0 * base + grow;
+      j = (int64_t)((sqrt(b * b + 8.0 * grow * (double)x) - b) / (2.0 * grow));
+    }
+    int t = uniform((int)std::clamp<int64_t>(j, 0, tiles - 1));
+    while (t > 0 && before(t) > x) --t;
+    while (t + 1 < tiles && before(t + 1) <= x) ++t;
+    return t;
   }
 };
-template <int R, int UNIT>
-__device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p, Seq& window) {
-  const int n_seq = a.stacked ? 1 : a.c.cache.n_seqs;
-  const int lanes = n_seq < 64 ? n_seq : 64;
-  window = load_window<R, UNIT>(a, 0, lane);
-  int64_t sum = (int64_t)window.tiles * window.units;
+template <bool FINE>
+constexpr int kTileFront = FINE ? kTileCost : kTileCost / kUnit;     // positions of kTileCost
+
+template <int R, bool CAUSAL, bool FINE>
+__device__ __forceinline__ void measure(const LineArgs& a, const Part& part, Seq& s) {
+  const int P = part.with_prefix ? (int)a.c.P : 0;
+  s.tiles = (s.n * a.c.group + R - 1) / R;
+  s.last = kTileFront<FINE> + (FINE ? P + s.len : (P + kUnit - 1) / kUnit + (s.len + kUnit - 1) / kUnit);
+  const bool grows = FINE && CAUSAL && part.with_own;
+  s.grow = !grows ? 0 : a.c.group < R ? R / a.c.group : 1;
+  s.base = !grows ? s.last : std::max(s.last - s.n, kTileFront<FINE>);
+}
+// 64 sequences from `base` on, one per lane; those behind the last have no tokens
+template <int R, bool CAUSAL, bool FINE>
+__device__ __forceinline__ Seq load_window(const LineArgs& a, const Part& part, int base, int lane) {
+  const CachedAttnArgs& c = a.c;
+  const int n_seq = part.stacked ? 1 : c.cache.n_seqs, b = base + lane, T = (int)c.n_tokens;
+  Seq s = {};
+  if (b < n_seq) {
+    const int o0 = c.offsets[b], o1 = c.offsets[part.stacked ? c.cache.n_seqs : b + 1];
+    const int len = part.with_own ? c.seq_lens[b] : 0;
+    s.first = std::clamp(o0, 0, T);
+    s.n = std::clamp(o1, s.first, T) - s.first;
+    s.len = std::clamp(len, 0, c.cache.table_stride << c.cache.page_shift);
+  }
+  measure<R, CAUSAL, FINE>(a, part, s);
+  return s;
+}
+template <int R, bool CAUSAL, bool FINE>
+__device__ __forceinline__ Seq of_lane(const LineArgs& a, const Part& part, const Seq& window, int l) {
+  Seq s;
+  s.first = __builtin_amdgcn_readlane(window.first, l);
+  s.n = __builtin_amdgcn_readlane(window.n, l);
+  s.len = __builtin_amdgcn_readlane(window.len, l);
+  measure<R, CAUSAL, FINE>(a, part, s);
+  return s;
+}
+
+// A part of the line in all, for a key head
+struct Extent {
+  int64_t length;
+  int tiles;
+};
+template <int R, bool CAUSAL, bool FINE>
+__device__ __forceinline__ Extent extent(const LineArgs& a, const Part& part, int lane, Seq& window) {
+  const int n_seq = part.stacked ? 1 : a.c.cache.n_seqs;
+  window = load_window<R, CAUSAL, FINE>(a, part, 0, lane);
+  int64_t sum = window.total();
   int tiles = window.tiles;
   for (int i = 64; i < n_seq; i += 64) {
-    const Seq s = load_window<R, UNIT>(a, i, lane);
-    sum += (int64_t)s.tiles * s.units;
+    const Seq s = load_window<R, CAUSAL, FINE>(a, part, i, lane);
+    sum += s.total();
     tiles += s.tiles;
   }
-  for (int i = 1; i < lanes; i <<= 1) {
+  for (int i = 1; i < n_seq && i < 64; i <<= 1) {
     sum += __shfl_xor(sum, i);
     tiles += __shfl_xor(tiles, i);
   }
-  const int64_t per_head = uniform64(sum);
-  const int tiles_per_head = uniform(tiles);
-  if (per_head == 0) return false;
-  const int64_t total = per_head * a.c.cache.H_kv;
-  const int shares = (int)std::clamp<int64_t>(quotient(total, a.min_units), 1, gridDim.x);
+  return {uniform64(sum), uniform(tiles)};
+}
+
+// A workgroup's share: positions [at, end) of the line
+struct Share {
+  int id;
+  int64_t at, end;
+  int64_t length, longer;    // of a share; the first `longer` shares have one more
+  // the share that has position x of the line
+  __device__ __forceinline__ int of(int64_t x) const {
+    const int64_t split = longer * (length + 1);
+    return (int)(x < split ? quotient(x, length + 1) : longer + quotient(x - split, length));
+  }
+};
+__device__ __forceinline__ bool find_share(const LineArgs& a, int64_t total, Share& s) {
+  if (total == 0) return false;
+  const int shares = (int)std::clamp<int64_t>(quotient(total, a.min_length), 1, gridDim.x);
   // workgroups go to the 8 XCDs in turn: shares next to each other, which read the same keys, go to one of them
   const int per_xcd = (shares + 7) / 8;
-  p.share = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_xcd || p.share >= shares) return false;
-  p.per_share = quotient(total, shares);
-  p.longer = total - p.per_share * shares;
-  p.at = p.share * p.per_share + std::min<int64_t>(p.share, p.longer);
-  p.end = p.at + p.per_share + (p.share < p.longer ? 1 : 0);
-  p.h = (int)quotient(p.at, per_head);
-  int64_t rest = p.at - p.h * per_head;
+  s.id = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_xcd || s.id >= shares) return false;
+  s.length = quotient(total, shares);
+  s.longer = total - s.length * shares;
+  s.at = s.id * s.length + std::min<int64_t>(s.id, s.longer);
+  s.end = s.at + s.length + (s.id < s.longer ? 1 : 0);
+  return true;
+}
+// (A cut that falls in a tile's front, its kTileCost, is one in front of the tile: see cut_piece().)
+
+// Where a walk along a part is
+struct Place {
+  int h, b, tile;
+  int tile_id;      // of (h, b, tile) in the part
+  int at;           // position in the tile
+  int base;         // first sequence of the window
+};
+// x: position in the part
+template <int R, bool CAUSAL, bool FINE>
+__device__ __forceinline__ bool find_place(const LineArgs& a, const Part& part, const Extent& ex, int64_t x, int lane, Place& p, Seq& window) {
+  const int n_seq = part.stacked ? 1 : a.c.cache.n_seqs;
+  const int lanes = n_seq < 64 ? n_seq : 64;
+  p.h = (int)quotient(x, ex.length);
+  int64_t rest = x - p.h * ex.length;
   int before = 0;
   for (p.base = 0;; p.base += 64) {
-    if (p.base > 0) window = load_window<R, UNIT>(a, p.base, lane);
-    int64_t scan = (int64_t)window.tiles * window.units;
+    if (p.base > 0 || n_seq > 64) window = load_window<R, CAUSAL, FINE>(a, part, p.base, lane);
+    int64_t scan = window.total();
     int tscan = window.tiles;
     for (int d = 1; d < lanes; d <<= 1) {
       const int64_t v = __shfl_up(scan, d);
@@ -190,35 +242,32 @@ __device__ __forceinline__ bool find_share(const LineArgs& a, int lane, Place& p
       continue;
     }
     const int l = __builtin_ctzll(in);
-    const Seq s = of_lane<R, UNIT>(a, window, l);
-    rest -= uniform64(__shfl(scan, l)) - (int64_t)s.tiles * s.units;
+    const Seq s = of_lane<R, CAUSAL, FINE>(a, part, window, l);
+    rest -= uniform64(__shfl(scan, l)) - s.total();
     p.b = p.base + l;
-    p.tile = (int)quotient(rest, s.units);
-    p.unit = (int)(rest - (int64_t)p.tile * s.units);
-    p.tile_id = p.h * tiles_per_head + before + uniform(__shfl(tscan, l)) - s.tiles + p.tile;
+    p.tile = s.tile_at(rest);
+    p.at = (int)(rest - s.before(p.tile));
+    p.tile_id = p.h * ex.tiles + before + uniform(__shfl(tscan, l)) - s.tiles + p.tile;
     return true;
   }
 }
-
-// On to the next tile, behind a piece of `done` units; false at the end of the share
-template <int R, int UNIT>
-__device__ __forceinline__ bool next_tile(const LineArgs& a, Place& p, Seq& window, Seq& s, int done, int lane) {
-  p.at += done;
-  p.unit = 0;
+// On to the start of the next tile; false behind the last
+template <int R, bool CAUSAL, bool FINE>
+__device__ __forceinline__ bool next_tile(const LineArgs& a, const Part& part, Place& p, Seq& window, Seq& s, int lane) {
+  p.at = 0;
   ++p.tile_id;
-  if (p.at >= p.end) return false;
   if (++p.tile < s.tiles) return true;
   p.tile = 0;
   do {
-    if (++p.b == (a.stacked ? 1 : a.c.cache.n_seqs)) {
+    if (++p.b == (part.stacked ? 1 : a.c.cache.n_seqs)) {
       p.b = 0;
       if (++p.h == a.c.cache.H_kv) return false;
     }
     if (p.b < p.base || p.b >= p.base + 64) {
       p.base = p.b;
-      window = load_window<R, UNIT>(a, p.b, lane);
+      window = load_window<R, CAUSAL, FINE>(a, part, p.b, lane);
     }
-    s = of_lane<R, UNIT>(a, window, p.b - p.base);
+    s = of_lane<R, CAUSAL, FINE>(a, part, window, p.b - p.base);
   } while (s.tiles == 0);
   return true;
 }
@@ -240,50 +289,75 @@ __device__ __forceinline__ int seen_by(const LineArgs& a, const Seq& s, int r) {
   return CAUSAL ? std::clamp(s.len - s.n + r / a.c.group + 1, 0, s.len) : s.len;
 }
 
-// Where a piece of units [u0, u1) goes: to o, or to a slot
+// What a share has of a tile: positions [at, to) of it, units [u0, u1) of keys; nothing if it ends in the tile's front
+struct Piece {
+  int to, u0, u1;
+  bool starts, ends;
+};
+template <int UNIT, bool FINE>
+__device__ __forceinline__ bool cut_piece(Piece& c, const Place& p, const Seq& s, int P, int64_t left, int most) {
+  constexpr int F = kTileFront<FINE>;
+  const int length = s.length(p.tile), prefix_units = (P + UNIT - 1) / UNIT;
+  c.to = (int)std::min<int64_t>(length, p.at + left);
+  c.starts = p.at <= F;
+  c.ends = c.to == length;
+  const int units = prefix_units + (most + UNIT - 1) / UNIT;
+  auto unit_at = [&](int x) {
+    x -= F;
+    return std::min(units, !FINE ? x : x <= P ? (x + UNIT - 1) / UNIT : prefix_units + (x - P + UNIT - 1) / UNIT);
+  };
+  c.u0 = c.starts ? 0 : unit_at(p.at);
+  c.u1 = c.ends ? units : unit_at(c.to);
+  return c.ends || c.to > F;
+}
+
+// Where a piece goes: to o, or to a slot
 struct Target {
   bool finish;
   int slot;
 };
-// (by one wave: `threads` of them from `thread` on) The piece that has a tile's first unit says where the others are.
+// The piece that starts a tile says where the others are; `first`: the share's first one, `tile`: where the tile starts on the line.
+// By the first 64 threads.
 template <int R>
-__device__ __forceinline__ Target place_piece(const LineArgs& a, const Place& p, const Seq& s, int64_t share_start, int u0, int u1, int thread,
-                                              int threads) {
-  Target t = {a.finish && u0 == 0 && u1 == s.units, 0};
-  if (!t.finish) t.slot = a.finish ? 2 * p.share + (p.at == share_start ? 0 : 1) : p.share + p.tile_id;
-  if (u0 == 0 && thread < threads) {
+__device__ __forceinline__ Target place_piece(const LineArgs& a, const Part& part, const Share& share, const Place& p, const Seq& s,
+                                              const Piece& c, bool first, int64_t tile) {
+  Target t = {a.finish && c.starts && c.ends, 0};
+  if (!t.finish) t.slot = a.finish ? 2 * share.id + (first ? 0 : 1) : share.id + p.tile_id;
+  if (c.starts && threadIdx.x < 64) {
     const int r0 = p.tile * R, n_rows = s.n * a.c.group;
     RowPieces rp = {0, 0, 0, 0};
     if (!t.finish) {
-      rp.n = p.share_of(p.at + s.units - 1) - p.share + 1;
+      rp.n = share.of(tile + s.length(p.tile) - 1) - share.id + 1;
       rp.first = t.slot * R;
-      rp.base = (a.finish ? 2 * p.share : t.slot) * R;
+      rp.base = (a.finish ? 2 * share.id : t.slot) * R;
       rp.stride = a.finish ? 2 * R : R;
     }
-    for (int i = thread; i < R; i += threads)
+    for (int i = threadIdx.x; i < R; i += 64)
       if (r0 + i < n_rows) {
         const Row r = row_of(a, p, s, r0 + i);
-        a.rows[(int64_t)r.token * a.H_q + r.head] = {rp.first + i, rp.base + i, rp.stride, rp.n};
+        part.rows[(int64_t)r.token * a.H_q + r.head] = {rp.first + i, rp.base + i, rp.stride, rp.n};
       }
   }
   return t;
 }
 // Four channels of a row of the tile; l: the row's sum
 template <int R>
-__device__ __forceinline__ void put(const LineArgs& a, const Place& p, const Seq& s, const Target& t, int r, int channel, const f32x4& o, float l) {
+__device__ __forceinline__ void put(const LineArgs& a, const Part& part, const Place& p, const Seq& s, const Target& t, int r, int channel,
+                                    const f32x4& o, float l) {
   if (p.tile * R + r >= s.n * a.c.group) return;
   if (t.finish) {
     const float f = l == 0.f ? 0.f : 1.f / l;
     const Row row = row_of(a, p, s, p.tile * R + r);
     *(u32x2*)((char*)a.c.o + (((int64_t)row.token * a.H_q + row.head) * kDHead + channel) * 2) =
         u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
-  } else if (t.slot < a.max_slots) {
-    *(f32x4*)(a.slot_o + ((int64_t)t.slot * R + r) * kDHead + channel) = o;
+  } else if (t.slot < part.max_slots) {
+    *(f32x4*)(part.slot_o + ((int64_t)t.slot * R + r) * kDHead + channel) = o;
   }
 }
 template <int R>
-__device__ __forceinline__ void put_sums(const LineArgs& a, const Place& p, const Seq& s, const Target& t, int r, float m, float l) {
-  if (!t.finish && t.slot < a.max_slots && p.tile * R + r < s.n * a.c.group) a.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
+__device__ __forceinline__ void put_sums(const LineArgs& a, const Part& part, const Place& p, const Seq& s, const Target& t, int r, float m,
+                                         float l) {
+  if (!t.finish && t.slot < part.max_slots && p.tile * R + r < s.n * a.c.group) part.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
 }
 
 // V^T operands: 16 channels x 32 keys in the order of the weights (see the top)
@@ -433,31 +507,31 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, b
   }
 }
 
-constexpr int waves_per_simd(int nq) { return nq == 1 ? 3 : 2; }
-
-template <int NQ, int KS, bool CAUSAL>
-__global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_per_simd(NQ), waves_per_simd(NQ)))) void attention_cached_kernel(
-    const LineArgs a) {
-  constexpr int R = 16 * NQ;
+// A share's way along a part of the line: four waves take the units of a piece in turn.  [x, end): positions in the part, `line`:
+// where it starts on the line.
+constexpr int kWaves = 4;
+template <int NQ, bool CAUSAL>
+__device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const Share& share, const Extent& ex, int64_t line, int64_t x,
+                                     int64_t end, Seq window, char* s_mem, float2* s_ml) {
+  constexpr int R = 16 * NQ, KS = kWaves;
   constexpr int DEPTH = 1;     // units of a wave on their way besides the one in work
-  __shared__ __attribute__((aligned(16))) char s_mem[KS * kUnitBytes];
-  __shared__ float2 s_ml[KS > 1 ? KS : 1][R];
   const CachedAttnArgs& c = a.c;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int l16 = lane & 15, grp = lane >> 4;
   bf16_t* sv = (bf16_t*)(s_mem + wave * kUnitBytes);
   Place p;
-  Seq window;
-  if (!find_share<R, kUnit>(a, lane, p, window)) return;
-  Seq s = of_lane<R, kUnit>(a, window, p.b - p.base);
-  const int prefix_units = a.with_prefix ? ((int)c.P + kUnit - 1) / kUnit : 0;
-  const int64_t share_start = p.at;
+  if (!find_place<R, CAUSAL, false>(a, part, ex, x, lane, p, window)) return;
+  Seq s = of_lane<R, CAUSAL, false>(a, part, window, p.b - p.base);
+  const int P = part.with_prefix ? (int)c.P : 0, prefix_units = (P + kUnit - 1) / kUnit;
   const int k_offset = l16 * kRowBytes + grp * 16, v_offset = lane * 16;
+  bool first = true;
 
-  while (p.at < p.end) {
-    const int u0 = p.unit;
-    const int u1 = (int)std::min<int64_t>(s.units, p.unit + (p.end - p.at));
+  while (true) {
     const int n_rows = s.n * c.group, r0 = p.tile * R;
+    const int least = uniform(seen_by<CAUSAL>(a, s, r0)), most = uniform(seen_by<CAUSAL>(a, s, std::min(r0 + R, n_rows) - 1));
+    Piece piece;
+    if (!cut_piece<kUnit, false>(piece, p, s, P, end - x, most)) return;
+    const int stop = piece.u1;
     // (constant memory: scalar loads, which are waited for apart from those of the keys)
     const auto* table = (const __attribute__((address_space(4))) int32_t*)(c.cache.table + (int64_t)p.b * c.cache.table_stride);
 
@@ -521,12 +595,9 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int least = uniform(seen_by<CAUSAL>(a, s, r0)), most = uniform(seen_by<CAUSAL>(a, s, std::min(r0 + R, n_rows) - 1));
-    // keys behind the last one that a row of the tile sees are not read
-    const int stop = std::min(u1, prefix_units + (most + kUnit - 1) / kUnit);
     // DEPTH units are on their way, the pages of the next one are asked for.  (The data moves through registers: two copies
     // of the step in the loop need more scalar registers than there are.)
-    int unit = u0 + wave;
+    int unit = piece.u0 + wave;
     UnitData d[DEPTH + 1];
     int ok[DEPTH + 1];
     Pages g = look_up(unit);
@@ -540,7 +611,7 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
       if (unit + DEPTH * KS < stop) ok[DEPTH] = fetch(unit + DEPTH * KS, g, d[DEPTH]);
       g = look_up(unit + (DEPTH + 1) * KS);
       const bool own = unit >= prefix_units;
-      unit_step<NQ, CAUSAL>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : (int)c.P, ok[0], own, lane);
+      unit_step<NQ, CAUSAL>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane);
 #pragma unroll
       for (int i = 0; i < DEPTH; ++i) {
         d[i] = d[i + 1];
@@ -549,30 +620,21 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
     }
 
     // ---- the piece's end ---------------------------------------------------------------------------------
-    const Target to = place_piece<R>(a, p, s, share_start, u0, u1, threadIdx.x, 64);
-    if constexpr (KS == 1) {
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        const float l = groups_sum(w.l[qt]);
-        const int r = 16 * qt + l16;
-        if (grp == 0) put_sums<R>(a, p, s, to, r, w.m[qt], l);
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct) put<R>(a, p, s, to, r, 16 * ct + 4 * grp, w.o[ct][qt], l);
-      }
-    } else {
+    const Target to = place_piece<R>(a, part, share, p, s, piece, first, line + x - p.at);
+    {
       float f[NQ];
 #pragma unroll
       for (int qt = 0; qt < NQ; ++qt) {
         const float l = groups_sum(w.l[qt]);
-        if (grp == 0) s_ml[wave][16 * qt + l16] = float2{w.m[qt], l};
+        if (grp == 0) s_ml[wave * R + 16 * qt + l16] = float2{w.m[qt], l};
       }
       __syncthreads();
       auto joined = [&](int r) {
-        float m = s_ml[0][r].x, l = 0.f;
+        float m = s_ml[r].x, l = 0.f;
 #pragma unroll
-        for (int i = 1; i < KS; ++i) m = fmaxf(m, s_ml[i][r].x);
+        for (int i = 1; i < KS; ++i) m = fmaxf(m, s_ml[i * R + r].x);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) l += s_ml[i][r].y * __builtin_amdgcn_exp2f(s_ml[i][r].x - m);
+        for (int i = 0; i < KS; ++i) l += s_ml[i * R + r].y * __builtin_amdgcn_exp2f(s_ml[i * R + r].x - m);
         return float2{m, l};
       };
 #pragma unroll
@@ -588,15 +650,43 @@ __global__ __launch_bounds__(64 * KS) __attribute__((amdgpu_waves_per_eu(waves_p
 #pragma unroll
           for (int k = 1; k < KS; ++k) o += so[k * R * 4 + i];
           const float2 ml = joined(i >> 2);
-          if (ct == 0 && (i & 3) == 0) put_sums<R>(a, p, s, to, i >> 2, ml.x, ml.y);
-          put<R>(a, p, s, to, i >> 2, 16 * ct + 4 * (i & 3), o, ml.y);
+          if (ct == 0 && (i & 3) == 0) put_sums<R>(a, part, p, s, to, i >> 2, ml.x, ml.y);
+          put<R>(a, part, p, s, to, i >> 2, 16 * ct + 4 * (i & 3), o, ml.y);
         }
         __syncthreads();
       }
     }
 
-    if (!next_tile<R, kUnit>(a, p, window, s, u1 - u0, lane)) return;
+    x += piece.to - p.at;
+    if (x >= end || !next_tile<R, CAUSAL, false>(a, part, p, window, s, lane)) return;
+    first = false;
   }
+}
+
+// NA query tiles of 16 rows for the first part of the line, the prefix against all sequences' rows, or 0: there is none;
+// NB for the second.
+constexpr int waves_per_simd(int nq) { return nq == 1 ? 3 : 2; }
+template <int NA, int NB, bool CAUSAL>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(waves_per_simd(NA > NB ? NA : NB), waves_per_simd(NA > NB ? NA : NB)))) void
+attention_cached_kernel(const LineArgs a) {
+  constexpr int kMost = NA > NB ? NA : NB;
+  __shared__ __attribute__((aligned(16))) char s_mem[kWaves * kUnitBytes];
+  __shared__ float2 s_ml[kWaves * 16 * kMost];
+  const int lane = threadIdx.x & 63;
+  Seq window_a = {}, window_b;
+  Extent ea = {0, 0};
+  if constexpr (NA > 0) ea = extent<16 * NA, false, false>(a, a.part[0], lane, window_a);
+  const Extent eb = extent<16 * NB, CAUSAL, false>(a, a.part[1], lane, window_b);
+  const int64_t total_a = ea.length * a.c.cache.H_kv, total_b = eb.length * a.c.cache.H_kv;
+  Share share;
+  if (!find_share(a, total_a + total_b, share)) return;
+  if constexpr (NA > 0)
+    if (share.at < total_a) {
+      walk<NA, false>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
+      __syncthreads();
+    }
+  if (share.end > total_a)
+    walk<NB, CAUSAL>(a, a.part[1], share, eb, total_a, std::max(share.at, total_a) - total_a, share.end - total_a, window_b, s_mem, s_ml);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------
@@ -648,12 +738,17 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
   const CachedAttnArgs& c = a.c;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int l16 = lane & 15, grp = lane >> 4;
-  Place p;
+  const Part& part = a.part[0];
   Seq window;
-  if (!find_share<R, UNIT>(a, lane, p, window)) return;
-  Seq s = of_lane<R, UNIT>(a, window, p.b - p.base);
-  const int prefix_units = a.with_prefix ? ((int)c.P + UNIT - 1) / UNIT : 0;
-  const int64_t share_start = p.at;
+  const Extent ex = extent<R, CAUSAL, true>(a, part, lane, window);
+  Share share;
+  if (!find_share(a, ex.length * c.cache.H_kv, share)) return;
+  Place p;
+  if (!find_place<R, CAUSAL, true>(a, part, ex, share.at, lane, p, window)) return;
+  Seq s = of_lane<R, CAUSAL, true>(a, part, window, p.b - p.base);
+  const int P = part.with_prefix ? (int)c.P : 0, prefix_units = (P + UNIT - 1) / UNIT;
+  int64_t x = share.at;
+  bool first = true;
   // lanes' offsets: K operands (channel halves), V operands (channel quarters), the rows that a wave brings (K, V)
   int k_at[2], v_at[4], to_k, to_v;
 #pragma unroll
@@ -682,14 +777,14 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
   };
 
   while (true) {
-    const int u0 = p.unit;
-    const int u1 = (int)std::min<int64_t>(s.units, p.unit + (p.end - p.at));
     const int n_rows = s.n * c.group, r0 = p.tile * R, wr0 = r0 + wave * 16 * NQ;
     const auto* table = (const __attribute__((address_space(4))) int32_t*)(c.cache.table + (int64_t)p.b * c.cache.table_stride);
     const bool active = uniform(wr0 < n_rows) != 0;
     const int least = uniform(seen_by<CAUSAL>(a, s, std::min(wr0, n_rows - 1)));
     const int most = uniform(seen_by<CAUSAL>(a, s, std::min(r0 + R, n_rows) - 1));
-    const int stop = std::min(u1, prefix_units + (most + UNIT - 1) / UNIT);
+    Piece piece;
+    if (!cut_piece<UNIT, true>(piece, p, s, P, share.end - x, most)) return;
+    const int u0 = piece.u0, stop = piece.u1;
 
     WideState w;
 #pragma unroll
@@ -896,7 +991,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       }
       for (int unit = u0; unit < stop; ++unit) {
         const bool own = unit >= prefix_units;
-        const int row0 = (own ? unit - prefix_units : unit) * UNIT, end = own ? least : (int)c.P;
+        const int row0 = (own ? unit - prefix_units : unit) * UNIT, end = own ? least : P;
         const uint32_t ok = ok_of(unit);
         if (active) step(kHalf, row0, end, ok & 3, own);
         barrier();      // K of this unit and V of the one before have been read by everybody
@@ -919,30 +1014,32 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       }
     }
 
-    const Target to = place_piece<R>(a, p, s, share_start, u0, u1, threadIdx.x, 64);
+    const Target to = place_piece<R>(a, part, share, p, s, piece, first, x - p.at);
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
       const float l = groups_sum(w.l[qt]);
       const int r = wave * 16 * NQ + 16 * qt + l16;
-      if (grp == 0) put_sums<R>(a, p, s, to, r, -w.m[qt], l);
+      if (grp == 0) put_sums<R>(a, part, p, s, to, r, -w.m[qt], l);
 #pragma unroll
-      for (int ct = 0; ct < 4; ++ct) put<R>(a, p, s, to, r, 16 * ct + 4 * grp, w.o[ct][qt], l);
+      for (int ct = 0; ct < 4; ++ct) put<R>(a, part, p, s, to, r, 16 * ct + 4 * grp, w.o[ct][qt], l);
     }
-    if (!next_tile<R, UNIT>(a, p, window, s, u1 - u0, lane)) return;
+    x += piece.to - p.at;
+    if (x >= share.end || !next_tile<R, CAUSAL, true>(a, part, p, window, s, lane)) return;
+    first = false;
     barrier();      // the buffers are free
   }
 }
 
 // ---- joining the pieces --------------------------------------------------------------------------------------
 
-struct Part {
+struct PartPieces {
   const RowPieces* rows;
   const float2* ml;
   const float* o;
   int32_t max_rows;
 };
 struct CombineArgs {
-  Part part[2];           // in the order of the keys
+  PartPieces part[2];     // in the order of the keys
   int32_t n_parts;
   int32_t n_seqs;
   int32_t H_q;
@@ -956,65 +1053,72 @@ template <int GP>
 __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
   __shared__ f32x4 s_o[GP > 1 ? 256 : 1];
   __shared__ float2 s_ml[GP > 1 ? 16 : 1];
-  const int group = threadIdx.x >> 4, l16 = threadIdx.x & 15;
-  const int64_t row = GP == 1 ? (int64_t)blockIdx.x * 16 + group : blockIdx.x;
+  constexpr int kAtOnce = 4;     // pieces on their way to a group
+  const int group = threadIdx.x >> 4, l16 = threadIdx.x & 15, turn = group % GP;
+  const int64_t row = (int64_t)blockIdx.x * (16 / GP) + group / GP;
   const int64_t t = row / a.H_q;
-  if (t >= a.n_tokens || t < a.offsets[0] || t >= a.offsets[a.n_seqs]) return;
+  const bool real = t < a.n_tokens && t >= a.offsets[0] && t < a.offsets[a.n_seqs];
   float m = kLowest, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   int pieces = 0;
-  for (int i = 0; i < a.n_parts; ++i) {
-    const Part& part = a.part[i];
+  for (int i = 0; real && i < a.n_parts; ++i) {
+    const PartPieces& part = a.part[i];
     const RowPieces rp = part.rows[row];
     pieces += rp.n;
-    for (int k = GP == 1 ? 0 : group; k < rp.n; k += GP) {
-      const int at = k == 0 ? rp.first : rp.base + k * rp.stride;
-      if (at < 0 || at >= part.max_rows) break;
-      const float2 ml = part.ml[at];
-      const f32x4 x = *(const f32x4*)(part.o + (int64_t)at * kDHead + 4 * l16);
-      const float top = fmaxf(m, ml.x);
-      const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml.x - top);
-      m = top;
-      l = l * f + ml.y * g;
-      o = o * f + x * g;
+    for (int k0 = turn; k0 < rp.n; k0 += GP * kAtOnce) {
+      float2 ml[kAtOnce];
+      f32x4 x[kAtOnce];
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e) {
+        const int k = std::min(k0 + e * GP, rp.n - 1);
+        const int64_t at = k == 0 ? rp.first : rp.base + (int64_t)k * rp.stride;
+        const int64_t in = std::clamp<int64_t>(at, 0, part.max_rows - 1);
+        ml[e] = part.ml[in];
+        x[e] = *(const f32x4*)(part.o + in * kDHead + 4 * l16);
+        if (k0 + e * GP >= rp.n || in != at) ml[e] = float2{kLowest, 0.f}, x[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e) {
+        const float top = fmaxf(m, ml[e].x);
+        const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(ml[e].x - top);
+        m = top;
+        l = l * f + ml[e].y * g;
+        o = o * f + x[e] * g;
+      }
     }
   }
-  if (pieces == 0) return;
   if constexpr (GP > 1) {
     if (l16 == 0) s_ml[group] = float2{m, l};
     s_o[threadIdx.x] = o;
     __syncthreads();
-    if (group != 0) return;
-    float top = s_ml[0].x;
+    if (turn != 0) return;
+    float top = m;
 #pragma unroll
-    for (int i = 1; i < GP; ++i) top = fmaxf(top, s_ml[i].x);
+    for (int i = 1; i < GP; ++i) top = fmaxf(top, s_ml[group + i].x);
     l = 0.f;
     o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < GP; ++i) {
-      const float f = __builtin_amdgcn_exp2f(s_ml[i].x - top);
-      l += s_ml[i].y * f;
-      o += s_o[i * 16 + l16] * f;
+      const float f = __builtin_amdgcn_exp2f(s_ml[group + i].x - top);
+      l += s_ml[group + i].y * f;
+      o += s_o[threadIdx.x + i * 16] * f;
     }
   }
+  if (pieces == 0) return;
   const float f = l == 0.f ? 0.f : 1.f / l;
   *(u32x2*)((char*)a.o + (row * kDHead + 4 * l16) * 2) = u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
 }
 
 // ---- what runs -----------------------------------------------------------------------------------------------
 
-struct Launch {
-  int rows;               // of a tile
-  int nq, ks;             // 16 * nq rows, ks waves that share out the keys; nq = 0: the wide kernel
-  bool stacked, with_prefix, with_own;
-  int shares;
-  int64_t slots;
-};
+// Tiles of the line's parts: query tiles of 16 rows in the kernel of few rows, 0: tiles of 256 rows in a launch of their own
 struct Choice {
-  Launch run[2];
-  int n;
-  bool finish;
-  int64_t rows_bytes;     // RowPieces of a launch
+  int tiles[2];             // of the part with the prefix against all rows (stacked), and of the sequences' part
+  bool stacked;             // there is a first part; else the second one has the prefix too
+  int shares[2];
+  int64_t slots[2];
+  int rows[2];              // of a tile
+  int64_t row_pieces;       // bytes of the RowPieces of a part
 };
 
 constexpr int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
@@ -1022,35 +1126,27 @@ constexpr int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   Choice c = {};
   const int64_t rows = n_tokens * (H_q / H_kv), mean = rows / n_seqs;
-  const bool stack = n_seqs > 1 && P > 0 && mean < 64;
-  auto few = [&](int64_t n) { return n <= 16; };
-  c.finish = !stack;
-  c.rows_bytes = align256(n_tokens * H_q * (int64_t)sizeof(RowPieces));
-  auto add = [&](int nq, int ks, bool stacked, bool prefix, bool own) {
-    Launch& l = c.run[c.n++];
-    l = {nq ? 16 * nq : kWideRows, nq, ks, stacked, prefix, own, 0, 0};
-    l.shares = ks == 1 ? 2048 : 512;
-    const int64_t tiles = H_kv * (stacked ? (rows + l.rows - 1) / l.rows : rows / l.rows + n_seqs);
-    l.slots = c.finish ? 2 * l.shares : l.shares + tiles;
-  };
-  // tiles of 256 rows for more than 64: below, their waves would have no rows
-  auto rows_for = [&](int64_t n) { return few(n) ? 1 : n <= 64 ? 4 : 0; };
-  if (stack) {
-    add(rows_for(rows), 4, true, true, false);
-    add(few(mean) ? 1 : 4, few(mean) ? 1 : 4, false, false, true);
-  } else {
-    add(rows_for(mean), 4, false, P > 0, true);
+  c.stacked = n_seqs > 1 && P > 0 && mean <= 64;
+  c.tiles[0] = !c.stacked ? 0 : rows <= 16 ? 1 : rows <= 1024 ? 4 : 0;
+  c.tiles[1] = mean <= 8 ? 1 : mean <= 24 ? 2 : mean <= 64 ? 4 : 0;
+  c.row_pieces = align256(n_tokens * H_q * (int64_t)sizeof(RowPieces));
+  const int most = std::max(c.tiles[0], c.tiles[1]);
+  for (int i = c.stacked ? 0 : 1; i < 2; ++i) {
+    c.rows[i] = c.tiles[i] ? 16 * c.tiles[i] : kWideRows;
+    c.shares[i] = 256 * (c.tiles[i] == 0 ? 2 : waves_per_simd(most));
+    const int64_t tiles = H_kv * (i == 0 ? (rows + c.rows[i] - 1) / c.rows[i] : rows / c.rows[i] + n_seqs);
+    c.slots[i] = c.stacked ? c.shares[i] + tiles : 2 * c.shares[i];
   }
   return c;
 }
-int64_t slot_bytes(const Launch& l) { return align256(l.slots * l.rows * 8) + align256(l.slots * l.rows * kDHead * 4); }
+int64_t slot_bytes(const Choice& c, int i) { return align256(c.slots[i] * c.rows[i] * 8) + align256(c.slots[i] * c.rows[i] * kDHead * 4); }
 
-template <int NQ, int KS>
+template <int NA, int NB>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
-  if (a.c.causal && a.with_own)
-    hipLaunchKernelGGL((attention_cached_kernel<NQ, KS, true>), dim3(shares), dim3(64 * KS), 0, stream, a);
+  if (a.c.causal)
+    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, true>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
   else
-    hipLaunchKernelGGL((attention_cached_kernel<NQ, KS, false>), dim3(shares), dim3(64 * KS), 0, stream, a);
+    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, false>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
 }
 
 }  // namespace
@@ -1058,7 +1154,7 @@ void start(const LineArgs& a, int shares, hipStream_t stream) {
 int64_t cached_attention_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   const Choice c = choose(n_tokens, n_seqs, H_q, H_kv, P);
   int64_t bytes = 0;
-  for (int i = 0; i < c.n; ++i) bytes += c.rows_bytes + slot_bytes(c.run[i]);
+  for (int i = c.stacked ? 0 : 1; i < 2; ++i) bytes += c.row_pieces + slot_bytes(c, i);
   return bytes;
 }
 
@@ -1066,47 +1162,53 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
   if (args.n_tokens == 0) return hipSuccess;
   const int H_kv = args.cache.H_kv, H_q = H_kv * args.group;
   const Choice ch = choose(args.n_tokens, args.cache.n_seqs, H_q, H_kv, args.P);
+  LineArgs a = {};
+  a.c = args;
+  a.H_q = H_q;
+  a.finish = !ch.stacked;
+  a.min_length = kWaves;
   CombineArgs cb = {};
-  cb.n_parts = ch.n;
   cb.n_seqs = args.cache.n_seqs;
   cb.H_q = H_q;
   cb.n_tokens = args.n_tokens;
   cb.offsets = args.offsets;
   cb.o = args.o;
   char* at = args.workspace;
-  for (int i = 0; i < ch.n; ++i) {
-    const Launch& l = ch.run[i];
-    LineArgs a = {};
-    a.c = args;
-    a.H_q = H_q;
-    a.stacked = l.stacked;
-    a.with_prefix = l.with_prefix;
-    a.with_own = l.with_own;
-    a.finish = ch.finish;
-    a.min_units = l.nq ? l.ks : 2;
-    a.max_slots = (int32_t)l.slots;
-    const int R = l.rows;
-    a.rows = (RowPieces*)at;
-    a.slot_ml = (float2*)(at + ch.rows_bytes);
-    a.slot_o = (float*)(at + ch.rows_bytes + align256(l.slots * R * 8));
-    at += ch.rows_bytes + slot_bytes(l);
-    cb.part[i] = {a.rows, a.slot_ml, a.slot_o, (int32_t)(l.slots * R)};
-    if (l.nq == 1 && l.ks == 1)
-      start<1, 1>(a, l.shares, stream);
-    else if (l.nq == 1)
-      start<1, 4>(a, l.shares, stream);
-    else if (l.nq == 4)
-      start<4, 4>(a, l.shares, stream);
-    else if (a.c.causal && a.with_own)
-      hipLaunchKernelGGL(attention_cached_wide_kernel<true>, dim3(l.shares), dim3(64 * kWideWaves), 0, stream, a);
-    else
-      hipLaunchKernelGGL(attention_cached_wide_kernel<false>, dim3(l.shares), dim3(64 * kWideWaves), 0, stream, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  for (int i = ch.stacked ? 0 : 1; i < 2; ++i) {
+    const int64_t rows = ch.slots[i] * ch.rows[i];
+    a.part[i] = {ch.stacked && i == 0, !ch.stacked || i == 0, i == 1, (int32_t)ch.slots[i], (RowPieces*)at, (float2*)(at + ch.row_pieces),
+                 (float*)(at + ch.row_pieces + align256(rows * 8))};
+    at += ch.row_pieces + slot_bytes(ch, i);
+    cb.part[cb.n_parts++] = {a.part[i].rows, a.part[i].slot_ml, a.part[i].slot_o, (int32_t)rows};
   }
+  // Tiles of 256 rows: the part is all of the launch's line
+  auto start_wide = [&](int i) {
+    LineArgs w = a;
+    w.part[0] = a.part[i];
+    w.min_length = 2 * kWideUnit;
+    if (args.causal && i == 1)
+      hipLaunchKernelGGL(attention_cached_wide_kernel<true>, dim3(ch.shares[i]), dim3(64 * kWideWaves), 0, stream, w);
+    else
+      hipLaunchKernelGGL(attention_cached_wide_kernel<false>, dim3(ch.shares[i]), dim3(64 * kWideWaves), 0, stream, w);
+  };
+  if (ch.stacked && ch.tiles[0] == 0) start_wide(0);
+  const int na = ch.tiles[0], nb = ch.tiles[1], shares = ch.shares[1];
+  if (nb == 0)
+    start_wide(1);
+  else if (na == 0)
+    nb == 1 ? start<0, 1>(a, shares, stream) : nb == 2 ? start<0, 2>(a, shares, stream) : start<0, 4>(a, shares, stream);
+  else if (na == 1)
+    start<1, 1>(a, shares, stream);
+  else
+    nb == 1 ? start<4, 1>(a, shares, stream) : nb == 2 ? start<4, 2>(a, shares, stream) : start<4, 4>(a, shares, stream);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   const int64_t rows = args.n_tokens * H_q;
+  // few rows have many pieces each
   if (rows <= 2048)
     hipLaunchKernelGGL(combine_kernel<16>, dim3((unsigned)rows), dim3(256), 0, stream, cb);
+  else if (rows <= 32768)
+    hipLaunchKernelGGL(combine_kernel<4>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, cb);
   else
     hipLaunchKernelGGL(combine_kernel<1>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, cb);
   return hipGetLastError();
