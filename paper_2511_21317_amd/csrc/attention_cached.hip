@@ -621,41 +621,36 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
 
     // ---- the piece's end ---------------------------------------------------------------------------------
     const Target to = place_piece<R>(a, part, share, p, s, piece, first, line + x - p.at);
-    {
-      float f[NQ];
+    // The waves meet, 16 rows at a time: each leaves its sums and products where its V rows were (chunk c of row r at c ^ r, which
+    // spreads the rows over the banks), and 16 lanes join a row's.
+    f32x4* so = (f32x4*)s_mem;      // [KS][16][16 chunks]
 #pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        const float l = groups_sum(w.l[qt]);
-        if (grp == 0) s_ml[wave * R + 16 * qt + l16] = float2{w.m[qt], l};
-      }
+    for (int qt = 0; qt < NQ; ++qt) {
+      if (qt) __syncthreads();
+      const float l = groups_sum(w.l[qt]);
+      if (grp == 0) s_ml[wave * 16 + l16] = float2{w.m[qt], l};
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct) so[(wave * 16 + l16) * 16 + ((4 * ct + grp) ^ l16)] = w.o[ct][qt];
       __syncthreads();
-      auto joined = [&](int r) {
-        float m = s_ml[r].x, l = 0.f;
+      const int row = threadIdx.x >> 4, chunk = threadIdx.x & 15;
+      float2 ml[KS];
+      float top = kLowest, sum = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 1; i < KS; ++i) m = fmaxf(m, s_ml[i * R + r].x);
-#pragma unroll
-        for (int i = 0; i < KS; ++i) l += s_ml[i * R + r].y * __builtin_amdgcn_exp2f(s_ml[i * R + r].x - m);
-        return float2{m, l};
-      };
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) f[qt] = __builtin_amdgcn_exp2f(w.m[qt] - joined(16 * qt + l16).x);
-      f32x4* so = (f32x4*)s_mem;      // [KS][R][4] of 16 channels
-#pragma unroll
-      for (int ct = 0; ct < 4; ++ct) {
-#pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) so[(wave * R + 16 * qt + l16) * 4 + grp] = w.o[ct][qt] * f[qt];
-        __syncthreads();
-        for (int i = threadIdx.x; i < R * 4; i += 64 * KS) {
-          f32x4 o = so[i];
-#pragma unroll
-          for (int k = 1; k < KS; ++k) o += so[k * R * 4 + i];
-          const float2 ml = joined(i >> 2);
-          if (ct == 0 && (i & 3) == 0) put_sums<R>(a, part, p, s, to, i >> 2, ml.x, ml.y);
-          put<R>(a, part, p, s, to, i >> 2, 16 * ct + 4 * (i & 3), o, ml.y);
-        }
-        __syncthreads();
+      for (int k = 0; k < KS; ++k) {
+        ml[k] = s_ml[k * 16 + row];
+        top = fmaxf(top, ml[k].x);
       }
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const float f = __builtin_amdgcn_exp2f(ml[k].x - top);
+        sum += ml[k].y * f;
+        o += so[(k * 16 + row) * 16 + (chunk ^ row)] * f;
+      }
+      if (chunk == 0) put_sums<R>(a, part, p, s, to, 16 * qt + row, top, sum);
+      put<R>(a, part, p, s, to, 16 * qt + row, 4 * chunk, o, sum);
     }
+    __syncthreads();
 
     x += piece.to - p.at;
     if (x >= end || !next_tile<R, CAUSAL, false>(a, part, p, window, s, lane)) return;
@@ -669,9 +664,8 @@ constexpr int waves_per_simd(int nq) { return nq == 1 ? 3 : 2; }
 template <int NA, int NB, bool CAUSAL>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(waves_per_simd(NA > NB ? NA : NB), waves_per_simd(NA > NB ? NA : NB)))) void
 attention_cached_kernel(const LineArgs a) {
-  constexpr int kMost = NA > NB ? NA : NB;
   __shared__ __attribute__((aligned(16))) char s_mem[kWaves * kUnitBytes];
-  __shared__ float2 s_ml[kWaves * 16 * kMost];
+  __shared__ float2 s_ml[kWaves * 16];
   const int lane = threadIdx.x & 63;
   Seq window_a = {}, window_b;
   Extent ea = {0, 0};
@@ -683,7 +677,6 @@ attention_cached_kernel(const LineArgs a) {
   if constexpr (NA > 0)
     if (share.at < total_a) {
       walk<NA, false>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
-      __syncthreads();
     }
   if (share.end > total_a)
     walk<NB, CAUSAL>(a, a.part[1], share, eb, total_a, std::max(share.at, total_a) - total_a, share.end - total_a, window_b, s_mem, s_ml);
@@ -840,9 +833,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       *(u32x4*)(s_mem + to + 8 * kRowBytes) = in[1];
     };
     // 4 bits for a unit, whether its quarters have pages: looked at only where some entry of the tile's is none
-    bool hole = false;
-    for (int i = lane; i < (most + (1 << c.cache.page_shift) - 1) >> c.cache.page_shift; i += 64) hole |= !there(table[i]);
-    const bool holes = __ballot(hole) != 0;
+    bool holes = false;
     auto ok_of = [&](int unit) {
       uint32_t ok = 15;
       if (holes && unit >= prefix_units) {
@@ -982,6 +973,9 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       k_next = rows_at(u0 + 2);
       request(in_k, k_rows(k_next));
       request(in_v, v_rows(v_next));
+      bool hole = false;
+      for (int i = lane; i < (most + (1 << c.cache.page_shift) - 1) >> c.cache.page_shift; i += 64) hole |= !there(table[i]);
+      holes = __ballot(hole) != 0;
       barrier();
       if (active) {
         bf16x8 ak[4];
