@@ -607,26 +607,26 @@ def qk_norm_rope(nr: NormRope, q, k, v, pos, q_out, k_out, v_out):
     first = q if q is not None else k if k is not None else v
     if first is None or first.dim() != 3:
         raise HttmError("expected q [N, H_q, 64], k or v [N, H_kv, 64]")
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None):
+        raise HttmError("every tensor needs its output, and every output its tensor")
     code, dtype, here = _rows_type(first), first.dtype, _here(first)
-    N = first.shape[0]
+    N, bf, byref = first.shape[0], torch.bfloat16, C.byref
     kv = k if k is not None else v
     H_kv = kv.shape[1] if kv is not None else 1
     H_q = q.shape[1] if q is not None else H_kv
-    rows, outs = [], []
-    for t, out, H in ((q, q_out, H_q), (k, k_out, H_kv), (v, v_out, H_kv)):
-        if (t is None) != (out is None):
-            raise HttmError("every tensor needs its output, and every output its tensor")
-        rows.append(C.byref(_rows(t, here, H, dtype)))
-        outs.append(None if out is None else _at(out, here, torch.bfloat16, (H, N, 64)))
-        if t is not None and t.shape[0] != N:
-            raise HttmError(f"expected {N} tokens, got {t.shape[0]}")
+    rows = _rows(q, here, H_q, dtype), _rows(k, here, H_kv, dtype), _rows(v, here, H_kv, dtype)
+    if (k is not None and k.shape[0] != N) or (v is not None and v.shape[0] != N):
+        raise HttmError(f"expected {N} tokens in k and v")
     p = None
     if nr.axes > 0 and (q is not None or k is not None):
         if pos is None:
             raise HttmError("positions are needed for a rotation")
         p = _at(pos, here, torch.int32, (N, nr.axes))
     nr.check_device(here)
-    rc = lib().httm_qk_norm_rope(C.byref(nr.struct), *rows, code, p, N, H_q, H_kv, 64, *outs, _stream_of(here))
+    rc = lib().httm_qk_norm_rope(byref(nr.struct), byref(rows[0]), byref(rows[1]), byref(rows[2]), code, p, N, H_q, H_kv, 64,
+                                 None if q is None else _at(q_out, here, bf, (H_q, N, 64)),
+                                 None if k is None else _at(k_out, here, bf, (H_kv, N, 64)),
+                                 None if v is None else _at(v_out, here, bf, (H_kv, N, 64)), _stream_of(here))
     if rc:
         _check(rc, "httm_qk_norm_rope")
     return q_out, k_out, v_out
