@@ -317,13 +317,13 @@ struct Target {
   int slot;
 };
 // The piece that starts a tile says where the others are; `first`: the share's first one, `tile`: where the tile starts on the line.
-// By the first 64 threads.
+// By all threads.
 template <int R>
 __device__ __forceinline__ Target place_piece(const LineArgs& a, const Part& part, const Share& share, const Place& p, const Seq& s,
                                               const Piece& c, bool first, int64_t tile) {
   Target t = {a.finish && c.starts && c.ends, 0};
   if (!t.finish) t.slot = a.finish ? 2 * share.id + (first ? 0 : 1) : share.id + p.tile_id;
-  if (c.starts && threadIdx.x < 64) {
+  if (c.starts) {
     const int r0 = p.tile * R, n_rows = s.n * a.c.group;
     RowPieces rp = {0, 0, 0, 0};
     if (!t.finish) {
@@ -332,7 +332,7 @@ __device__ __forceinline__ Target place_piece(const LineArgs& a, const Part& par
       rp.base = (a.finish ? 2 * share.id : t.slot) * R;
       rp.stride = a.finish ? 2 * R : R;
     }
-    for (int i = threadIdx.x; i < R; i += 64)
+    for (int i = threadIdx.x; i < R; i += 256)
       if (r0 + i < n_rows) {
         const Row r = row_of(a, p, s, r0 + i);
         part.rows[(int64_t)r.token * a.H_q + r.head] = {rp.first + i, rp.base + i, rp.stride, rp.n};
@@ -340,7 +340,7 @@ __device__ __forceinline__ Target place_piece(const LineArgs& a, const Part& par
   }
   return t;
 }
-// Four channels of a row of the tile; l: the row's sum
+// Four channels of row r of the tile; l: the row's sum
 template <int R>
 __device__ __forceinline__ void put(const LineArgs& a, const Part& part, const Place& p, const Seq& s, const Target& t, int r, int channel,
                                     const f32x4& o, float l) {
@@ -1009,14 +1009,31 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
     }
 
     const Target to = place_piece<R>(a, part, share, p, s, piece, first, x - p.at);
+    // Out through the LDS, 32 rows of a wave at a time (chunk c of row r at c ^ r % 16): a loop that is 30 instructions long and writes whole
+    // rows.  Straight from the registers it is a thousand, each run once and fetched first, and took 3 us a piece.
+    barrier();      // everybody is done with the keys
+    f32x4* so = (f32x4*)(s_mem + wave * kSide);
 #pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) {
-      const float l = groups_sum(w.l[qt]);
-      const int r = wave * 16 * NQ + 16 * qt + l16;
-      if (grp == 0) put_sums<R>(a, part, p, s, to, r, -w.m[qt], l);
+    for (int pair = 0; pair < NQ / 2; ++pair) {
+      float l[2];
 #pragma unroll
-      for (int ct = 0; ct < 4; ++ct) put<R>(a, part, p, s, to, r, 16 * ct + 4 * grp, w.o[ct][qt], l);
+      for (int i = 0; i < 2; ++i) {
+        const int qt = 2 * pair + i;
+        l[i] = groups_sum(w.l[qt]);
+        if (grp == 0) put_sums<R>(a, part, p, s, to, wave * 16 * NQ + 16 * qt + l16, -w.m[qt], l[i]);
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) so[(16 * i + l16) * 16 + ((4 * ct + grp) ^ l16)] = w.o[ct][qt];
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + grp;      // (16 lanes a row; its sum is in lane r % 16 of either half)
+        const float sum = __shfl(i < 4 ? l[0] : l[1], r & 15);
+        put<R>(a, part, p, s, to, wave * 16 * NQ + 32 * pair + r, 4 * l16, so[r * 16 + (l16 ^ (r & 15))], sum);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+
     x += piece.to - p.at;
     if (x >= share.end || !next_tile<R, CAUSAL, true>(a, part, p, window, s, lane)) return;
     first = false;
