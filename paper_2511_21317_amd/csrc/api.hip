@@ -817,7 +817,7 @@ int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const ht
 
 int64_t httm_attention_cached_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   if (n_tokens < 0 || n_seqs < 1 || H_kv < 1 || H_q < 1 || H_q % H_kv || P < 0) return HTTM_E_INVALID_ARG;
-  if (n_seqs > HTTM_MAX_SEQS || H_q > HTTM_MAX_HEADS || n_tokens >= ((int64_t)1 << 21) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
+  if (n_seqs > HTTM_MAX_SEQS || H_q > HTTM_MAX_HEADS || n_tokens >= ((int64_t)1 << 20) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
   return cached_attention_workspace(n_tokens, n_seqs, H_q, H_kv, P);
 }
 
@@ -829,7 +829,7 @@ int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void
   int rc = check_cache(cache, H_q, &a.cache);
   if (rc != HTTM_OK) return rc;
   if (n_tokens < 0 || P < 0 || !std::isfinite(scale) || !std::isnormal(scale) || scale < 0.f) return HTTM_E_INVALID_ARG;
-  if (d_head != 64 || n_tokens >= ((int64_t)1 << 21) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
+  if (d_head != 64 || n_tokens >= ((int64_t)1 << 20) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
   if (P > 0 && (!k_prefix || !v_prefix || !aligned16(k_prefix) || !aligned16(v_prefix))) return HTTM_E_INVALID_ARG;
   if (!offsets || !seq_lens || ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(seq_lens)) & 3u)) return HTTM_E_INVALID_ARG;
   if (n_tokens == 0) return HTTM_OK;

@@ -56,6 +56,7 @@ struct Part {
 struct LineArgs {
   CachedAttnArgs c;
   int32_t H_q;
+  uint32_t group_magic;   // ceil(2^32 / group), for more than 1
   int32_t finish;         // (one part) whole tiles are written to o; else every piece is left in its slot
   int32_t min_length;     // positions that a share has at least
   Part part[2];
@@ -276,8 +277,13 @@ __device__ __forceinline__ bool next_tile(const LineArgs& a, const Part& part, P
 struct Row {
   int token, head;
 };
+// r / group by a product with 2^32 / group: exact for what rows there can be, 2^20 tokens of 64 heads (the compiler's division by
+// a variable takes 25 instructions)
+__device__ __forceinline__ int token_of(const LineArgs& a, int r) {
+  return a.c.group == 1 ? r : (int)__umulhi((uint32_t)r, a.group_magic);
+}
 __device__ __forceinline__ Row row_of(const LineArgs& a, const Place& p, const Seq& s, int r) {
-  const int i = r / a.c.group;
+  const int i = token_of(a, r);
   return {s.first + i, p.h * a.c.group + (r - i * a.c.group)};
 }
 __device__ __forceinline__ const char* q_row(const LineArgs& a, const Row& r) {
@@ -286,7 +292,7 @@ __device__ __forceinline__ const char* q_row(const LineArgs& a, const Row& r) {
 // Own keys that row r sees
 template <bool CAUSAL>
 __device__ __forceinline__ int seen_by(const LineArgs& a, const Seq& s, int r) {
-  return CAUSAL ? std::clamp(s.len - s.n + r / a.c.group + 1, 0, s.len) : s.len;
+  return CAUSAL ? std::clamp(s.len - s.n + token_of(a, r) + 1, 0, s.len) : s.len;
 }
 
 // What a share has of a tile: positions [at, to) of it, units [u0, u1) of keys; nothing if it ends in the tile's front
@@ -1025,7 +1031,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
         for (int ct = 0; ct < 4; ++ct) so[(16 * i + l16) * 16 + ((4 * ct + grp) ^ l16)] = w.o[ct][qt];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 1
+#pragma unroll 2
       for (int i = 0; i < 8; ++i) {
         const int r = 4 * i + grp;      // (16 lanes a row; its sum is in lane r % 16 of either half)
         const float sum = __shfl(i < 4 ? l[0] : l[1], r & 15);
@@ -1176,6 +1182,7 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
   LineArgs a = {};
   a.c = args;
   a.H_q = H_q;
+  a.group_magic = (uint32_t)((((uint64_t)1 << 32) + args.group - 1) / args.group);
   a.finish = !ch.stacked;
   a.min_length = kWaves;
   CombineArgs cb = {};

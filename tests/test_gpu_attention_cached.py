@@ -114,6 +114,13 @@ SHAPES = {   # new tokens, rows, prefix, heads, key heads, page
     "frames": ([261, 261, 200], [261, 522, 999], 2001, 2, 2, 256),
     "a prompt": ([700], [700], 0, 3, 1, 128),
     "more tokens than rows": ([40, 5], [13, 2], 0, 2, 1, 16),
+    "pieces for many streams": ([20] * 60, spread(20, 90, 60), 301, 2, 2, 16),
+    "more streams than lanes": (spread(0, 3, 150), spread(0, 70, 150, 0.7), 45, 2, 1, 16),
+    "one long among short": ([1] * 20, [3] * 11 + [40000] + [5] * 8, 33, 2, 2, 64),
+    "rows of 64 heads": ([1, 1, 2], [100, 1, 333], 65, 64, 1, 16),
+    "a prompt of grouped heads": ([1500], [1500], 0, 5, 1, 16),
+    "a prompt behind another": ([300, 700], [2300, 701], 129, 64, 1, 32),
+    "prompts of odd groups": ([257, 511, 1], [300, 511, 70], 31, 12, 4, 16),
     "a whole scene": ([1374, 1374], [1374, 2748], 5516, 2, 2, 64),
 }
 
@@ -241,6 +248,13 @@ def test_cache_beyond_32_bit_offsets():
     q_out = torch.empty(41, H, D, dtype=torch.bfloat16, device="cuda")
     httm.cache_append(httm.NormRope(norm="none", axes=0), x[:, :H], x[:, H:2 * H], x[:, 2 * H:], None, b.cache, b.offsets, b.seq_lens, q_out)
     assert torch.equal(v[int(table[0, 1]), :, 499 - 256], x[0, 2 * H:]) and torch.equal(k[int(table[1, 1]), :, 299 - 256], x[40, H:2 * H])
+
+
+def test_as_many_sequences_as_there_may_be():
+    n = 4096
+    Batch([1] * n, [(7 * i) % 19 for i in range(n)], 21, 1, 1, 16).check()
+    with pytest.raises(httm.HttmError):
+        httm.attention_cached_workspace(n, n + 1, 1, 1, 0)
 
 
 def test_two_streams_at_once():
