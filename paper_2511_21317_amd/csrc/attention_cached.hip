@@ -92,7 +92,6 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
   return uniform64(q);
 }
 
-
 // A sequence as the line sees it.  Positions on the line are units of kUnit keys, or single keys where tiles are large (FINE).  A
 // tile is as long as the keys that its last row sees, behind its front; with `causal` and FINE those grow by `grow` from tile to
 // tile (rounded down, the last tile apart: lengths on the line only share out the work).
@@ -356,14 +355,14 @@ __device__ __forceinline__ void put(const LineArgs& a, const Part& part, const P
     const Row row = row_of(a, p, s, p.tile * R + r);
     *(u32x2*)((char*)a.c.o + (((int64_t)row.token * a.H_q + row.head) * kDHead + channel) * 2) =
         u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
-  } else if (t.slot < part.max_slots) {
+  } else if ((uint32_t)t.slot < (uint32_t)part.max_slots) {
     *(f32x4*)(part.slot_o + ((int64_t)t.slot * R + r) * kDHead + channel) = o;
   }
 }
 template <int R>
 __device__ __forceinline__ void put_sums(const LineArgs& a, const Part& part, const Place& p, const Seq& s, const Target& t, int r, float m,
                                          float l) {
-  if (!t.finish && t.slot < part.max_slots && p.tile * R + r < s.n * a.c.group) part.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
+  if (!t.finish && (uint32_t)t.slot < (uint32_t)part.max_slots && p.tile * R + r < s.n * a.c.group) part.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
 }
 
 // V^T operands: 16 channels x 32 keys in the order of the weights (see the top)
@@ -572,7 +571,8 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
         } else {
           const int row = (unit - prefix_units) * kUnit + 16 * i;
           const bool there = g.page[i] >= 0 && g.page[i] < c.cache.n_pages;
-          const int64_t at = ((((int64_t)g.page[i] * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
+          const int64_t page = there ? g.page[i] : 0;
+          const int64_t at = (((page * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
           k = c.cache.k_pages + at;
           v = c.cache.v_pages + at;
           n = there ? s.len - row : 0;
@@ -818,8 +818,8 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
         r.n = std::clamp((int)c.P - row, 0, 16);
       } else {
         const int page = page_of(unit, wave);
-        r.offset = ((((int64_t)page * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
         r.n = there(page) ? std::clamp(s.len - row, 0, 16) : 0;
+        r.offset = ((((int64_t)(r.n ? page : 0) * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
       }
       return r;
     };

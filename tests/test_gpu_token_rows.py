@@ -74,7 +74,8 @@ def positions(N, axes, far, seed):
 
 @pytest.mark.parametrize("norm,axes,rot_dim,pairing,base", [
     ("layer", 2, 64, "halves", 100.0), ("rms", 1, 64, "halves", 10000.0), ("rms", 1, 48, "neighbours", 500000.0),
-    ("none", 3, 48, "halves", 10000.0), ("layer", 3, 48, "neighbours", 100.0), ("rms", 1, 16, "halves", 10000.0), ("none", 2, 32, "neighbours", 100.0),
+    ("none", 3, 48, "halves", 10000.0), ("layer", 3, 48, "neighbours", 100.0), ("rms", 1, 16, "halves", 10000.0), ("rms", 1, 48, "halves", 10000.0), ("rms", 1, 32, "halves", 500000.0),
+    ("none", 2, 32, "neighbours", 100.0),
     ("layer", 0, 64, "halves", 100.0), ("none", 0, 0, "halves", 1.0)])
 @pytest.mark.parametrize("N,H_q,H_kv,dtype,far", [(1, 1, 1, "bf16", 40), (13, 6, 2, "fp32", 2**31 - 1), (261, 16, 16, "bf16", 5000),
                                                   (1003, 5, 3, "fp16", 2**31 - 1)])
