@@ -383,7 +383,6 @@ struct WaveState {
   bf16x8 qf[NQ][2];     // Q^T, 32 channels each
   f32x4 o[4][NQ];       // O^T, 16 channels each
   float m[NQ], l[NQ];   // shift in log2 units, sum over the lane's keys
-  int limit[NQ];        // causal: own keys that the lane's row sees
 };
 
 // One unit of keys on its way to a wave
@@ -428,19 +427,17 @@ __device__ __forceinline__ void add_seen(f32x4 (&o)[4][NQ], const bf16x8 (&av)[4
 #pragma unroll
       for (int qt = 0; qt < NQ; ++qt) {
         const f32x4 d = mfma16(one, p[qt], f32x4{0.f, 0.f, 0.f, 0.f});
-        const bool seen = row0 + j < limit[qt];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) o[ct][qt][r] += seen ? d[r] : 0.f;
+        o[ct][qt] += row0 + j < limit[qt] ? d : f32x4{0.f, 0.f, 0.f, 0.f};
       }
     }
   }
 }
 
 // Scores, statistics and product of a unit.  row0: its first key; end: keys from there on are masked in all rows (causal
-// own keys: in some); ok: bit per half of 16 keys, whether it has a page.
-template <int NQ, bool CAUSAL>
+// own keys: in some); ok: bit per half of 16 keys, whether it has a page; limit_of(qt): own keys that the lane's row sees.
+template <int NQ, bool CAUSAL, typename Limit>
 __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, bf16_t* sv, float c, int row0, int end, int ok, bool own,
-                                          int lane) {
+                                          int lane, Limit limit_of) {
   const int l16 = lane & 15, grp = lane >> 4;
   const bool masked = ok != 3 || row0 + kUnit > end;
   const bool wild = CAUSAL && masked && own && __ballot(not_finite(d.v)) != 0;
@@ -460,7 +457,7 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, b
   if (masked) {
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
-      const int limit = (CAUSAL && own ? w.limit[qt] : end) - row0 - 4 * grp;
+      const int limit = (CAUSAL && own ? limit_of(qt) : end) - row0 - 4 * grp;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -503,13 +500,17 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, b
   load_v_operands(av, sv, l16, grp);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   if (CAUSAL && __builtin_expect(wild, 0)) {
-    add_seen<NQ>(w.o, av, p, w.limit, row0, lane);
-  } else {
+    int limit[NQ];
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
+    for (int qt = 0; qt < NQ; ++qt) limit[qt] = limit_of(qt);
+    add_seen<NQ>(w.o, av, p, limit, row0, lane);
 #pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) w.o[ct][qt] = mfma16(av[ct], p[qt], w.o[ct][qt]);
+    for (int ct = 0; ct < 4; ++ct) av[ct] = bf16x8{};
   }
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) w.o[ct][qt] = mfma16(av[ct], p[qt], w.o[ct][qt]);
 }
 
 // A share's way along a part of the line: four waves take the units of a piece in turn.  [x, end): positions in the part, `line`:
@@ -595,12 +596,12 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
       const char* q = q_row(a, row_of(a, p, s, r));
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) w.qf[qt][ks] = *(const bf16x8*)(q + (ks * 4 + grp) * 16);
-      if (CAUSAL) w.limit[qt] = seen_by<CAUSAL>(a, s, r);
       w.m[qt] = kLowest;
       w.l[qt] = 0.f;
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    auto limit_of = [&](int qt) { return seen_by<CAUSAL>(a, s, std::min(r0 + 16 * qt + l16, n_rows - 1)); };
     // DEPTH units are on their way, the pages of the next one are asked for.  (The data moves through registers: two copies
     // of the step in the loop need more scalar registers than there are.)
     int unit = piece.u0 + wave;
@@ -617,7 +618,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
       if (unit + DEPTH * KS < stop) ok[DEPTH] = fetch(unit + DEPTH * KS, g, d[DEPTH]);
       g = look_up(unit + (DEPTH + 1) * KS);
       const bool own = unit >= prefix_units;
-      unit_step<NQ, CAUSAL>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane);
+      unit_step<NQ, CAUSAL>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane, limit_of);
 #pragma unroll
       for (int i = 0; i < DEPTH; ++i) {
         d[i] = d[i + 1];
