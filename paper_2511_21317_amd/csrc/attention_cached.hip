@@ -14,7 +14,7 @@
 // Prefix, computed once.  Where sequences have few rows each, the line has two parts: the prefix against tiles that are cut
 // from the rows of all sequences together, so that its keys are read once per tile of the whole batch and not per
 // sequence, and behind it every sequence's own keys; combine_kernel joins the two.  Where a sequence fills tiles by
-// itself, that would save nothing: there its tiles run over prefix and own keys in one go.
+// itself, or prefix and batch are small, that would save nothing: there its tiles run over prefix and own keys in one go (choose()).
 //
 // A wave.  S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (A = 16 keys x 32 channels, B = 32 channels x 16 rows): a lane has
 // one row's scores of 4 of 16 keys, so that statistics are sums in a lane and two exchanges.  The weights go from the
@@ -24,6 +24,11 @@
 //
 // Softmax.  m is a running shift, not the maximum: it follows when a score is more than 2^kSlack above it, which
 // after the first unit is rare, and a comparison per score pays for it.
+//
+// Measured, and what bounds it.  Tiles of few rows: memory, 64 streams of 100 to 5496 rows behind 28 700 shared keys, 16 heads, 160 us, 5.3 TB/s of
+// what has to be read (a sum over 2 GiB reaches 6.16); one token to 5516 keys, 16 heads, is a chain of latencies, 10.7 us for 3.9 us of reading.
+// Tiles of 256 rows: vector issue and power, 4 frames of 1374 tokens behind 28 650 shared keys, 16 heads, 0.90 to 0.95 PFLOP/s in the loop (a bf16
+// product of 8192^3 reaches 1.20).
 #include <algorithm>
 
 #include "attention_common.hpp"
@@ -1144,9 +1149,20 @@ constexpr int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   Choice c = {};
   const int64_t rows = n_tokens * (H_q / H_kv), mean = rows / n_seqs;
-  c.stacked = n_seqs > 1 && P > 0 && mean <= 64;
+  // Rows of all sequences together against the prefix spare walks along it (`spared` keys of a head, 256 bytes each, in part from caches) and cost every row
+  // a second set of pieces, apart from the first.  The line between the two is a fit to 220 random batches of 2 to 120 sequences, 1 to 32 rows each, 1 to 16
+  // heads and 64 to 28 000 shared keys: the other side would be at most 13 % quicker, 0.4 % on average.  us together / each sequence by itself, with (spared keys
+  // in thousands, rows x heads): 13.0 / 10.8 (34, 96), 57.1 / 29.2 (150, 21 840), 23.6 / 20.9 (257, 720),
+  // 13.8 / 19.0 (321, 84), 20.5 / 22.5 (389, 1120), 26.9 / 28.7 (477, 3312), 35.3 / 54.7 (770, 624), 34.0 / 140.7 (6548, 936).
+  // Sequences of more rows fill tiles: 24 x 60 rows 46.7 / 32.7.
+  const int64_t spared = (n_seqs - (rows + 63) / 64) * P * H_kv;
+  c.stacked = mean <= 32 && spared > 250000 + 20 * rows * H_kv;
+  // Up to 1024 rows of all sequences go with the own keys in one launch (drafts of 48 streams 62.3, with the prefix in 256-row tiles 71.3; 256 streams
+  // 93.6, 104).
   c.tiles[0] = !c.stacked ? 0 : rows <= 16 ? 1 : rows <= 1024 ? 4 : 0;
-  c.tiles[1] = mean <= 8 ? 1 : mean <= 24 ? 2 : mean <= 64 ? 4 : 0;
+  // Tiles of 32 rows from 9 rows on, though waves of 16 need fewer registers: 4 to 20 rows 62.3 / 68.6.  256-row tiles from 129 on: 8 x 100 rows
+  // 50.2, in 64-row tiles 43.6; 8 x 160 54.6 / 60.0.
+  c.tiles[1] = mean <= 8 ? 1 : mean <= 24 ? 2 : mean <= 128 ? 4 : 0;
   c.row_pieces = align256(n_tokens * H_q * (int64_t)sizeof(RowPieces));
   const int most = std::max(c.tiles[0], c.tiles[1]);
   for (int i = c.stacked ? 0 : 1; i < 2; ++i) {

@@ -6,6 +6,8 @@
 //
 // The kernel moves 128 bytes in and 128 out per row (256 in from fp32) and does some ten operations per element: it is bound
 // by memory, or by one launch where there are few rows.
+// Measured: 137 400 tokens of 3 x 16 heads, 1.7 GB, 310 us, 5.4 TB/s (a copy of 2 GiB reaches 4.96); 10 992 tokens 26 us; 522 tokens 5.9 us, of
+// which 2.4 are a launch.
 //
 // Layout.  Eight lanes hold a row, 8 channels (16 bytes of bf16) each, so a wave has the same head of eight
 // consecutive tokens: eight 128-byte lines in, and out to [H, N, 64] 1 KB in a piece.  The sums of a norm are sums in
