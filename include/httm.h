@@ -518,7 +518,7 @@ HTTM_API int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q,
  * and infinities included.
  * q: n_tokens x H_q rows, bf16.  k_prefix, v_prefix: [H_kv, P, d_head] bf16, P < 2^24; may be NULL with P = 0.
  * cache: may have no rows in it (all lengths 0: attention to the prefix alone).
- * scale: positive, finite (1/8 = 1/sqrt(d_head); ln 2 for keys with log2(e) / 8 in them: HTTM_FLAG_LOG2_KEYS).
+ * scale: positive, finite, also times log2(e) (1/8 = 1/sqrt(d_head); ln 2 for keys with log2(e) / 8 in them: HTTM_FLAG_LOG2_KEYS).
  * o: [n_tokens, H_q * d_head] bf16.  n_tokens < 2^20; 0 tokens are no error.
  * workspace: device, 256-byte aligned, httm_attention_cached_workspace(...) bytes; its contents before and after the call are
  * meaningless.  Results do not depend on it and are run-to-run identical. */

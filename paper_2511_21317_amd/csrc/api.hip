@@ -828,7 +828,7 @@ int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void
   std::memset(&a, 0, sizeof(a));
   int rc = check_cache(cache, H_q, &a.cache);
   if (rc != HTTM_OK) return rc;
-  if (n_tokens < 0 || P < 0 || !std::isfinite(scale) || !std::isnormal(scale) || scale < 0.f) return HTTM_E_INVALID_ARG;
+  if (n_tokens < 0 || P < 0 || !std::isnormal(scale) || scale < 0.f || !std::isfinite(scale * 1.4426950408889634f)) return HTTM_E_INVALID_ARG;
   if (d_head != 64 || n_tokens >= ((int64_t)1 << 20) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
   if (P > 0 && (!k_prefix || !v_prefix || !aligned16(k_prefix) || !aligned16(v_prefix))) return HTTM_E_INVALID_ARG;
   if (!offsets || !seq_lens || ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(seq_lens)) & 3u)) return HTTM_E_INVALID_ARG;

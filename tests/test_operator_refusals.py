@@ -98,7 +98,7 @@ def test_append(kw, code):
     (dict(d_head=128), UNSUPPORTED), (dict(n=1 << 21), UNSUPPORTED), (dict(n=-1), INVALID), (dict(P=-1), INVALID), (dict(P=1 << 24), UNSUPPORTED),
     (dict(kp=None), INVALID), (dict(vp=ADDR + 8), INVALID), (dict(q=rows(data=None)), INVALID), (dict(q=rows(head_stride=12)), INVALID),
     (dict(o=None), INVALID), (dict(workspace=None), INVALID), (dict(workspace=ADDR + 16), INVALID), (dict(size=0), SMALL),
-    (dict(scale=0.0), INVALID), (dict(scale=-0.125), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID),
+    (dict(scale=0.0), INVALID), (dict(scale=-0.125), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=3e38), INVALID),
     (dict(offsets=None), INVALID), (dict(seq_lens=ADDR + 2), INVALID), (dict(n=0, workspace=None, o=None), 0)])
 def test_cached(kw, code):
     assert call_cached(**kw) == code
