@@ -1160,9 +1160,11 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   // Up to 1024 rows of all sequences go with the own keys in one launch (drafts of 48 streams 62.3, with the prefix in 256-row tiles 71.3; 256 streams
   // 93.6, 104).
   c.tiles[0] = !c.stacked ? 0 : rows <= 16 ? 1 : rows <= 1024 ? 4 : 0;
-  // Tiles of 32 rows from 9 rows on, though waves of 16 need fewer registers: 4 to 20 rows 62.3 / 68.6.  256-row tiles from 129 on: 8 x 100 rows
-  // 50.2, in 64-row tiles 43.6; 8 x 160 54.6 / 60.0.
-  c.tiles[1] = mean <= 8 ? 1 : mean <= 24 ? 2 : mean <= 128 ? 4 : 0;
+  // Tiles as small as hold a sequence's rows, on average: 100 random batches, time with the smaller tile / with the larger, geometric mean: 16 or 32 rows
+  // at 9 to 16 rows a sequence 0.95, 32 or 64 at 25 to 32 0.87, at 33 to 48 0.96, but up to 1.3 where the second tile's walk counts; the
+  // other way round 16 against 32 at 17 to 24 1.15.  Together with the prefix's 64-row tiles the registers are theirs, and 32 rows are quicker from 9 on: 62.3,
+  // with 16 68.6.  256-row tiles from 129 on: 8 x 100 rows 50.2, in 64-row tiles 43.6; 8 x 160 54.6 / 60.0.
+  c.tiles[1] = mean <= (c.tiles[0] ? 8 : 16) ? 1 : mean <= 32 ? 2 : mean <= 128 ? 4 : 0;
   c.row_pieces = align256(n_tokens * H_q * (int64_t)sizeof(RowPieces));
   const int most = std::max(c.tiles[0], c.tiles[1]);
   for (int i = c.stacked ? 0 : 1; i < 2; ++i) {
@@ -1235,14 +1237,15 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
   else if (na == 1)
     start<1, 1>(a, shares, stream);
   else
-    nb == 1 ? start<4, 1>(a, shares, stream) : nb == 2 ? start<4, 2>(a, shares, stream) : start<4, 4>(a, shares, stream);
+    nb == 1 ? start<4, 1>(a, shares, stream) : start<4, 2>(a, shares, stream);    // (at most 32 rows a sequence together with the prefix)
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = args.n_tokens * H_q;
-  // few rows have many pieces each
-  if (rows <= 2048)
+  // Few rows have many pieces each, many rows fill the chip without a group's others.  Time of both kernels on 110 random batches, geometric mean: 16 groups / 4 up to
+  // 512 rows 1.00, and above 1.03; 4 / 1 up to 2048 0.99, from there to 8192 1.03, to 32 768 1.08.  16 / 4 at 2048 to 8192: 1.10.
+  if (rows <= 512)
     hipLaunchKernelGGL(combine_kernel<16>, dim3((unsigned)rows), dim3(256), 0, stream, cb);
-  else if (rows <= 32768)
+  else if (rows <= 2048)
     hipLaunchKernelGGL(combine_kernel<4>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, cb);
   else
     hipLaunchKernelGGL(combine_kernel<1>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, cb);
