@@ -1163,8 +1163,12 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   // Tiles as small as hold a sequence's rows, on average: 100 random batches, time with the smaller tile / with the larger, geometric mean: 16 or 32 rows
   // at 9 to 16 rows a sequence 0.95, 32 or 64 at 25 to 32 0.87, at 33 to 48 0.96, but up to 1.3 where the second tile's walk counts; the
   // other way round 16 against 32 at 17 to 24 1.15.  Together with the prefix's 64-row tiles the registers are theirs, and 32 rows are quicker from 9 on: 62.3,
-  // with 16 68.6.  256-row tiles from 129 on: 8 x 100 rows 50.2, in 64-row tiles 43.6; 8 x 160 54.6 / 60.0.
-  c.tiles[1] = mean <= (c.tiles[0] ? 8 : 16) ? 1 : mean <= 32 ? 2 : mean <= 128 ? 4 : 0;
+  // with 16 68.6.
+  // 256-row tiles, in which a key is read for four times as many rows, where there is work to spread them over the chip, by the keys known here: 102 random
+  // batches of 129 to 2047 rows a sequence, 64-row tiles 0.66 to 1.18 of the time below 30 million rows x keys, from 100 million on 1.16 to 1.41; this line is
+  // 0.7 % from the better side on average.  Not up to 128 rows, which would be half a tile: 8 x 100 rows 50.2, in 64-row tiles 43.6.
+  const int64_t work = rows * H_kv * (P + n_tokens / n_seqs);
+  c.tiles[1] = mean <= (c.tiles[0] ? 8 : 16) ? 1 : mean <= 32 ? 2 : mean <= 128 || work < 30000000 ? 4 : 0;
   c.row_pieces = align256(n_tokens * H_q * (int64_t)sizeof(RowPieces));
   const int most = std::max(c.tiles[0], c.tiles[1]);
   for (int i = c.stacked ? 0 : 1; i < 2; ++i) {

@@ -128,6 +128,14 @@ SHAPES = {   # new tokens, rows, prefix, heads, key heads, page
     "together, pieces": ([28, 27, 0, 30] * 6, spread(30, 200, 24), 15013, 4, 4, 64),
     "together, many rows": ([20] * 60, spread(20, 90, 60), 2603, 4, 4, 16),
     "together, more than lanes": ([1, 0, 2] * 60, spread(0, 70, 180, 0.7), 700, 8, 4, 16),
+    # enough rows and keys for tiles of 256 rows
+    "wide, a frame": ([261], [783], 29001, 4, 4, 64),
+    "wide, frames": ([261, 261, 200], [261, 522, 999], 24001, 2, 2, 256),
+    "wide, a prompt": ([3300], [3300], 0, 3, 1, 128),
+    "wide, grouped heads": ([2500], [2500], 0, 5, 1, 16),
+    "wide, odd groups": ([257, 511, 1], [300, 511, 70], 4031, 12, 4, 16),
+    "wide, pieces of prompts": ([0, 400, 130, 64, 300] * 4, spread(0, 900, 20), 2500, 4, 4, 32),
+    "wide, more tokens than rows": ([4000, 300], [1300, 20], 2001, 4, 4, 16),
     "a whole scene": ([1374, 1374], [1374, 2748], 5516, 2, 2, 64),
 }
 
@@ -138,7 +146,7 @@ def test_shapes(shape, causal):
     Batch(*SHAPES[shape], seed=len(shape), pad_front=3, pad=4).check(causal)
 
 
-@pytest.mark.parametrize("shape", ["streams", "drafts", "frames", "together, drafts", "together, many rows"])
+@pytest.mark.parametrize("shape", ["streams", "drafts", "frames", "together, drafts", "together, many rows", "wide, frames"])
 def test_peaked_scores(shape):
     """Scores of some 100 nats between the keys: the shift has to follow, and most weights vanish."""
     Batch(*SHAPES[shape], seed=3, k_scale=30.0).check(True)
@@ -161,12 +169,13 @@ def test_rising_and_falling_scores():
 def test_scale():
     Batch(*SHAPES["drafts"], seed=4).check(True, scale=0.7)
     Batch(*SHAPES["frames"], seed=4).check(False, scale=0.01)
+    Batch(*SHAPES["wide, frames"], seed=4).check(False, scale=0.01)
 
 
 def test_values_that_are_not_finite_stay_where_they_are_seen():
     """A later token's V of inf or NaN, or its K of NaN, reaches no earlier token."""
     for new, lens, P in (([5, 3], [40, 35], 50), ([200], [200], 100), ([1, 70], [9, 333], 64), ([5, 3] * 7, [40, 35] * 7, 17000),
-                         ([1, 100], [9, 333], 64)):
+                         ([1, 100], [9, 333], 64), ([200], [200], 40000)):
         b = Batch(new, lens, P, 4, 2, 16)
         for i, L in enumerate(lens):
             if new[i] < 2:
@@ -201,6 +210,13 @@ def test_pages_that_are_none_are_left_out():
     for i, j, bad in ((0, 2, -1), (4, 0, 2**31 - 1), (17, 12, -1)):
         b.cache.page_table[i, j] = bad
         drop[i][16 * j:16 * j + 16] = True
+    b.check(True, drop=drop)
+    b = Batch([2, 1, 690], [100, 50, 800], 24033, 2, 2, 16)            # tiles of 256 rows
+    drop = [torch.zeros(n, dtype=torch.bool, device="cuda") for n in b.lens]
+    for i, j, bad in ((0, 2, -1), (2, 0, 2**31 - 1), (2, 12, -1), (2, 49, 1 << 20)):
+        b.cache.page_table[i, j] = bad
+        drop[i][16 * j:16 * j + 16] = True
+    b.check(False, drop=drop)
     b.check(True, drop=drop)
 
 
@@ -240,7 +256,7 @@ def test_queries_of_any_strides():
 
 
 def test_runs_are_identical_and_workspaces_do_not_matter():
-    for name in ("streams", "frames", "many streams", "together, drafts", "together, many rows"):
+    for name in ("streams", "frames", "many streams", "together, drafts", "together, many rows", "wide, frames"):
         b = Batch(*SHAPES[name])
         want = b.run(True)
         for fill in (0, 0xFF, 0x7F):
@@ -286,7 +302,7 @@ def test_two_streams_at_once():
     assert all(torch.equal(x, y) for x, y in got)
 
 
-@pytest.mark.parametrize("B,n,P", [(4, 1, 700), (1, 1, 3000), (2, 100, 300), (2, 200, 300), (14, 1, 16000), (20, 8, 15000)])
+@pytest.mark.parametrize("B,n,P", [(4, 1, 700), (1, 1, 3000), (2, 100, 300), (2, 200, 300), (2, 200, 19000), (14, 1, 16000), (20, 8, 15000)])
 def test_graph_follows_the_lengths(B, n, P):
     """A captured call reads the lengths on the device: replays serve the sequences as they grow."""
     b = Batch([n] * B, [n + 200] * B, P, 4, 2, 16)
