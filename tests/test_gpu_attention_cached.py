@@ -128,6 +128,8 @@ SHAPES = {   # new tokens, rows, prefix, heads, key heads, page
     "together, pieces": ([28, 27, 0, 30] * 6, spread(30, 200, 24), 15013, 4, 4, 64),
     "together, many rows": ([20] * 60, spread(20, 90, 60), 2603, 4, 4, 16),
     "together, more than lanes": ([1, 0, 2] * 60, spread(0, 70, 180, 0.7), 700, 8, 4, 16),
+    "together, more rows": ([12] * 90, spread(0, 60, 90), 3501, 4, 4, 16),
+    "together, a row each": ([1] * 1100, spread(0, 40, 1100), 1003, 1, 1, 16),
     # enough rows and keys for tiles of 256 rows
     "wide, a frame": ([261], [783], 29001, 4, 4, 64),
     "wide, frames": ([261, 261, 200], [261, 522, 999], 24001, 2, 2, 256),
