@@ -923,7 +923,8 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
         top[qt] = max8(w.cur[0][qt], w.cur[1][qt]);
         over[qt] = fmaf(top[qt], c.scale_log2, w.m[qt]);
       }
-      if (__ballot(max8(f32x4{over[0], over[1], over[2], over[3]}, f32x4{over[0], over[0], over[0], over[0]}) > kSlack)) raise_shift(w, top, c.scale_log2);
+      // (not "above": a row whose scores are no numbers makes the maximum none, and must not hide the lane's three others)
+      if (__ballot(!(max8(f32x4{over[0], over[1], over[2], over[3]}, f32x4{over[0], over[0], over[0], over[0]}) <= kSlack))) raise_shift(w, top, c.scale_log2);
       load_k(ak, half);
       __builtin_amdgcn_sched_barrier(0);
       // (a wave inside this block goes first: the other one of its SIMD fills what it leaves.  16 heads x 8192 tokens x 16384 keys 620 -> 578 us)
