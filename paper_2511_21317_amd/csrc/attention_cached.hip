@@ -716,17 +716,18 @@ struct WideState {
   float l[kWideQ];          // sums over the lane's keys
   float m[kWideQ];          // minus the shift, in log2 units
 };
-// The shift follows the scores of the step in work, and all that is relative to it
+// The shift follows the scores of the step in work, and all that is relative to it.  It is a whole number (of log2 units), so that the factor is a
+// power of two and the weights that wait for their product, up to 2^kSlack, keep the rounding they have.
 __device__ __forceinline__ void raise_shift(WideState& w, const float (&top)[kWideQ], float c) {
 #pragma unroll
   for (int qt = 0; qt < kWideQ; ++qt) {
-    const float m = fminf(w.m[qt], -(groups_max(top[qt]) * c));
-    const float f = __builtin_amdgcn_exp2f(m - w.m[qt]);
+    const float m = fminf(w.m[qt], floorf(-(groups_max(top[qt]) * c)));
+    // (2^-1024 is 0: the first shift comes from kLowest)
+    const float f = ldexpf(1.f, (int)fmaxf(m - w.m[qt], -1024.f));
     w.m[qt] = m;
     w.l[qt] *= f;
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] *= f;
-    // the weights that wait for their product follow too; f is 1 or below 2^-kSlack, where a second rounding is nothing
     u32x4 x = __builtin_bit_cast(u32x4, w.p[qt]);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = pack_bf16x2(bf16_lo(x[e]) * f, bf16_hi(x[e]) * f);
