@@ -513,6 +513,8 @@ _device = getattr(torch._C, "_cuda_getDevice", None)      # (torch.cuda.current_
 
 def _here(t: torch.Tensor) -> int:
     """The current device, which a launch goes to; `t` must be there."""
+    if t is None:
+        raise HttmError("a tensor is missing")
     if not t.is_cuda:
         raise HttmError("tensor must live on the GPU")
     here = _device()
@@ -529,6 +531,8 @@ def _refuse(t, here, dtype=None, shape=None):
 
 def _at(t: torch.Tensor, here: int, dtype, shape=None) -> int:
     """As _dev(), for a tensor on the current device."""
+    if t is None:
+        raise HttmError("a tensor is missing")
     if t.get_device() == here and t.dtype is dtype and t.is_contiguous() and (shape is None or t.shape == shape):
         return t.data_ptr()
     _refuse(t, here, dtype, shape)
@@ -587,6 +591,8 @@ class PagedCache:
     [n_seqs, pages of a sequence] int32."""
 
     def __init__(self, k_pages, v_pages, page_table):
+        if k_pages is None or page_table is None:
+            raise HttmError("a tensor is missing")
         shape, table_shape = k_pages.shape, page_table.shape
         if len(shape) != 4 or shape[3] != 64 or len(table_shape) != 2:
             raise HttmError("expected k_pages [n_pages, H_kv, page_size, 64] and page_table [n_seqs, pages]")
@@ -603,6 +609,8 @@ class PagedCache:
 
 
 def _rows_type(t) -> int:
+    if t is None:
+        raise HttmError("a tensor is missing")
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise HttmError(f"rows must be bf16, fp16 or fp32, got {t.dtype}")
@@ -678,8 +686,8 @@ def attention_cached(q, k_prefix, v_prefix, cache: PagedCache, offsets, seq_lens
     share and to their own rows in the cache.  offsets, seq_lens as for cache_append; out [n, H_q * 64] bf16.
     workspace: a uint8 tensor of at least attention_cached_workspace(...) bytes."""
     bf = torch.bfloat16
-    if q.dim() != 3:
-        raise HttmError(f"expected q [n, H_q, 64], got {tuple(q.shape)}")
+    if q is None or q.dim() != 3:
+        raise HttmError(f"expected q [n, H_q, 64], got {None if q is None else tuple(q.shape)}")
     here = _here(q)
     n, H_q, _ = q.shape
     P, kp, vp = 0, None, None
