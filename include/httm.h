@@ -428,7 +428,10 @@ HTTM_API int httm_outlier_stats(const httm_plan_t* plan, float* tau, int32_t* co
  *     query head h reads key head h / (H_q / H_kv).
  *   - Data in device memory (offsets, lengths, tables, positions) is not seen by the argument checks.  The kernels bound
  *     every address they make from it: see the calls for what becomes of values out of range.
- *   - No call keeps anything between calls; with a workspace of its own each, calls may overlap freely. */
+ *   - No call keeps anything between calls; with a workspace of its own each, calls may overlap freely.
+ *   - What a call writes (outputs, workspace, rows of the cache that it appends) may not lie over what it reads, nor over another output;
+ *     q_out, k_out and v_out may be their own sources where these are bf16 and lie as the output does.  An output of rows over rows of q, k or v,
+ *     or over another one, is refused; the rest is the caller's to see to. */
 
 /* Element type of a tensor whose type the caller chooses */
 enum { HTTM_BF16 = 0, HTTM_FP16 = 1, HTTM_FP32 = 2 };

@@ -709,6 +709,42 @@ int check_rows(const httm_rows_t* r, TokenRows* out) {
   return HTTM_OK;
 }
 
+constexpr int64_t kOutRow = 64 * 2;      // bytes of a bf16 row
+
+// Whether two ranges of bytes have one in common
+bool meet(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+// Whether some row of n tokens and H heads lies in a range; rows around the range, on both sides of it, do not count
+bool rows_meet(const TokenRows& r, int64_t n, int H, int element_bytes, const void* range, int64_t bytes) {
+  const int64_t row = 64 * element_bytes, token = r.token_stride * element_bytes, head = r.head_stride * element_bytes;
+  if (!r.data || !meet(r.data, (n - 1) * token + (H - 1) * head + row, range, bytes)) return false;
+  const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(range) - reinterpret_cast<uintptr_t>(r.data)), to = from + bytes;
+  for (int h = 0; h < H; ++h) {
+    const int64_t behind = from - row - h * head;     // the first token whose row ends behind `from`, and whether it starts before `to`
+    const int64_t t = behind < 0 || token == 0 ? 0 : behind / token + 1;
+    if (t < n && t * token + h * head + row > from && t * token + h * head < to) return true;
+  }
+  return false;
+}
+// Whether a launch of rows would write one that another wave still reads: outputs of `bytes` over a source, but for the very rows
+// that they are made from (dense bf16 sources with the given strides), or over each other
+bool outputs_meet(const NormRopeArgs& a, int dtype, const int64_t (&bytes)[3], const int64_t (&token)[3], const int64_t (&head)[3]) {
+  const int size = dtype == HTTM_FP32 ? 4 : 2;
+  for (int i = 0; i < 3; ++i) {
+    if (!a.out[i]) continue;
+    for (int j = 0; j < 3; ++j) {
+      const TokenRows& r = a.src[j];
+      const bool same = i == j && dtype == HTTM_BF16 && r.data == a.out[i] && (a.N == 1 || r.token_stride == token[i]) &&
+                        (a.H[i] == 1 || r.head_stride == head[i]);
+      if (!same && rows_meet(r, a.N, a.H[j], size, a.out[i], bytes[i])) return true;
+      if (j < i && a.out[j] && meet(a.out[i], bytes[i], a.out[j], bytes[j])) return true;
+    }
+  }
+  return false;
+}
+
 int check_cache(const httm_paged_t* c, int H_q, PagedArgs* out) {
   if (!c || !c->k_pages || !c->v_pages || !c->page_table || c->n_pages < 1 || c->n_seqs < 1 || c->table_stride < 1 ||
       c->page_size < 1 || c->H_kv < 1 || H_q < 1 || H_q % c->H_kv)
@@ -785,6 +821,9 @@ int httm_qk_norm_rope(const httm_norm_rope_t* nr, const httm_rows_t* q, const ht
   }
   if (a.H[0] + a.H[1] + a.H[2] == 0) return HTTM_E_INVALID_ARG;
   if (a.axes > 0 && a.H[0] + a.H[1] > 0 && (!pos || (reinterpret_cast<uintptr_t>(pos) & 3u))) return HTTM_E_INVALID_ARG;
+  const int64_t heads[] = {a.H[0], a.H[1], a.H[2]};
+  if (outputs_meet(a, dtype, {heads[0] * N * kOutRow, heads[1] * N * kOutRow, heads[2] * N * kOutRow}, {64, 64, 64}, {64 * N, 64 * N, 64 * N}))
+    return HTTM_E_INVALID_ARG;
   a.pos = pos;
   HTTM_HIP(launch_norm_rope(a, dtype, false, (hipStream_t)stream));
   return HTTM_OK;
@@ -811,6 +850,7 @@ int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const ht
   a.offsets = offsets;
   a.seq_lens = seq_lens;
   a.out[0] = (char*)q_out;
+  if (outputs_meet(a, dtype, {n_tokens * a.H[0] * kOutRow, 0, 0}, {64 * a.H[0], 0, 0}, {64, 0, 0})) return HTTM_E_INVALID_ARG;
   HTTM_HIP(launch_norm_rope(a, dtype, true, (hipStream_t)stream));
   return HTTM_OK;
 }
@@ -837,6 +877,7 @@ int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void
   rc = check_rows(q, &a.q);
   if (rc != HTTM_OK) return rc;
   if (workspace_bytes < cached_attention_workspace(n_tokens, cache->n_seqs, H_q, cache->H_kv, P)) return HTTM_E_WORKSPACE_TOO_SMALL;
+  if (rows_meet(a.q, n_tokens, H_q, 2, o, n_tokens * H_q * kOutRow)) return HTTM_E_INVALID_ARG;
   a.k_prefix = (const char*)k_prefix;
   a.v_prefix = (const char*)v_prefix;
   a.P = P;
