@@ -512,9 +512,7 @@ _device = getattr(torch._C, "_cuda_getDevice", None)      # (torch.cuda.current_
 
 
 def _here(t: torch.Tensor) -> int:
-    """The current device, which a launch goes to; `t` must be there."""
-    if t is None:
-        raise HttmError("a tensor is missing")
+    """The current device, which a launch goes to; `t` (not None) must be there."""
     if not t.is_cuda:
         raise HttmError("tensor must live on the GPU")
     here = _device()
@@ -662,6 +660,8 @@ def cache_append(nr: NormRope, q, k, v, pos, cache: PagedCache, offsets, seq_len
     rows = _rows(q, here, (n, H_q, 64), dtype), _rows(k, here, shape, dtype), _rows(v, here, shape, dtype)
     out = None if q_out is None else _at(q_out, here, torch.bfloat16, (n, H_q, 64))
     p = _at(pos, here, torch.int32, (n, nr.axes)) if pos is not None and nr.axes > 0 else None
+    if not 0 <= first_pos < 1 << 31:      # (ctypes would take it modulo 2^64)
+        raise HttmError(f"first_pos must be from 0 to 2^31 - 1, got {first_pos}")
     nr.check_device(here)
     cache.check_device(here)
     rc = lib().httm_cache_append(nr.struct, *rows, code, p, first_pos, n, H_q, 64, cache.struct,
@@ -674,6 +674,9 @@ def cache_append(nr: NormRope, q, k, v, pos, cache: PagedCache, offsets, seq_len
 
 def attention_cached_workspace(n_tokens: int, n_seqs: int, H_q: int, H_kv: int, P: int) -> int:
     """Bytes of workspace of attention_cached()."""
+    sizes = n_tokens, n_seqs, H_q, H_kv, P
+    if min(sizes) < 0 or max(sizes) >= 1 << 31:      # (ctypes would take them modulo 2^32 or 2^64)
+        raise HttmError(f"sizes must be from 0 to 2^31 - 1, got {sizes}")
     n = int(lib().httm_attention_cached_workspace(int(n_tokens), int(n_seqs), int(H_q), int(H_kv), int(P)))
     if n < 0:
         _check(n, "httm_attention_cached_workspace")
