@@ -450,7 +450,7 @@ enum {
  * token's position.  These are split evenly among the `axes` coordinates of a position (row and column of the patch
  * grid: 2; place in a text: 1): axis a has the w = rot_dim / axes channels from a * w on, in w / 2 pairs, and pair i turns by
  * t = position[a] * base^(-2 i / w): (x, y) -> (x cos t - y sin t, y cos t + x sin t).  Computed in fp32, the angle
- * modulo a turn in 64-bit fixed point, so that it is exact at any position. */
+ * modulo a turn in 64-bit fixed point: good to 2^-25 of a turn at any position. */
 typedef struct httm_norm_rope {
   int32_t norm;         /* HTTM_NORM_* */
   int32_t axes;         /* position coordinates, 0 (no rotation) to 3 */
@@ -516,7 +516,8 @@ HTTM_API int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q,
  * and to their own cache:
  *   o[t][h] = sum_j e^(scale * q.k_j) v_j / sum_j e^(scale * q.k_j)
  * over the P rows of the prefix and the rows of the token's sequence: all of them, or with `causal` the rows up to the token's
- * own.  Weights and sums in fp32, weights rounded to bf16 for the product with v.  A token that sees no key gets
+ * own.  Scores, sums and products are held in fp32, weights rounded to bf16 for the product with v (and, in tiles of 256 rows,
+ * for their sum).  A token that sees no key gets
  * zeros; padding is left as it was.  What stands in rows and pages that a token does not see has no effect on it, NaN
  * and infinities included.
  * q: n_tokens x H_q rows, bf16.  k_prefix, v_prefix: [H_kv, P, d_head] bf16, P < 2^24; may be NULL with P = 0.

@@ -25,6 +25,12 @@
 // Softmax.  m is a running shift, not the maximum: it follows when a score is more than 2^kSlack above it, which
 // after the first unit is rare, and a comparison per score pays for it.
 //
+// Rounding.  Scores, shifts, sums and products are held in fp32.  Weights are rounded to bf16 once, as the matrix instruction takes them: half a step of
+// each, 2^-8 at most, which random errors leave at 0.0023 of the output, root mean square, with the output's own rounding; fp32
+// weights would leave 0.0017, for twice the products with V.  Tiles of few rows add up the weights in front of that rounding.  Tiles of 256 rows
+// add them up behind it, two in an instruction (v_dot2_f32_bf16) where unrounded ones take an addition each: what a weight is off then enters sum and
+// product alike, sum p (v - o) instead of sum p v.
+//
 // Measured, and what bounds it.  Tiles of few rows: memory, 64 streams of 100 to 5496 rows behind 28 700 shared keys, 16 heads, 160 us, 5.3 TB/s of
 // what has to be read (a sum over 2 GiB reaches 6.16); one token to 5516 keys, 16 heads, is a chain of latencies, 10.7 us for 3.9 us of reading.
 // Tiles of 256 rows: vector issue and power, 4 frames of 1374 tokens behind 28 650 shared keys, 16 heads, 0.90 to 0.95 PFLOP/s in the loop (a bf16
@@ -1168,7 +1174,9 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   // with 16 68.6.
   // 256-row tiles, in which a key is read for four times as many rows, where there is work to spread them over the chip, by the keys known here: 102 random
   // batches of 129 to 2047 rows a sequence, 64-row tiles 0.66 to 1.18 of the time below 30 million rows x keys, from 100 million on 1.16 to 1.41; this line is
-  // 0.7 % from the better side on average.  Not up to 128 rows, which would be half a tile: 8 x 100 rows 50.2, in 64-row tiles 43.6.
+  // 0.7 % from the better side on average.  The sequences' own keys lie on the device: only new tokens count for them here, and rows cached earlier do not, so that
+  // pieces of prompts behind long histories of their own take 64-row tiles where 256 would do: 4 x 512 rows to 30 000 own keys, 8 heads 259 us (in 256-row
+  // tiles 193), 512 to 20 000, 16 heads 102 (85), 8 x 200 to 4000 72 (61); 2 x 1000 to 8000, 16 heads on 4, 100 (102).  Not up to 128 rows, which would be half a tile: 8 x 100 rows 50.2, in 64-row tiles 43.6.
   const int64_t work = rows * H_kv * (P + n_tokens / n_seqs);
   c.tiles[1] = mean <= (c.tiles[0] ? 8 : 16) ? 1 : mean <= 32 ? 2 : mean <= 128 || work < 30000000 ? 4 : 0;
   c.row_pieces = align256(n_tokens * H_q * (int64_t)sizeof(RowPieces));
