@@ -43,3 +43,25 @@ def test_a_query_that_is_not_finite_has_its_own_row_alone(tiles, rest, value, ri
     assert not bad.any(), f"{int(bad.any(-1).sum())} of {bad.shape[0]} other rows off, {int(torch.isnan(got[fine]).any(-1).sum())} of them NaN"
     if value == "nan":
         assert torch.isnan(got[~fine]).all()
+
+
+@pytest.mark.parametrize("new,lens,P", [([70], [170], 300), ([300, 530], [300, 700], 16001)], ids=["few_rows", "256_rows"])
+def test_a_key_that_is_not_finite_reaches_later_rows_alone(new, lens, P):
+    """Every token's own key is far above all that it has seen, and one token's is NaN: the shifts of the rows in front of it follow."""
+    H = 4
+    b = Batch(new, lens, P, H, H, 16, seed=7)
+    for i, (n, m) in enumerate(zip(new, lens)):
+        b.k[i][:, m - n:] = 30 * b.q[b.off[i]:b.off[i + 1]].transpose(0, 1)
+        j = torch.arange(m)
+        b.cache.k_pages[b.cache.page_table[i, (j // 16).cuda()].long(), :, (j % 16).cuda()] = b.k[i].transpose(0, 1)
+    ref, tol = (t.view(b.n, H, D) for t in b.reference(True))
+    hit = torch.zeros(b.n, dtype=torch.bool, device="cuda")
+    for i, (n, m) in enumerate(zip(new, lens)):
+        at = n - 19         # (the rows in front of it that share a step of 32 keys and a lane with rows behind it)
+        row = m - n + at
+        b.cache.k_pages[int(b.cache.page_table[i, row // 16]), :, row % 16, 9] = float("nan")
+        hit[b.off[i] + at:b.off[i + 1]] = True
+    got = b.run(True).view(b.n, H, D)
+    assert torch.isnan(got[hit]).all()
+    bad = ~((got.double() - ref).abs() <= tol)[~hit]
+    assert not bad.any(), f"{int(bad.any(-1).sum())} of {bad.shape[0]} rows in front off"
