@@ -281,6 +281,11 @@ def _own(st, kind):
     return st["kept"], st["new_lens"], st["weights"], *rows
 
 
+def _unit(exponent):
+    """2^(exponent - 127) in 32 bits, exactly."""
+    return (exponent.int() << 23).view(torch.float32)
+
+
 def _pack(x):
     """Rows in 4 bits: codes, two channels a byte, the even one low, and an exponent per 32 channels.
 
@@ -290,7 +295,7 @@ def _pack(x):
     blocks = x.reshape(*x.shape[:-1], D // BLOCK, BLOCK)
     top = blocks.abs().amax(dim=-1)
     exponent = torch.clamp(((top.view(torch.int32) + 0x200000) >> 23) - 2, 1, 252)
-    a = torch.ldexp(blocks.abs(), 127 - exponent[..., None])
+    a = blocks.abs() / _unit(exponent)[..., None]
     code = (a > 0.25).int() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)
     code = (code + 8 * torch.signbit(blocks)).reshape(*x.shape[:-1], D // 2, 2)
     return (code[..., 0] + 16 * code[..., 1]).to(torch.uint8), exponent.to(torch.uint8)
@@ -300,9 +305,9 @@ def _unpack(codes, exponents):
     """Codes [..., 32] and exponents [..., 2] as 32-bit values [..., 64]."""
     c = torch.stack([codes & 15, codes >> 4], dim=-1).flatten(-2).int()
     m, e = c & 1, (c >> 1) & 3
-    value = torch.where(e > 0, torch.ldexp(1.0 + 0.5 * m, e - 1), 0.5 * m)
+    value = torch.where(e > 0, (2.0 + m) * _unit(e + 125), 0.5 * m)
     value = torch.where(c > 7, -value, value).unflatten(-1, (D // BLOCK, BLOCK))
-    return torch.ldexp(value, exponents.int()[..., None] - 127).flatten(-2)
+    return (value * _unit(exponents)[..., None]).flatten(-2)
 
 
 def _tokens(st):
@@ -459,7 +464,7 @@ def _nearest(x):
     top = y.abs().amax(dim=-1, keepdim=True)
     m, e = torch.frexp(top)                      # top = m 2^e, m from 0.5 to 1: 4 or 6 times the unit, or 8 of half of it
     e = torch.where(m >= 0.875, e + 1, e) - 3
-    unit = torch.ldexp(torch.ones_like(top), torch.clamp(e, -126, 125))
+    unit = (torch.clamp(e, -126, 125).long() + 1023 << 52).view(torch.float64)      # 2^e
     level = torch.tensor(_LEVELS, dtype=torch.float64, device="cuda")
     best, value = torch.full_like(y, math.inf), torch.zeros_like(y)
     for i in (0, 2, 4, 6, 1, 3, 5, 7):           # of two that are as near, the one whose last bit is 0
@@ -490,8 +495,8 @@ def _exact_rows(st, case, b, total):
         if case["store"] == "mx4":
             y = torch.empty((*x.shape[:2], D), dtype=torch.float64, device="cuda")
             y[..., 0::2], y[..., 1::2] = level[(x % 16).long()], level[(x // 16).long()]
-            e = st["scales"][pages].transpose(0, 1).flatten(1, 2)[:, :total, which::2].double()
-            x = y * torch.exp2(e - 127).repeat_interleave(BLOCK, dim=-1)
+            e = st["scales"][pages].transpose(0, 1).flatten(1, 2)[:, :total, which::2].long()
+            x = y * (e + 896 << 52).view(torch.float64).repeat_interleave(BLOCK, dim=-1)
         out.append(x.double())
     return out
 
