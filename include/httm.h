@@ -532,6 +532,70 @@ HTTM_API int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, c
                                    int H_q, int d_head, float scale, int causal, void* o, void* workspace,
                                    int64_t workspace_bytes, void* stream);
 
+/* ---- the cache in 4 bits, and within a budget ---------------------------------------------------------------
+ *
+ * A stream that is watched for long is bound by its cache: every key and value has 256 bytes a head.  Two ways to hold more: in 4 bits a
+ * key and value have 68, and the keys that nothing looks at can leave.
+ *
+ * Rows in 4 bits (the open MX format with e2m1 elements).  The 64 channels of a row are two blocks of 32.  A block has an exponent
+ * byte e, and a channel a code of 4 bits, a sign (8) and the index of one of 0, 0.5, 1, 1.5, 2, 3, 4, 6: the value is that times 2^(e - 127); e = 255
+ * makes the block NaN.  Rows are rounded as follows: e - 127 is the exponent of the block's largest |x|, rounded to two significant bits, less 2,
+ * within -126 and 125; each channel becomes the nearest value, the even code of two that are as near.  So none is off by more than half a step (one
+ * quarter of its value above the unit 2^(e - 127), 1/7 of the largest), but for |x| above 7 * 2^125, which are held as 6 * 2^125.  A block with an infinity or NaN becomes NaN.
+ *
+ * A cache in 4 bits is an httm_paged_t whose k_pages and v_pages are [n_pages, H_kv, page_size, d_head / 2] bytes, channel 2 i in the low
+ * half of byte i, with `scales` beside it: [n_pages, H_kv, page_size, 4] bytes, the exponents of a row: key and value of channels 0 .. 31, key and
+ * value of channels 32 .. 63.  All three 16-byte aligned, none over another.
+ * The calls below take `scales` NULL for a cache of bf16 rows.  What the section above says of offsets, lengths, tables and pages holds
+ * for them as well. */
+
+/* httm_cache_append to a cache in 4 bits: keys and values are rounded once, from what norm, rotation and k_scale leave in fp32. */
+HTTM_API int httm_cache_append_mx4(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v,
+                                   int dtype, const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head,
+                                   const httm_paged_t* cache, void* scales, const int32_t* offsets, const int32_t* seq_lens, void* q_out,
+                                   void* stream);
+
+/* The reverse of the append: the last rows of every sequence, those of the batch's tokens, as the cache holds them.
+ * k_out, v_out: [n_tokens, H_kv, d_head] bf16 (exact from 4 bits).  A token's row that does not exist or has no page is
+ * read as zeros; padding is left as it was.  n_tokens < 2^25; 0 tokens are no error. */
+HTTM_API int httm_cache_read(const httm_paged_t* cache, const void* scales, const int32_t* offsets, const int32_t* seq_lens,
+                             int64_t n_tokens, int d_head, void* k_out, void* v_out, void* stream);
+
+/* httm_attention_cached, over either kind of cache, with the logarithms of the sums (or lse NULL):
+ *   lse[t][h] = ln sum_j e^(scale * q.k_j), minus infinity for a token that sees no key.  lse: [n_tokens, H_q] fp32.
+ * Keys and values in 4 bits enter as the values they stand for (exact in bf16).  In tiles of 256 rows the sum is one of weights rounded to bf16: a logarithm is
+ * off by 2^-9 at most, by random 2^-9 / sqrt(3 n) of n keys that count alike. */
+HTTM_API int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P,
+                                       const httm_paged_t* cache, const void* scales, const int32_t* offsets, const int32_t* seq_lens,
+                                       int64_t n_tokens, int H_q, int d_head, float scale, int causal, void* o, float* lse, void* workspace,
+                                       int64_t workspace_bytes, void* stream);
+
+/* What attention weight the keys of every sequence get from the batch's tokens, added to what they had:
+ *   weights[b][h][j] = decay * weights[b][h][j] + sum over rows r that see key j of e^(scale * q_r.k_j - lse_r)
+ * over the tokens of sequence b and the query heads of key head h, for the rows j of the sequence; the batch's own tokens, its last rows, have no weight
+ * yet and get the sum alone.  Called after attention with the same arguments and its lse.  With `causal` a token sees the rows up to its own.
+ * A row whose lse is minus infinity adds nothing, and a row of the cache without a page gets nothing.
+ * weights: [n_seqs, H_kv, columns] fp32, columns at least table_stride * page_size; entries from the sequence's length on are
+ * left as they were.  decay: finite, not negative.  n_tokens < 2^20.  Results are run-to-run identical. */
+HTTM_API int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm_paged_t* cache, const void* scales, const int32_t* offsets,
+                              const int32_t* seq_lens, int64_t n_tokens, int H_q, int d_head, float scale, int causal, float decay,
+                              float* weights, int64_t columns, void* stream);
+
+/* Cuts every sequence of more than `keep` rows to `keep`, for each key head by itself: its first `first` and its last `last` rows
+ * stay, and of those between them the keep - first - last of highest weight (of equal ones the earlier; NaN below everything).
+ * Rows move as little as they can: those that stay in front of row keep - last stay where they are; the rows that become free there are filled, in
+ * ascending order, by those that stay behind it, in ascending order; the last rows move to the end, in order.  Weights move with their rows.
+ * What lies behind row `keep` is left as it was.
+ * new_lens: [n_seqs] int32 out, the lengths behind it (not over seq_lens, which is not written).
+ * kept: [n_seqs, H_kv, keep] int32 out or NULL: where the row now at d was, -1 behind the sequence's end.
+ * The rows from `first` on are written: their pages may belong to no other sequence.  A sequence one of whose rows has no page is left as it is, its kept
+ * all -1.
+ * workspace: device, 256-byte aligned, httm_cache_evict_workspace(...) bytes. */
+HTTM_API int64_t httm_cache_evict_workspace(int n_seqs, int H_kv, int64_t keep);
+HTTM_API int httm_cache_evict(const httm_paged_t* cache, void* scales, const int32_t* seq_lens, float* weights, int64_t columns, int d_head,
+                              int64_t keep, int64_t first, int64_t last, int32_t* new_lens, int32_t* kept, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,4 +7,5 @@ from .binding import (  # noqa: F401
     reorder_match_merge_filtered, attention_outliers, unmerge_filtered, outlier_stats, global_match,
     attention_log2, attention_log2_static, attention_scratch_bytes, attention_split_plan, attention_route, attention_wide_plan, FLAG_LOG2_KEYS, LOG2_KEY_SCALE,
     NormRope, PagedCache, qk_norm_rope, cache_append, attention_cached, attention_cached_workspace,
+    PackedCache, cache_read, cache_weigh, cache_evict, cache_evict_workspace,
 )

@@ -113,7 +113,16 @@ def lib() -> C.CDLL:
     L.httm_attention_cached_workspace.argtypes = [i64, C.c_int, C.c_int, C.c_int, i64]
     L.httm_attention_cached_workspace.restype = i64
     L.httm_attention_cached.argtypes = [rows, vp, vp, i64, paged, vp, vp, i64, C.c_int, C.c_int, C.c_float, C.c_int, vp, vp, i64, vp]
-    for name in ("httm_qk_norm_rope", "httm_cache_append", "httm_attention_cached", "httm_geom_sizes", "httm_workspace_layout", "httm_geom_tables", "httm_geom_block_forms", "httm_plan_create", "httm_plan_clone",
+    scales, f32 = vp, C.c_float
+    L.httm_cache_append_mx4.argtypes = [norm_rope, rows, rows, rows, C.c_int, vp, i64, i64, C.c_int, C.c_int, paged, scales, vp, vp, vp, vp]
+    L.httm_cache_read.argtypes = [paged, scales, vp, vp, i64, C.c_int, vp, vp, vp]
+    L.httm_attention_cached_lse.argtypes = [rows, vp, vp, i64, paged, scales, vp, vp, i64, C.c_int, C.c_int, f32, C.c_int, vp, vp, vp, i64, vp]
+    L.httm_cache_weigh.argtypes = [rows, vp, paged, scales, vp, vp, i64, C.c_int, C.c_int, f32, C.c_int, f32, vp, i64, vp]
+    L.httm_cache_evict_workspace.argtypes = [C.c_int, C.c_int, i64]
+    L.httm_cache_evict_workspace.restype = i64
+    L.httm_cache_evict.argtypes = [paged, scales, vp, vp, i64, C.c_int, i64, i64, i64, vp, vp, vp, i64, vp]
+    for name in ("httm_cache_append_mx4", "httm_cache_read", "httm_attention_cached_lse", "httm_cache_weigh", "httm_cache_evict",
+                 "httm_qk_norm_rope", "httm_cache_append", "httm_attention_cached", "httm_geom_sizes", "httm_workspace_layout", "httm_geom_tables", "httm_geom_block_forms", "httm_plan_create", "httm_plan_clone",
                  "httm_plan_destroy", "httm_plan_query", "httm_reorder", "httm_match_merge",
                  "httm_reorder_match_merge",
                  "httm_attention", "httm_attention_scratch", "httm_attention_log2", "httm_attention_log2_scratch", "httm_attention_log2_static", "httm_attention_split_plan", "httm_attention_route", "httm_attention_wide_plan", "httm_unmerge", "httm_layer_forward",
@@ -588,6 +597,8 @@ class PagedCache:
     """Keys and values in pages (httm_paged_t): k_pages, v_pages [n_pages, H_kv, page_size, 64] bf16, page_table
     [n_seqs, pages of a sequence] int32."""
 
+    scales_at = None      # (of a PackedCache)
+
     def __init__(self, k_pages, v_pages, page_table):
         if k_pages is None or page_table is None:
             raise HttmError("a tensor is missing")
@@ -604,6 +615,26 @@ class PagedCache:
     def check_device(self, here):
         if self.device != here:
             raise HttmError(f"the cache is on cuda:{self.device}, the current device is cuda:{here}")
+
+
+class PackedCache(PagedCache):
+    """Keys and values in pages, in 4 bits (include/httm.h has the format): k_codes, v_codes [n_pages, H_kv, page_size, 32] uint8, two
+    channels a byte; scales [n_pages, H_kv, page_size, 4] uint8, exponents of key and value for channels 0..31 and for 32..63; page_table
+    [n_seqs, pages of a sequence] int32.  Taken by every call that takes a PagedCache."""
+
+    def __init__(self, k_codes, v_codes, scales, page_table):
+        if k_codes is None or page_table is None:
+            raise HttmError("a tensor is missing")
+        shape, table_shape = k_codes.shape, page_table.shape
+        if len(shape) != 4 or shape[3] != 32 or len(table_shape) != 2:
+            raise HttmError("expected k_codes [n_pages, H_kv, page_size, 32] and page_table [n_seqs, pages]")
+        here, u8 = _here(k_codes), torch.uint8
+        self.device = here
+        self.k_codes, self.v_codes, self.scales, self.page_table = k_codes, v_codes, scales, page_table
+        self.n_seqs, self.H_kv, self.page_size = table_shape[0], shape[1], shape[2]
+        self.scales_at = _at(scales, here, u8, (*shape[:3], 4))
+        self.struct = _pack_paged(_at(k_codes, here, u8), _at(v_codes, here, u8, shape), _at(page_table, here, torch.int32), shape[0],
+                                  table_shape[0], table_shape[1], shape[2], shape[1])
 
 
 def _rows_type(t) -> int:
@@ -646,7 +677,7 @@ def qk_norm_rope(nr: NormRope, q, k, v, pos, q_out, k_out, v_out):
 
 
 def cache_append(nr: NormRope, q, k, v, pos, cache: PagedCache, offsets, seq_lens, q_out, first_pos: int = 0):
-    """New tokens of the sequences of a batch into the cache: q [n, H_q, 64] (or None, with q_out), k, v [n, H_kv, 64]; offsets
+    """New tokens of the sequences of a batch into the cache (a PackedCache takes them in 4 bits): q [n, H_q, 64] (or None, with q_out), k, v [n, H_kv, 64]; offsets
     [n_seqs + 1], seq_lens [n_seqs] (with the new tokens) int32 on the GPU; q_out [n, H_q, 64] bf16.
     pos: [n, axes] int32, or None with one axis: first_pos + a token's row in its sequence."""
     code, dtype, here = _rows_type(k), k.dtype, _here(k)
@@ -664,12 +695,31 @@ def cache_append(nr: NormRope, q, k, v, pos, cache: PagedCache, offsets, seq_len
         raise HttmError(f"first_pos must be from 0 to 2^31 - 1, got {first_pos}")
     nr.check_device(here)
     cache.check_device(here)
-    rc = lib().httm_cache_append(nr.struct, *rows, code, p, first_pos, n, H_q, 64, cache.struct,
-                                 _at(offsets, here, torch.int32, (cache.n_seqs + 1,)), _at(seq_lens, here, torch.int32, (cache.n_seqs,)),
-                                 out, _stream_of(here))
+    batch = _at(offsets, here, torch.int32, (cache.n_seqs + 1,)), _at(seq_lens, here, torch.int32, (cache.n_seqs,))
+    if cache.scales_at is None:
+        rc = lib().httm_cache_append(nr.struct, *rows, code, p, first_pos, n, H_q, 64, cache.struct, *batch, out, _stream_of(here))
+    else:
+        rc = lib().httm_cache_append_mx4(nr.struct, *rows, code, p, first_pos, n, H_q, 64, cache.struct, cache.scales_at, *batch, out,
+                                         _stream_of(here))
     if rc:
         _check(rc, "httm_cache_append")
     return q_out
+
+
+def cache_read(cache: PagedCache, offsets, seq_lens, k_out, v_out):
+    """The rows of a batch's tokens, the last of every sequence, out of the cache: k_out, v_out [n, H_kv, 64] bf16; offsets, seq_lens as for
+    cache_append.  Rows without a page are read as zeros, padding is left as it was."""
+    if k_out is None or k_out.dim() != 3:
+        raise HttmError(f"expected k_out [n, {cache.H_kv}, 64], got {None if k_out is None else tuple(k_out.shape)}")
+    here, bf = _here(k_out), torch.bfloat16
+    shape = (k_out.shape[0], cache.H_kv, 64)
+    cache.check_device(here)
+    rc = lib().httm_cache_read(cache.struct, cache.scales_at, _at(offsets, here, torch.int32, (cache.n_seqs + 1,)),
+                               _at(seq_lens, here, torch.int32, (cache.n_seqs,)), shape[0], 64, _at(k_out, here, bf, shape),
+                               _at(v_out, here, bf, shape), _stream_of(here))
+    if rc:
+        _check(rc, "httm_cache_read")
+    return k_out, v_out
 
 
 def attention_cached_workspace(n_tokens: int, n_seqs: int, H_q: int, H_kv: int, P: int) -> int:
@@ -684,10 +734,11 @@ def attention_cached_workspace(n_tokens: int, n_seqs: int, H_q: int, H_kv: int, 
 
 
 def attention_cached(q, k_prefix, v_prefix, cache: PagedCache, offsets, seq_lens, out, scale: float = 0.125, causal: bool = False,
-                     workspace=None):
+                     workspace=None, lse=None):
     """Attention of a batch's tokens q [n, H_q, 64] (any strides) to the prefix [H_kv, P, 64] (or None) that all sequences
     share and to their own rows in the cache.  offsets, seq_lens as for cache_append; out [n, H_q * 64] bf16.
-    workspace: a uint8 tensor of at least attention_cached_workspace(...) bytes."""
+    workspace: a uint8 tensor of at least attention_cached_workspace(...) bytes.
+    lse: [n, H_q] fp32 for the logarithms of the sums (cache_weigh() takes them), or None.  cache: bf16 rows or a PackedCache."""
     bf = torch.bfloat16
     if q is None or q.dim() != 3:
         raise HttmError(f"expected q [n, H_q, 64], got {None if q is None else tuple(q.shape)}")
@@ -705,10 +756,70 @@ def attention_cached(q, k_prefix, v_prefix, cache: PagedCache, offsets, seq_lens
     if workspace is None:
         raise HttmError("a workspace of attention_cached_workspace() bytes is needed")
     cache.check_device(here)
-    rc = lib().httm_attention_cached(_rows(q, here, (n, H_q, 64), bf), kp, vp, P, cache.struct,
-                                     _at(offsets, here, torch.int32, (cache.n_seqs + 1,)), _at(seq_lens, here, torch.int32, (cache.n_seqs,)),
-                                     n, H_q, 64, scale, 1 if causal else 0, _at(out, here, bf, (n, H_q * 64)),
-                                     _at(workspace, here, torch.uint8), workspace.numel(), _stream_of(here))
+    rc = lib().httm_attention_cached_lse(_rows(q, here, (n, H_q, 64), bf), kp, vp, P, cache.struct, cache.scales_at,
+                                         _at(offsets, here, torch.int32, (cache.n_seqs + 1,)), _at(seq_lens, here, torch.int32, (cache.n_seqs,)),
+                                         n, H_q, 64, scale, 1 if causal else 0, _at(out, here, bf, (n, H_q * 64)),
+                                         None if lse is None else _at(lse, here, torch.float32, (n, H_q)),
+                                         _at(workspace, here, torch.uint8), workspace.numel(), _stream_of(here))
     if rc:
         _check(rc, "httm_attention_cached")
     return out
+
+
+def _weights(weights, cache, here):
+    """[n_seqs, H_kv, columns] fp32"""
+    if weights is None or weights.dim() != 3:
+        raise HttmError(f"expected weights [{cache.n_seqs}, {cache.H_kv}, columns], got {None if weights is None else tuple(weights.shape)}")
+    return _at(weights, here, torch.float32, (cache.n_seqs, cache.H_kv, weights.shape[2]))
+
+
+def cache_weigh(q, lse, cache: PagedCache, offsets, seq_lens, weights, scale: float = 0.125, causal: bool = False, decay: float = 1.0):
+    """What attention weight the batch's tokens gave to every key of their sequence, added to `decay` times what it had: weights
+    [n_seqs, H_kv, columns] fp32, columns at least the rows that a sequence can have (pages of the table * page_size).  New rows get
+    theirs alone.  q, offsets, seq_lens, scale, causal as for attention_cached(), whose lse [n, H_q] it takes."""
+    if q is None or q.dim() != 3:
+        raise HttmError(f"expected q [n, H_q, 64], got {None if q is None else tuple(q.shape)}")
+    here = _here(q)
+    n, H_q, _ = q.shape
+    cache.check_device(here)
+    rc = lib().httm_cache_weigh(_rows(q, here, (n, H_q, 64), torch.bfloat16), _at(lse, here, torch.float32, (n, H_q)), cache.struct,
+                                cache.scales_at, _at(offsets, here, torch.int32, (cache.n_seqs + 1,)),
+                                _at(seq_lens, here, torch.int32, (cache.n_seqs,)), n, H_q, 64, scale, 1 if causal else 0, decay,
+                                _weights(weights, cache, here), weights.shape[2], _stream_of(here))
+    if rc:
+        _check(rc, "httm_cache_weigh")
+    return weights
+
+
+def cache_evict_workspace(n_seqs: int, H_kv: int, keep: int) -> int:
+    """Bytes of workspace of cache_evict()."""
+    sizes = n_seqs, H_kv, keep
+    if min(sizes) < 0 or max(sizes) >= 1 << 31:      # (ctypes would take them modulo 2^32 or 2^64)
+        raise HttmError(f"sizes must be from 0 to 2^31 - 1, got {sizes}")
+    n = int(lib().httm_cache_evict_workspace(int(n_seqs), int(H_kv), int(keep)))
+    if n < 0:
+        _check(n, "httm_cache_evict_workspace")
+    return n
+
+
+def cache_evict(cache: PagedCache, seq_lens, weights, keep: int, new_lens, first: int = 0, last: int = 0, kept=None, workspace=None):
+    """Cuts every sequence of more than `keep` rows to `keep`, each key head by itself: the `first` first and the `last` last rows stay,
+    and of the others those of highest weight (weights as for cache_weigh(); they move with their rows).  Places that become free are filled from behind.
+    seq_lens [n_seqs] int32 are the lengths, new_lens [n_seqs] those behind it; kept [n_seqs, H_kv, keep] int32 or None: where every row
+    was.  workspace: a uint8 tensor of at least cache_evict_workspace(...) bytes."""
+    i32 = torch.int32
+    if seq_lens is None:
+        raise HttmError("a tensor is missing")
+    if min(keep, first, last) < 0 or max(keep, first, last) >= 1 << 31:      # (ctypes would take them modulo 2^64)
+        raise HttmError(f"keep, first and last must be from 0 to 2^31 - 1, got {keep}, {first}, {last}")
+    here = _here(seq_lens)
+    cache.check_device(here)
+    if workspace is None:
+        raise HttmError("a workspace of cache_evict_workspace() bytes is needed")
+    rc = lib().httm_cache_evict(cache.struct, cache.scales_at, _at(seq_lens, here, i32, (cache.n_seqs,)), _weights(weights, cache, here),
+                                weights.shape[2], 64, keep, first, last, _at(new_lens, here, i32, (cache.n_seqs,)),
+                                None if kept is None else _at(kept, here, i32, (cache.n_seqs, cache.H_kv, keep)),
+                                _at(workspace, here, torch.uint8), workspace.numel(), _stream_of(here))
+    if rc:
+        _check(rc, "httm_cache_evict")
+    return new_lens

@@ -2,6 +2,7 @@
 // httm_layer_forward.  See include/httm.h for the contract of every entry point.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <memory>
@@ -745,7 +746,8 @@ bool outputs_meet(const NormRopeArgs& a, int dtype, const int64_t (&bytes)[3], c
   return false;
 }
 
-int check_cache(const httm_paged_t* c, int H_q, PagedArgs* out) {
+// `scales`: of a cache in 4 bits, or nullptr
+int check_cache(const httm_paged_t* c, void* scales, int H_q, PagedArgs* out) {
   if (!c || !c->k_pages || !c->v_pages || !c->page_table || c->n_pages < 1 || c->n_seqs < 1 || c->table_stride < 1 ||
       c->page_size < 1 || c->H_kv < 1 || H_q < 1 || H_q % c->H_kv)
     return HTTM_E_INVALID_ARG;
@@ -754,9 +756,22 @@ int check_cache(const httm_paged_t* c, int H_q, PagedArgs* out) {
       (c->page_size & (c->page_size - 1)) || c->n_pages > INT32_MAX ||
       (int64_t)c->table_stride * c->page_size > ((int64_t)1 << 30))
     return HTTM_E_UNSUPPORTED;
-  *out = {(char*)c->k_pages, (char*)c->v_pages, c->page_table, c->n_pages, c->n_seqs, c->table_stride, __builtin_ctz(c->page_size), c->H_kv};
+  if (scales) {
+    const int64_t rows = c->n_pages * c->H_kv * c->page_size;
+    if (!aligned16(scales) || meet(c->k_pages, rows * 32, c->v_pages, rows * 32) || meet(scales, rows * 4, c->k_pages, rows * 32) ||
+        meet(scales, rows * 4, c->v_pages, rows * 32))
+      return HTTM_E_INVALID_ARG;
+  }
+  *out = {(char*)c->k_pages, (char*)c->v_pages, (uint8_t*)scales, c->page_table, c->n_pages, c->n_seqs, c->table_stride, __builtin_ctz(c->page_size), c->H_kv};
   return HTTM_OK;
 }
+
+// Whether a range lies over the cache's pages
+bool meets_pages(const PagedArgs& c, const void* range, int64_t bytes) {
+  const int64_t rows = (c.n_pages * c.H_kv) << c.page_shift, row = c.scales ? 32 : 128;
+  return meet(c.k_pages, rows * row, range, bytes) || meet(c.v_pages, rows * row, range, bytes) || (c.scales && meet(c.scales, rows * 4, range, bytes));
+}
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Norm, rotation and sources of a launch
 int fill_norm_rope(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype, int64_t N,
@@ -829,12 +844,12 @@ int httm_qk_norm_rope(const httm_norm_rope_t* nr, const httm_rows_t* q, const ht
   return HTTM_OK;
 }
 
-int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype,
-                      const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head, const httm_paged_t* cache,
-                      const int32_t* offsets, const int32_t* seq_lens, void* q_out, void* stream) {
+static int append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype,
+                  const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head, const httm_paged_t* cache, void* scales,
+                  const int32_t* offsets, const int32_t* seq_lens, void* q_out, void* stream) {
   NormRopeArgs a;
   PagedArgs paged;
-  int rc = check_cache(cache, H_q, &paged);
+  int rc = check_cache(cache, scales, H_q, &paged);
   if (rc != HTTM_OK) return rc;
   rc = fill_norm_rope(nr, q, k, v, dtype, n_tokens, H_q, cache->H_kv, d_head, &a);
   if (rc != HTTM_OK) return rc;
@@ -855,18 +870,53 @@ int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const ht
   return HTTM_OK;
 }
 
+int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype,
+                      const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head, const httm_paged_t* cache,
+                      const int32_t* offsets, const int32_t* seq_lens, void* q_out, void* stream) {
+  return append(nr, q, k, v, dtype, pos, first_pos, n_tokens, H_q, d_head, cache, nullptr, offsets, seq_lens, q_out, stream);
+}
+
+int httm_cache_append_mx4(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v, int dtype,
+                          const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head, const httm_paged_t* cache,
+                          void* scales, const int32_t* offsets, const int32_t* seq_lens, void* q_out, void* stream) {
+  if (!scales) return HTTM_E_INVALID_ARG;
+  return append(nr, q, k, v, dtype, pos, first_pos, n_tokens, H_q, d_head, cache, scales, offsets, seq_lens, q_out, stream);
+}
+
+int httm_cache_read(const httm_paged_t* cache, const void* scales, const int32_t* offsets, const int32_t* seq_lens, int64_t n_tokens,
+                    int d_head, void* k_out, void* v_out, void* stream) {
+  CacheReadArgs a;
+  std::memset(&a, 0, sizeof(a));
+  const int rc = check_cache(cache, const_cast<void*>(scales), cache ? cache->H_kv : 0, &a.cache);
+  if (rc != HTTM_OK) return rc;
+  if (n_tokens < 0 || !offsets || !seq_lens || !aligned4(offsets) || !aligned4(seq_lens)) return HTTM_E_INVALID_ARG;
+  if (d_head != 64 || n_tokens >= ((int64_t)1 << 25)) return HTTM_E_UNSUPPORTED;
+  if (n_tokens == 0) return HTTM_OK;
+  const int64_t bytes = n_tokens * cache->H_kv * kOutRow;
+  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || meet(k_out, bytes, v_out, bytes) || meets_pages(a.cache, k_out, bytes) ||
+      meets_pages(a.cache, v_out, bytes))
+    return HTTM_E_INVALID_ARG;
+  a.offsets = offsets;
+  a.seq_lens = seq_lens;
+  a.N = n_tokens;
+  a.out[0] = (char*)k_out;
+  a.out[1] = (char*)v_out;
+  HTTM_HIP(launch_cache_read(a, (hipStream_t)stream));
+  return HTTM_OK;
+}
+
 int64_t httm_attention_cached_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   if (n_tokens < 0 || n_seqs < 1 || H_kv < 1 || H_q < 1 || H_q % H_kv || P < 0) return HTTM_E_INVALID_ARG;
   if (n_seqs > HTTM_MAX_SEQS || H_q > HTTM_MAX_HEADS || n_tokens >= ((int64_t)1 << 20) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
   return cached_attention_workspace(n_tokens, n_seqs, H_q, H_kv, P);
 }
 
-int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P, const httm_paged_t* cache,
-                          const int32_t* offsets, const int32_t* seq_lens, int64_t n_tokens, int H_q, int d_head, float scale,
-                          int causal, void* o, void* workspace, int64_t workspace_bytes, void* stream) {
+int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P, const httm_paged_t* cache,
+                              const void* scales, const int32_t* offsets, const int32_t* seq_lens, int64_t n_tokens, int H_q, int d_head,
+                              float scale, int causal, void* o, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
   CachedAttnArgs a;
   std::memset(&a, 0, sizeof(a));
-  int rc = check_cache(cache, H_q, &a.cache);
+  int rc = check_cache(cache, const_cast<void*>(scales), H_q, &a.cache);
   if (rc != HTTM_OK) return rc;
   if (n_tokens < 0 || P < 0 || !std::isnormal(scale) || scale < 0.f || !std::isfinite(scale * 1.4426950408889634f)) return HTTM_E_INVALID_ARG;
   if (d_head != 64 || n_tokens >= ((int64_t)1 << 20) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
@@ -878,6 +928,10 @@ int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void
   if (rc != HTTM_OK) return rc;
   if (workspace_bytes < cached_attention_workspace(n_tokens, cache->n_seqs, H_q, cache->H_kv, P)) return HTTM_E_WORKSPACE_TOO_SMALL;
   if (rows_meet(a.q, n_tokens, H_q, 2, o, n_tokens * H_q * kOutRow)) return HTTM_E_INVALID_ARG;
+  const int64_t lse_bytes = n_tokens * H_q * (int64_t)sizeof(float);
+  if (lse && (!aligned4(lse) || meet(lse, lse_bytes, o, n_tokens * H_q * kOutRow) || rows_meet(a.q, n_tokens, H_q, 2, lse, lse_bytes) ||
+              meet(lse, lse_bytes, workspace, workspace_bytes) || meets_pages(a.cache, lse, lse_bytes)))
+    return HTTM_E_INVALID_ARG;
   a.k_prefix = (const char*)k_prefix;
   a.v_prefix = (const char*)v_prefix;
   a.P = P;
@@ -888,8 +942,94 @@ int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void
   a.causal = causal != 0;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.o = o;
+  a.lse = lse;
   a.workspace = (char*)workspace;
   HTTM_HIP(launch_cached_attention(a, (hipStream_t)stream));
+  return HTTM_OK;
+}
+
+int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P, const httm_paged_t* cache,
+                          const int32_t* offsets, const int32_t* seq_lens, int64_t n_tokens, int H_q, int d_head, float scale,
+                          int causal, void* o, void* workspace, int64_t workspace_bytes, void* stream) {
+  return httm_attention_cached_lse(q, k_prefix, v_prefix, P, cache, nullptr, offsets, seq_lens, n_tokens, H_q, d_head, scale, causal, o, nullptr,
+                                   workspace, workspace_bytes, stream);
+}
+
+int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm_paged_t* cache, const void* scales, const int32_t* offsets,
+                     const int32_t* seq_lens, int64_t n_tokens, int H_q, int d_head, float scale, int causal, float decay, float* weights,
+                     int64_t columns, void* stream) {
+  WeighArgs a;
+  std::memset(&a, 0, sizeof(a));
+  int rc = check_cache(cache, const_cast<void*>(scales), H_q, &a.cache);
+  if (rc != HTTM_OK) return rc;
+  if (n_tokens < 0 || !std::isnormal(scale) || scale < 0.f || !std::isfinite(scale * 1.4426950408889634f) || !std::isfinite(decay) || decay < 0.f)
+    return HTTM_E_INVALID_ARG;
+  if (d_head != 64 || n_tokens >= ((int64_t)1 << 20)) return HTTM_E_UNSUPPORTED;
+  if (!offsets || !seq_lens || !aligned4(offsets) || !aligned4(seq_lens) || !weights || !aligned4(weights)) return HTTM_E_INVALID_ARG;
+  if (columns < (int64_t)cache->table_stride * cache->page_size || columns > INT32_MAX) return HTTM_E_INVALID_ARG;
+  rc = check_rows(q, &a.q);
+  if (rc != HTTM_OK) return rc;
+  const int64_t bytes = (int64_t)cache->n_seqs * cache->H_kv * columns * (int64_t)sizeof(float);
+  if (n_tokens > 0 && (!a.q.data || !lse || !aligned4(lse) || rows_meet(a.q, n_tokens, H_q, 2, weights, bytes) ||
+                       meet(lse, n_tokens * H_q * (int64_t)sizeof(float), weights, bytes)))
+    return HTTM_E_INVALID_ARG;
+  if (meets_pages(a.cache, weights, bytes)) return HTTM_E_INVALID_ARG;
+  a.lse = lse;
+  a.offsets = offsets;
+  a.seq_lens = seq_lens;
+  a.n_tokens = n_tokens;
+  a.group = H_q / cache->H_kv;
+  a.causal = causal != 0;
+  a.scale = scale;
+  a.decay = decay;
+  a.weights = weights;
+  a.columns = columns;
+  HTTM_HIP(launch_cache_weigh(a, (hipStream_t)stream));
+  return HTTM_OK;
+}
+
+int64_t httm_cache_evict_workspace(int n_seqs, int H_kv, int64_t keep) {
+  if (n_seqs < 1 || H_kv < 1 || keep < 1) return HTTM_E_INVALID_ARG;
+  if (n_seqs > HTTM_MAX_SEQS || H_kv > HTTM_MAX_HEADS || keep > ((int64_t)1 << 30)) return HTTM_E_UNSUPPORTED;
+  return cache_evict_workspace(n_seqs, H_kv, (int)keep);
+}
+
+int httm_cache_evict(const httm_paged_t* cache, void* scales, const int32_t* seq_lens, float* weights, int64_t columns, int d_head, int64_t keep,
+                     int64_t first, int64_t last, int32_t* new_lens, int32_t* kept, void* workspace, int64_t workspace_bytes, void* stream) {
+  EvictArgs a;
+  std::memset(&a, 0, sizeof(a));
+  const int rc = check_cache(cache, scales, cache ? cache->H_kv : 0, &a.cache);
+  if (rc != HTTM_OK) return rc;
+  if (keep < 1 || first < 0 || last < 0 || first > keep || last > keep - first) return HTTM_E_INVALID_ARG;
+  if (d_head != 64 || keep > ((int64_t)1 << 30)) return HTTM_E_UNSUPPORTED;
+  if (!seq_lens || !new_lens || !weights || !workspace || !aligned4(seq_lens) || !aligned4(new_lens) || !aligned4(weights) || !aligned4(kept) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return HTTM_E_INVALID_ARG;
+  if (columns < (int64_t)cache->table_stride * cache->page_size || columns > INT32_MAX) return HTTM_E_INVALID_ARG;
+  if (workspace_bytes < cache_evict_workspace(cache->n_seqs, cache->H_kv, (int)keep)) return HTTM_E_WORKSPACE_TOO_SMALL;
+  // nothing that is written lies over anything else
+  const int64_t heads = (int64_t)cache->n_seqs * cache->H_kv, four = sizeof(int32_t);
+  struct Range {
+    const void* at;
+    int64_t bytes;
+  };
+  const Range r[] = {{new_lens, cache->n_seqs * four}, {weights, heads * columns * four}, {workspace, workspace_bytes}, {kept, kept ? heads * keep * four : 0},
+                     {seq_lens, cache->n_seqs * four}, {cache->page_table, (int64_t)cache->n_seqs * cache->table_stride * four}};
+  for (int i = 0; i < 6; ++i) {
+    if (r[i].bytes && meets_pages(a.cache, r[i].at, r[i].bytes)) return HTTM_E_INVALID_ARG;
+    for (int j = 0; j < std::min(i, 4); ++j)
+      if (r[i].bytes && r[j].bytes && meet(r[i].at, r[i].bytes, r[j].at, r[j].bytes)) return HTTM_E_INVALID_ARG;
+  }
+  a.seq_lens = seq_lens;
+  a.weights = weights;
+  a.columns = columns;
+  a.keep = (int32_t)keep;
+  a.first = (int32_t)first;
+  a.last = (int32_t)last;
+  a.new_lens = new_lens;
+  a.kept = kept;
+  a.workspace = (char*)workspace;
+  HTTM_HIP(launch_cache_evict(a, (hipStream_t)stream));
   return HTTM_OK;
 }
 

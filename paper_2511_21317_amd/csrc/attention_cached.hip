@@ -40,6 +40,7 @@
 #include "attention_common.hpp"
 #include "dev_common.hpp"
 #include "kernels.hpp"
+#include "mx4.hpp"
 
 namespace httm {
 
@@ -356,6 +357,10 @@ __device__ __forceinline__ Target place_piece(const LineArgs& a, const Part& par
   }
   return t;
 }
+// The logarithm of a row's sum of l 2^m; of none, minus infinity
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
 // Four channels of row r of the tile; l: the row's sum
 template <int R>
 __device__ __forceinline__ void put(const LineArgs& a, const Part& part, const Place& p, const Seq& s, const Target& t, int r, int channel,
@@ -373,7 +378,13 @@ __device__ __forceinline__ void put(const LineArgs& a, const Part& part, const P
 template <int R>
 __device__ __forceinline__ void put_sums(const LineArgs& a, const Part& part, const Place& p, const Seq& s, const Target& t, int r, float m,
                                          float l) {
-  if (!t.finish && (uint32_t)t.slot < (uint32_t)part.max_slots && p.tile * R + r < s.n * a.c.group) part.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
+  if (p.tile * R + r >= s.n * a.c.group) return;
+  if (!t.finish) {
+    if ((uint32_t)t.slot < (uint32_t)part.max_slots) part.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
+  } else if (a.c.lse) {
+    const Row row = row_of(a, p, s, p.tile * R + r);
+    a.c.lse[(int64_t)row.token * a.H_q + row.head] = log_sum(m, l);
+  }
 }
 
 // V^T operands: 16 channels x 32 keys in the order of the weights (see the top)
@@ -396,15 +407,29 @@ struct WaveState {
   float m[NQ], l[NQ];   // shift in log2 units, sum over the lane's keys
 };
 
-// One unit of keys on its way to a wave
+// One unit of keys on its way to a wave.  Next to a cache in 4 bits a lane has 16 channels in a piece, of K and of V, of one row of
+// either half of 16: 16 * grp + 0..7 and + 8..15.  (Which 32 channels an operand of K Q^T has does not matter, as long as Q is taken alike.)
 struct UnitData {
   u32x4 k[4];       // [key half * 2 + channel half]: the A operands
-  u32x4 v[4];       // 8 rows each
+  u32x4 v[4];       // 8 rows each; with 4 bits as k
 };
+// The codes of a row's 16 channels, as they lie: {k, k, v, v}, and the block's two exponents
+struct MxHalf {
+  u32x4 codes;
+  uint32_t exponents;
+};
+__device__ __forceinline__ void expand(UnitData& d, int half, const MxHalf& x) {
+  const float ku = mx4_key_unit(x.exponents), vu = mx4_value_unit(x.exponents);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    d.k[2 * half + e] = mx4_values(x.codes[e], ku);
+    d.v[2 * half + e] = mx4_values(x.codes[2 + e], vu);
+  }
+}
 
 // Rows of K or V: 16 from `at` on, of which the first `n` are there; the others are read as zeros, wherever they would be
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_rows(const char* at, int n) {
-  return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, n * kRowBytes, kRawBufferWord3);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_rows(const char* at, int n, int row_bytes = kRowBytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, n * row_bytes, kRawBufferWord3);
 }
 __device__ __forceinline__ u32x4 load_row(__amdgpu_buffer_rsrc_t rows, int offset) {
   return __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 0, 0);
@@ -446,7 +471,7 @@ __device__ __forceinline__ void add_seen(f32x4 (&o)[4][NQ], const bf16x8 (&av)[4
 
 // Scores, statistics and product of a unit.  row0: its first key; end: keys from there on are masked in all rows (causal
 // own keys: in some); ok: bit per half of 16 keys, whether it has a page; limit_of(qt): own keys that the lane's row sees.
-template <int NQ, bool CAUSAL, typename Limit>
+template <int NQ, bool CAUSAL, bool MX4, typename Limit>
 __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, bf16_t* sv, float c, int row0, int end, int ok, bool own,
                                           int lane, Limit limit_of) {
   const int l16 = lane & 15, grp = lane >> 4;
@@ -454,8 +479,8 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, b
   const bool wild = CAUSAL && masked && own && __ballot(not_finite(d.v)) != 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int r = 8 * i + (lane >> 3);
-    *(u32x4*)(sv + r * kDHead + ((lane & 7) ^ v_swizzle(r)) * 8) = d.v[i];
+    const int r = MX4 ? 16 * (i >> 1) + l16 : 8 * i + (lane >> 3), chunk = MX4 ? 2 * grp + (i & 1) : lane & 7;
+    *(u32x4*)(sv + r * kDHead + (chunk ^ v_swizzle(r)) * 8) = d.v[i];
   }
   f32x4 s[2][NQ];
 #pragma unroll
@@ -527,7 +552,7 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, b
 // A share's way along a part of the line: four waves take the units of a piece in turn.  [x, end): positions in the part, `line`:
 // where it starts on the line.
 constexpr int kWaves = 4;
-template <int NQ, bool CAUSAL>
+template <int NQ, bool CAUSAL, bool MX4>
 __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const Share& share, const Extent& ex, int64_t line, int64_t x,
                                      int64_t end, Seq window, char* s_mem, float2* s_ml) {
   constexpr int R = 16 * NQ, KS = kWaves;
@@ -540,7 +565,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
   if (!find_place<R, CAUSAL, false>(a, part, ex, x, lane, p, window)) return;
   Seq s = of_lane<R, CAUSAL, false>(a, part, window, p.b - p.base);
   const int P = part.with_prefix ? (int)c.P : 0, prefix_units = (P + kUnit - 1) / kUnit;
-  const int k_offset = l16 * kRowBytes + grp * 16, v_offset = lane * 16;
+  const int k_offset = l16 * kRowBytes + grp * (MX4 ? 32 : 16), v_offset = MX4 ? k_offset : lane * 16;
   bool first = true;
 
   while (true) {
@@ -567,13 +592,28 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
       }
       return g;
     };
-    // Requests a unit's rows; returns its ok bits
+    // Requests a unit's rows, of own keys in 4 bits the codes in the first half of their place; returns its ok bits
     auto fetch = [&](int unit, const Pages& g, UnitData& d) {
       int ok = 3;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const char *k, *v;
         int n;
+        if (MX4 && unit >= prefix_units) {
+          const int row = (unit - prefix_units) * kUnit + 16 * i;
+          const bool there = g.page[i] >= 0 && g.page[i] < c.cache.n_pages;
+          const int64_t page = there ? g.page[i] : 0;
+          const int64_t at = ((page * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1));
+          n = std::clamp(there ? s.len - row : 0, 0, 16);
+          ok &= there ? 3 : ~(1 << i);
+          const int in = l16 * kMxRowBytes + grp * 8;
+          const u32x2 kc = __builtin_amdgcn_raw_buffer_load_b64(half_rows(c.cache.k_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
+          const u32x2 vc = __builtin_amdgcn_raw_buffer_load_b64(half_rows(c.cache.v_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
+          d.k[2 * i] = u32x4{kc[0], kc[1], vc[0], vc[1]};
+          d.k[2 * i + 1][0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
+              half_rows((const char*)c.cache.scales + at * kMxScaleBytes, n, kMxScaleBytes), l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
+          continue;
+        }
         if (unit < prefix_units) {
           const int row = unit * kUnit + 16 * i;
           const int64_t at = (p.h * c.P + row) * kRowBytes;
@@ -593,9 +633,9 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
         n = std::clamp(n, 0, 16);
         const __amdgpu_buffer_rsrc_t kr = half_rows(k, n), vr = half_rows(v, n);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) d.k[2 * i + ks] = load_row(kr, k_offset + ks * 64);
+        for (int ks = 0; ks < 2; ++ks) d.k[2 * i + ks] = load_row(kr, k_offset + ks * (MX4 ? 16 : 64));
 #pragma unroll
-        for (int e = 0; e < 2; ++e) d.v[2 * i + e] = load_row(vr, v_offset + e * 1024);
+        for (int e = 0; e < 2; ++e) d.v[2 * i + e] = load_row(vr, v_offset + e * (MX4 ? 16 : 1024));
       }
       return ok;
     };
@@ -606,7 +646,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
       const int r = std::min(r0 + 16 * qt + l16, n_rows - 1);
       const char* q = q_row(a, row_of(a, p, s, r));
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) w.qf[qt][ks] = *(const bf16x8*)(q + (ks * 4 + grp) * 16);
+      for (int ks = 0; ks < 2; ++ks) w.qf[qt][ks] = *(const bf16x8*)(q + (MX4 ? 2 * grp + ks : ks * 4 + grp) * 16);
       w.m[qt] = kLowest;
       w.l[qt] = 0.f;
 #pragma unroll
@@ -629,7 +669,13 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
       if (unit + DEPTH * KS < stop) ok[DEPTH] = fetch(unit + DEPTH * KS, g, d[DEPTH]);
       g = look_up(unit + (DEPTH + 1) * KS);
       const bool own = unit >= prefix_units;
-      unit_step<NQ, CAUSAL>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane, limit_of);
+      if constexpr (MX4)
+        if (own) {
+          const MxHalf half[2] = {{d[0].k[0], d[0].k[1][0]}, {d[0].k[2], d[0].k[3][0]}};
+          expand(d[0], 0, half[0]);
+          expand(d[0], 1, half[1]);
+        }
+      unit_step<NQ, CAUSAL, MX4>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane, limit_of);
 #pragma unroll
       for (int i = 0; i < DEPTH; ++i) {
         d[i] = d[i + 1];
@@ -679,7 +725,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
 // NA query tiles of 16 rows for the first part of the line, the prefix against all sequences' rows, or 0: there is none;
 // NB for the second.
 constexpr int waves_per_simd(int nq) { return nq == 1 ? 3 : 2; }
-template <int NA, int NB, bool CAUSAL>
+template <int NA, int NB, bool CAUSAL, bool MX4>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(waves_per_simd(NA > NB ? NA : NB), waves_per_simd(NA > NB ? NA : NB)))) void
 attention_cached_kernel(const LineArgs a) {
   __shared__ __attribute__((aligned(16))) char s_mem[kWaves * kUnitBytes];
@@ -694,10 +740,10 @@ attention_cached_kernel(const LineArgs a) {
   if (!find_share(a, total_a + total_b, share)) return;
   if constexpr (NA > 0)
     if (share.at < total_a) {
-      walk<NA, false>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
+      walk<NA, false, MX4>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
     }
   if (share.end > total_a)
-    walk<NB, CAUSAL>(a, a.part[1], share, eb, total_a, std::max(share.at, total_a) - total_a, share.end - total_a, window_b, s_mem, s_ml);
+    walk<NB, CAUSAL, MX4>(a, a.part[1], share, eb, total_a, std::max(share.at, total_a) - total_a, share.end - total_a, window_b, s_mem, s_ml);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------
@@ -741,7 +787,7 @@ __device__ __forceinline__ void raise_shift(WideState& w, const float (&top)[kWi
   }
 }
 
-template <bool CAUSAL>
+template <bool CAUSAL, bool MX4>
 __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_cached_wide_kernel(const LineArgs a) {
   constexpr int NQ = kWideQ, R = kWideRows, UNIT = kWideUnit;
   // K of two units, V of two.  All that reads or writes them goes by offsets that change sides once a unit.
@@ -769,9 +815,10 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
     const int row = 4 * grp + (l16 >> 2);
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) v_at[ct] = 2 * kSide + row * kRowBytes + ((2 * ct + ((l16 & 3) >> 1)) ^ v_swizzle(row)) * 16 + 8 * (l16 & 1);
-    const int in = 16 * wave + (lane >> 3);      // and the row 8 further, whose place among the chunks is the same one
-    to_k = in * kRowBytes + ((lane & 7) ^ k_swizzle(in)) * 16;
-    to_v = 2 * kSide + in * kRowBytes + ((lane & 7) ^ v_swizzle(in)) * 16;
+    // and the row 8 further, whose place among the chunks is the same one; with 4 bits the chunk beside it (of 16 channels in a lane)
+    const int in = 16 * wave + (MX4 ? lane >> 2 : lane >> 3), chunk = MX4 ? 2 * (lane & 3) : lane & 7;
+    to_k = in * kRowBytes + (chunk ^ k_swizzle(in)) * 16;
+    to_v = 2 * kSide + in * kRowBytes + (chunk ^ v_swizzle(in)) * 16;
   }
   auto change_sides = [&] {
 #pragma unroll
@@ -818,7 +865,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
     auto there = [&](int page) { return page >= 0 && page < (int)c.cache.n_pages; };
     // A wave brings the unit's rows 16 * wave .. + 15, of K and, a unit later, of V
     struct RowsAt {
-      int64_t offset;     // from k_prefix or k_pages, and from v_prefix or v_pages
+      int64_t offset;     // from k_prefix or k_pages, and from v_prefix or v_pages, in bytes; of rows in 4 bits in rows
       int n;
       bool own;
     };
@@ -832,24 +879,48 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       } else {
         const int page = page_of(unit, wave);
         r.n = there(page) ? std::clamp(s.len - row, 0, 16) : 0;
-        r.offset = ((((int64_t)(r.n ? page : 0) * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) * kRowBytes;
+        r.offset = ((((int64_t)(r.n ? page : 0) * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) *
+                   (MX4 ? 1 : kRowBytes);
       }
       return r;
     };
-    auto k_rows = [&](const RowsAt& r) { return half_rows((r.own ? c.cache.k_pages : c.k_prefix) + r.offset, r.n); };
-    auto v_rows = [&](const RowsAt& r) { return half_rows((r.own ? c.cache.v_pages : c.v_prefix) + r.offset, r.n); };
     u32x4 in_k[2], in_v[2];
-    auto request = [&](u32x4 (&in)[2], const __amdgpu_buffer_rsrc_t rows) {
+    bool k_own = false, v_own = false;      // what they hold is codes (MX4): two words, and in the second of them an exponent as a unit
+    auto request = [&](u32x4 (&in)[2], const RowsAt& r, const char* prefix, const char* pages, int exponent) {
+      if (MX4 && r.own) {
+        const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(half_rows(pages + r.offset * kMxRowBytes, r.n, kMxRowBytes), lane * 8, 0, 0);
+        in[0][0] = codes[0];
+        in[0][1] = codes[1];
+        in[1][0] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(half_rows((const char*)c.cache.scales + r.offset * kMxScaleBytes, r.n, kMxScaleBytes),
+                                                                (lane >> 2) * kMxScaleBytes + (lane & 2) + exponent, 0, 0);
+        return;
+      }
+      const __amdgpu_buffer_rsrc_t rows = half_rows((r.own ? pages : prefix) + r.offset, r.n);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) in[i] = load_row(rows, lane * 16 + i * 1024);
+      for (int i = 0; i < 2; ++i) in[i] = load_row(rows, MX4 ? lane * 32 + i * 16 : lane * 16 + i * 1024);
     };
-    auto store_k = [&](int to, const u32x4 (&in)[2]) {
-      *(u32x4*)(s_mem + to) = in[0];
-      *(u32x4*)(s_mem + (to ^ 64) + 8 * kRowBytes) = in[1];      // (k_swizzle() of the row 8 further: 4 more)
+    auto request_k = [&](u32x4 (&in)[2], const RowsAt& r) { request(in, r, c.k_prefix, c.cache.k_pages, 0); };
+    auto request_v = [&](u32x4 (&in)[2], const RowsAt& r) { request(in, r, c.v_prefix, c.cache.v_pages, 1); };
+    auto expanded = [&](u32x4 (&in)[2], bool own) {
+      if (MX4 && own) {
+        const float unit = __uint_as_float(in[1][0] << 23);
+        const uint32_t c0 = in[0][0], c1 = in[0][1];
+        in[0] = mx4_values(c0, unit);
+        in[1] = mx4_values(c1, unit);
+      }
     };
-    auto store_v = [&](int to, const u32x4 (&in)[2]) {
+    auto store_k = [&](int to, u32x4 (&in)[2], bool own) {
+      expanded(in, own);
       *(u32x4*)(s_mem + to) = in[0];
-      *(u32x4*)(s_mem + to + 8 * kRowBytes) = in[1];
+      if constexpr (MX4)
+        *(u32x4*)(s_mem + (to ^ 16)) = in[1];
+      else
+        *(u32x4*)(s_mem + (to ^ 64) + 8 * kRowBytes) = in[1];      // (k_swizzle() of the row 8 further: 4 more)
+    };
+    auto store_v = [&](int to, u32x4 (&in)[2], bool own) {
+      expanded(in, own);
+      *(u32x4*)(s_mem + to) = in[0];
+      *(u32x4*)(s_mem + (MX4 ? to ^ 16 : to + 8 * kRowBytes)) = in[1];
     };
     // 4 bits for a unit, whether its quarters have pages: looked at only where some entry of the tile's is none
     bool holes = false;
@@ -981,18 +1052,20 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       RowsAt v_next = rows_at(u0), k_next = rows_at(u0 + 1);
       {
         u32x4 k1[2];
-        request(in_k, k_rows(v_next));
-        request(in_v, v_rows(v_next));
-        request(k1, k_rows(k_next));
-        store_k(to_k, in_k);
-        store_k(to_k ^ kSide, k1);
-        store_v(to_v ^ kSide, in_v);
+        request_k(in_k, v_next);
+        request_v(in_v, v_next);
+        request_k(k1, k_next);
+        store_k(to_k, in_k, v_next.own);
+        store_k(to_k ^ kSide, k1, k_next.own);
+        store_v(to_v ^ kSide, in_v, v_next.own);
         *(u32x4*)(s_mem + (v_at[0] & ~(kSide - 1)) + kHalf + threadIdx.x * 16) = u32x4{0, 0, 0, 0};
       }
       v_next = k_next;
       k_next = rows_at(u0 + 2);
-      request(in_k, k_rows(k_next));
-      request(in_v, v_rows(v_next));
+      request_k(in_k, k_next);
+      request_v(in_v, v_next);
+      k_own = k_next.own;
+      v_own = v_next.own;
       bool hole = false;
       for (int i = lane; i < (most + (1 << c.cache.page_shift) - 1) >> c.cache.page_shift; i += 64) hole |= !there(table[i]);
       holes = __ballot(hole) != 0;
@@ -1009,12 +1082,14 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
         const uint32_t ok = ok_of(unit);
         if (active) step(kHalf, row0, end, ok & 3, own);
         barrier();      // K of this unit and V of the one before have been read by everybody
-        store_k(to_k, in_k);
-        store_v(to_v, in_v);
+        store_k(to_k, in_k, k_own);
+        store_v(to_v, in_v, v_own);
         v_next = k_next;
         k_next = rows_at(unit + 3);
-        request(in_k, k_rows(k_next));
-        request(in_v, v_rows(v_next));
+        request_k(in_k, k_next);
+        request_v(in_v, v_next);
+        k_own = k_next.own;
+        v_own = v_next.own;
         change_sides();
         if (active) step(0, row0 + 32, end, ok >> 2, own);
       }
@@ -1077,6 +1152,7 @@ struct CombineArgs {
   int64_t n_tokens;
   const int32_t* offsets;
   void* o;
+  float* lse;
 };
 
 // 16 lanes have a piece's 64 channels; GP groups of them take a row's pieces in turn.
@@ -1126,6 +1202,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
     float top = m;
 #pragma unroll
     for (int i = 1; i < GP; ++i) top = fmaxf(top, s_ml[group + i].x);
+    m = top;
     l = 0.f;
     o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -1136,6 +1213,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
     }
   }
   if (pieces == 0) return;
+  if (a.lse && l16 == 0) a.lse[row] = log_sum(m, l);
   const float f = l == 0.f ? 0.f : 1.f / l;
   *(u32x2*)((char*)a.o + (row * kDHead + 4 * l16) * 2) = u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
 }
@@ -1191,12 +1269,23 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
 }
 int64_t slot_bytes(const Choice& c, int i) { return align256(c.slots[i] * c.rows[i] * 8) + align256(c.slots[i] * c.rows[i] * kDHead * 4); }
 
-template <int NA, int NB>
+template <int NA, int NB, bool MX4>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
   if (a.c.causal)
-    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, true>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, true, MX4>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
   else
-    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, false>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, false, MX4>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
+}
+template <int NA, int NB>
+void start(const LineArgs& a, int shares, hipStream_t stream) {
+  a.c.cache.scales ? start<NA, NB, true>(a, shares, stream) : start<NA, NB, false>(a, shares, stream);
+}
+template <bool MX4>
+void start_wide(const LineArgs& a, bool causal, int shares, hipStream_t stream) {
+  if (causal)
+    hipLaunchKernelGGL((attention_cached_wide_kernel<true, MX4>), dim3(shares), dim3(64 * kWideWaves), 0, stream, a);
+  else
+    hipLaunchKernelGGL((attention_cached_wide_kernel<false, MX4>), dim3(shares), dim3(64 * kWideWaves), 0, stream, a);
 }
 
 }  // namespace
@@ -1224,6 +1313,7 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
   cb.n_tokens = args.n_tokens;
   cb.offsets = args.offsets;
   cb.o = args.o;
+  cb.lse = args.lse;
   char* at = args.workspace;
   for (int i = ch.stacked ? 0 : 1; i < 2; ++i) {
     const int64_t rows = ch.slots[i] * ch.rows[i];
@@ -1233,19 +1323,18 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
     cb.part[cb.n_parts++] = {a.part[i].rows, a.part[i].slot_ml, a.part[i].slot_o, (int32_t)rows};
   }
   // Tiles of 256 rows: the part is all of the launch's line
-  auto start_wide = [&](int i) {
+  auto wide = [&](int i) {
     LineArgs w = a;
     w.part[0] = a.part[i];
     w.min_length = 2 * kWideUnit;
-    if (args.causal && i == 1)
-      hipLaunchKernelGGL(attention_cached_wide_kernel<true>, dim3(ch.shares[i]), dim3(64 * kWideWaves), 0, stream, w);
-    else
-      hipLaunchKernelGGL(attention_cached_wide_kernel<false>, dim3(ch.shares[i]), dim3(64 * kWideWaves), 0, stream, w);
+    // (the part of the prefix has no rows in 4 bits)
+    const bool causal = args.causal && i == 1;
+    i == 1 && args.cache.scales ? start_wide<true>(w, causal, ch.shares[i], stream) : start_wide<false>(w, causal, ch.shares[i], stream);
   };
-  if (ch.stacked && ch.tiles[0] == 0) start_wide(0);
+  if (ch.stacked && ch.tiles[0] == 0) wide(0);
   const int na = ch.tiles[0], nb = ch.tiles[1], shares = ch.shares[1];
   if (nb == 0)
-    start_wide(1);
+    wide(1);
   else if (na == 0)
     nb == 1 ? start<0, 1>(a, shares, stream) : nb == 2 ? start<0, 2>(a, shares, stream) : start<0, 4>(a, shares, stream);
   else if (na == 1)

@@ -202,8 +202,9 @@ struct TokenRows {
   int64_t head_stride;
 };
 struct PagedArgs {
-  char* k_pages;
+  char* k_pages;            // bf16 rows, or with `scales` codes of 4 bits (mx4.hpp)
   char* v_pages;
+  uint8_t* scales;
   const int32_t* table;
   int64_t n_pages;
   int32_t n_seqs;
@@ -233,6 +234,15 @@ struct NormRopeArgs {
 };
 // dtype: HTTM_BF16 / _FP16 / _FP32 of the sources; append: into a.cache instead of [H, N, 64] tensors.
 hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, bool append, hipStream_t stream);
+// The rows of a batch's tokens out of the cache, as bf16 [N][H_kv][64]
+struct CacheReadArgs {
+  PagedArgs cache;
+  const int32_t* offsets;
+  const int32_t* seq_lens;
+  int64_t N;
+  char* out[2];             // k, v
+};
+hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
 
 // ---- attention of a batch with a shared prefix and a paged cache --------------------------------------
 struct CachedAttnArgs {
@@ -248,9 +258,39 @@ struct CachedAttnArgs {
   int32_t causal;
   float scale_log2;         // scale * log2(e)
   void* o;                  // [n_tokens][H_kv * group * 64] bf16
+  float* lse;               // [n_tokens][H_kv * group] or nullptr
   char* workspace;
 };
 int64_t cached_attention_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P);
 hipError_t launch_cached_attention(const CachedAttnArgs& a, hipStream_t stream);
+
+// ---- accumulated attention weights, eviction ----------------------------------------------------------
+struct WeighArgs {
+  TokenRows q;
+  const float* lse;         // [n_tokens][H_kv * group]
+  PagedArgs cache;
+  const int32_t* offsets;
+  const int32_t* seq_lens;
+  int64_t n_tokens;
+  int32_t group;
+  int32_t causal;
+  float scale;
+  float decay;
+  float* weights;           // [n_seqs][H_kv][columns]
+  int64_t columns;
+};
+hipError_t launch_cache_weigh(const WeighArgs& a, hipStream_t stream);
+struct EvictArgs {
+  PagedArgs cache;
+  const int32_t* seq_lens;
+  float* weights;
+  int64_t columns;
+  int32_t keep, first, last;
+  int32_t* new_lens;
+  int32_t* kept;            // [n_seqs][H_kv][keep] or nullptr
+  char* workspace;
+};
+int64_t cache_evict_workspace(int n_seqs, int H_kv, int keep);
+hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t stream);
 
 }  // namespace httm

@@ -21,6 +21,7 @@
 
 #include "dev_common.hpp"
 #include "kernels.hpp"
+#include "mx4.hpp"
 
 namespace httm {
 
@@ -156,14 +157,15 @@ struct CachePlace {
   int64_t row;        // in its sequence
   int64_t page_row;   // page * H_kv * page_size + row in the page: add head * page_size
 };
-__device__ __forceinline__ CachePlace find_place(const NormRopeArgs& a, int64_t t, int lane) {
+__device__ __forceinline__ CachePlace find_place(const PagedArgs& cache, const int32_t* offsets, const int32_t* seq_lens, int64_t N, int64_t t,
+                                                 int lane) {
   CachePlace c = {false, false, 0, 0};
   // how many offsets are not above t: 64 at a time, one load for the whole wave.  us for 4096 tokens of 32 + 2 x 8 heads in 1 / 64 / 512 / 4096 sequences: 16.4 /
   // 17.0 / 22.8 / 64.9; one token each of 32 / 70 / 1000: 4.6 / 4.9 / 13.6
   int below = 0;
-  const int n_off = a.cache.n_seqs + 1, mine = lane >> 3;
+  const int n_off = cache.n_seqs + 1, mine = lane >> 3;
   for (int i = 0; i < n_off; i += 64) {
-    const int off = i + lane < n_off ? a.offsets[i + lane] : INT32_MAX;
+    const int off = i + lane < n_off ? offsets[i + lane] : INT32_MAX;
 #pragma unroll
     for (int j = 0; j < kTokens; ++j) {
       const int64_t tj = __shfl((int)t, 8 * j);
@@ -172,21 +174,33 @@ __device__ __forceinline__ CachePlace find_place(const NormRopeArgs& a, int64_t 
     }
   }
   const int b = below - 1;
-  if (t >= a.N || b < 0 || b >= a.cache.n_seqs) return c;
+  if (t >= N || b < 0 || b >= cache.n_seqs) return c;
   c.real = true;
-  const int64_t most = (int64_t)a.cache.table_stride << a.cache.page_shift;
-  const int64_t len = std::clamp<int64_t>(a.seq_lens[b], 0, most);
-  c.row = len - a.offsets[b + 1] + t;
+  const int64_t most = (int64_t)cache.table_stride << cache.page_shift;
+  const int64_t len = std::clamp<int64_t>(seq_lens[b], 0, most);
+  c.row = len - offsets[b + 1] + t;
   if (c.row < 0 || c.row >= most) return c;
-  const int64_t page = a.cache.table[(int64_t)b * a.cache.table_stride + (c.row >> a.cache.page_shift)];
-  if (page < 0 || page >= a.cache.n_pages) return c;
+  const int64_t page = cache.table[(int64_t)b * cache.table_stride + (c.row >> cache.page_shift)];
+  if (page < 0 || page >= cache.n_pages) return c;
   c.in_cache = true;
-  c.page_row = ((page * a.cache.H_kv) << a.cache.page_shift) + (c.row & ((1 << a.cache.page_shift) - 1));
+  c.page_row = ((page * cache.H_kv) << cache.page_shift) + (c.row & ((1 << cache.page_shift) - 1));
   return c;
 }
 
+// Largest |x| of the four lanes that have a block of 32 channels, as bits: in that order a NaN is above everything
+__device__ __forceinline__ uint32_t block_top(const float (&x)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = std::max(top, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+  top = std::max(top, __float_as_uint(moved<kXor1>(__uint_as_float(top))));
+  return std::max(top, __float_as_uint(moved<kXor2>(__uint_as_float(top))));
+}
+
+// Where a wave's rows go: [H, N, 64] tensors, or the pages of a cache of bf16 rows or of rows in 4 bits
+enum { TO_DENSE, TO_PAGES, TO_MX4 };
+
 // A wave's part of q, k or v: heads [head0, head1) of its eight tokens
-template <int DT, bool APPEND, bool NT, int AHEAD>
+template <int DT, int DEST, bool NT, int AHEAD>
 __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeArgs a, int heads_per_wave) {
   const int lane = threadIdx.x & 63, chunk = lane & 7;
   const int64_t t = (int64_t)blockIdx.x * kTokens + (lane >> 3);
@@ -213,7 +227,8 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
   request(head0);
 
   CachePlace place = {true, false, 0, 0};
-  if constexpr (APPEND) place = find_place(a, t, lane);
+  constexpr bool APPEND = DEST != TO_DENSE;
+  if constexpr (APPEND) place = find_place(a.cache, a.offsets, a.seq_lens, a.N, t, lane);
   const bool write = t < a.N && place.real && (!APPEND || part == 0 || place.in_cache);
 
   LaneRope rope = {};
@@ -247,9 +262,13 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
   } else if (part == 0) {
     out += (t * a.H[0] + head0) * kRowBytes;
   } else {
-    out = (part == 1 ? a.cache.k_pages : a.cache.v_pages) + (place.page_row + ((int64_t)head0 << a.cache.page_shift)) * kRowBytes;
-    out_bytes = (int64_t)kRowBytes << a.cache.page_shift;
+    constexpr int kBytesOut = DEST == TO_MX4 ? kMxRowBytes : kRowBytes;
+    out = (part == 1 ? a.cache.k_pages : a.cache.v_pages) + (place.page_row + ((int64_t)head0 << a.cache.page_shift)) * kBytesOut;
+    out_bytes = (int64_t)kBytesOut << a.cache.page_shift;
   }
+  uint8_t* scale_out = DEST == TO_MX4 ? a.cache.scales + (place.page_row + ((int64_t)head0 << a.cache.page_shift)) * kMxScaleBytes +
+                                            2 * (chunk >> 2) + (part == 2 ? 1 : 0)
+                                      : nullptr;
   for (int head = head0; head < head1; head += AHEAD) {
     RawChunk<DT> raw[AHEAD];
 #pragma unroll
@@ -258,7 +277,7 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       u32x4 packed;
-      if (part == 2 && DT == HTTM_BF16) {
+      if (part == 2 && DT == HTTM_BF16 && DEST != TO_MX4) {
         packed = raw[i].w[0];
       } else {
         float x[8];
@@ -270,6 +289,14 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= scale;
           }
+        }
+        if (DEST == TO_MX4 && part > 0) {
+          const uint32_t exponent = mx4_exponent(block_top(x)), codes = mx4_codes(x, exponent);
+          if (write && head + i < head1) {
+            *((uint32_t*)(out + (head - head0 + i) * out_bytes) + chunk) = codes;
+            if ((chunk & 3) == 0) scale_out[((int64_t)(head - head0 + i) << a.cache.page_shift) * kMxScaleBytes] = (uint8_t)exponent;
+          }
+          continue;
         }
         packed = pack_chunk(x);
       }
@@ -284,28 +311,71 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
   }
 }
 
+// Rows of the cache to [N][H_kv][64], as values: heads [head0, head1) of eight tokens' keys or values, eight lanes a row.  Bound by memory: 
+// 68 or 256 bytes in and 256 out for a token and head.
+template <bool MX4>
+__global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(const CacheReadArgs a, int heads_per_wave) {
+  constexpr int kAtOnce = 4;
+  const int lane = threadIdx.x & 63, chunk = lane & 7, H = a.cache.H_kv;
+  const int64_t t = (int64_t)blockIdx.x * kTokens + (lane >> 3);
+  const int waves = (H + heads_per_wave - 1) / heads_per_wave;
+  int wave = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= 2 * waves) return;
+  const int part = wave >= waves ? 1 : 0;
+  wave -= part * waves;
+  const int head0 = wave * heads_per_wave, head1 = std::min(head0 + heads_per_wave, H);
+  const CachePlace place = find_place(a.cache, a.offsets, a.seq_lens, a.N, t, lane);
+  constexpr int kBytesIn = MX4 ? kMxRowBytes : kRowBytes;
+  const char* in = (part ? a.cache.v_pages : a.cache.k_pages) + place.page_row * kBytesIn;
+  const uint8_t* scales = MX4 ? a.cache.scales + place.page_row * kMxScaleBytes + 2 * (chunk >> 2) + part : nullptr;
+  char* out = a.out[part] + t * H * kRowBytes;
+  for (int head = head0; head < head1; head += kAtOnce) {
+    u32x4 x[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      x[i] = u32x4{0, 0, 0, 0};
+      const int64_t row = (int64_t)std::min(head + i, head1 - 1) << a.cache.page_shift;
+      if (place.in_cache) {
+        if constexpr (MX4) {
+          x[i][0] = *((const uint32_t*)(in + row * kBytesIn) + chunk);
+          x[i][1] = scales[row * kMxScaleBytes];
+        } else {
+          x[i] = *((const u32x4*)(in + row * kBytesIn) + chunk);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const u32x4 y = MX4 ? mx4_values(x[i][0], __uint_as_float(x[i][1] << 23)) : x[i];
+      if (place.real && head + i < head1) *((u32x4*)(out + (head + i) * kRowBytes) + chunk) = y;
+    }
+  }
+}
+
 }  // namespace
 
-template <int DT, bool APPEND, bool NT>
+template <int DT, int DEST, bool NT>
 void start_norm_rope(const NormRopeArgs& a, int64_t groups, int heads_per_wave, hipStream_t stream) {
   int waves = 0;
   for (int h : a.H) waves += (h + heads_per_wave - 1) / heads_per_wave;
   const dim3 grid((unsigned)groups, (unsigned)((waves + kWaves - 1) / kWaves)), block(64 * kWaves);
   if (heads_per_wave == 1)
-    hipLaunchKernelGGL((norm_rope_kernel<DT, APPEND, NT, 1>), grid, block, 0, stream, a, heads_per_wave);
+    hipLaunchKernelGGL((norm_rope_kernel<DT, DEST, NT, 1>), grid, block, 0, stream, a, heads_per_wave);
   else if (heads_per_wave == 2)
-    hipLaunchKernelGGL((norm_rope_kernel<DT, APPEND, NT, 2>), grid, block, 0, stream, a, heads_per_wave);
+    hipLaunchKernelGGL((norm_rope_kernel<DT, DEST, NT, 2>), grid, block, 0, stream, a, heads_per_wave);
   else
-    hipLaunchKernelGGL((norm_rope_kernel<DT, APPEND, NT, 4>), grid, block, 0, stream, a, heads_per_wave);
+    hipLaunchKernelGGL((norm_rope_kernel<DT, DEST, NT, 4>), grid, block, 0, stream, a, heads_per_wave);
 }
 template <int DT>
 void start_norm_rope(const NormRopeArgs& a, bool append, bool nt, int64_t groups, int heads_per_wave, hipStream_t stream) {
-  if (append)
-    start_norm_rope<DT, true, false>(a, groups, heads_per_wave, stream);
+  if (append && a.cache.scales)
+    start_norm_rope<DT, TO_MX4, false>(a, groups, heads_per_wave, stream);
+  else if (append)
+    start_norm_rope<DT, TO_PAGES, false>(a, groups, heads_per_wave, stream);
   else if (nt)
-    start_norm_rope<DT, false, true>(a, groups, heads_per_wave, stream);
+    start_norm_rope<DT, TO_DENSE, true>(a, groups, heads_per_wave, stream);
   else
-    start_norm_rope<DT, false, false>(a, groups, heads_per_wave, stream);
+    start_norm_rope<DT, TO_DENSE, false>(a, groups, heads_per_wave, stream);
 }
 
 hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, bool append, hipStream_t stream) {
@@ -325,6 +395,19 @@ hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, bool append, hipSt
     start_norm_rope<HTTM_FP16>(a, append, nt, groups, per, stream);
   else
     start_norm_rope<HTTM_FP32>(a, append, nt, groups, per, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream) {
+  if (a.N == 0) return hipSuccess;
+  const int64_t groups = (a.N + kTokens - 1) / kTokens;
+  const int H = a.cache.H_kv, per = groups * H < 2048 ? 1 : 4;
+  const int waves = 2 * ((H + per - 1) / per);
+  const dim3 grid((unsigned)groups, (unsigned)((waves + kWaves - 1) / kWaves)), block(64 * kWaves);
+  if (a.cache.scales)
+    hipLaunchKernelGGL(cache_read_kernel<true>, grid, block, 0, stream, a, per);
+  else
+    hipLaunchKernelGGL(cache_read_kernel<false>, grid, block, 0, stream, a, per);
   return hipGetLastError();
 }
 

@@ -1,0 +1,374 @@
+"""The cache in 4 bits: what the append writes, what comes back, and attention to it, against the definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2511_21317_amd as httm
+from mx4_util import PackedBatch, exponents, nearest, pack, power, scales_of, unpack
+from test_gpu_attention_cached import SHAPES, Batch, D, spread
+from test_gpu_token_rows import DTYPES, affine, formula, positions
+
+pytestmark = pytest.mark.gpu
+
+PLAIN = dict(norm="none", axes=0)
+
+
+def same(a, b, what):
+    bad = (a != b) & ~(torch.isnan(a) & torch.isnan(b))
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} differ, first {bad.nonzero()[0].tolist()}: {a[bad][0].item()} for {b[bad][0].item()}"
+
+
+class Pages:
+    """An empty packed cache with a mark in every byte, and a batch of new tokens."""
+
+    def __init__(self, new, lens, H, page, pad_front=0, pad=0, seed=0, spare=2):
+        torch.manual_seed(seed + sum(lens))
+        need = [max(0, -(-n // page)) for n in lens]
+        n_pages = sum(need) + spare
+        order, at = torch.randperm(n_pages).to(torch.int32), 0
+        table = torch.full((len(lens), max(need + [0]) + 1), -1, dtype=torch.int32)
+        for b, n in enumerate(need):
+            table[b, :n] = order[at:at + n]
+            at += n
+        u8 = dict(dtype=torch.uint8, device="cuda")
+        self.codes = [torch.full((n_pages, H, page, 32), 0xA5, **u8) for _ in range(2)]
+        self.scales = torch.full((n_pages, H, page, 4), 0x5A, **u8)
+        self.cache = httm.PackedCache(*self.codes, self.scales, table.cuda())
+        off = [pad_front]
+        for a in new:
+            off.append(off[-1] + a)
+        self.n, self.off, self.new, self.lens, self.H, self.page = off[-1] + pad, off, new, lens, H, page
+        self.table = table
+        self.offsets, self.seq_lens = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in (off, lens))
+
+    def places(self):
+        """(token, page, row) of every token that has a row with a page."""
+        out = []
+        for b, (n, L) in enumerate(zip(self.new, self.lens)):
+            for i in range(n):
+                row = L - n + i
+                if row >= 0:
+                    out.append((self.off[b] + i, int(self.table[b, row // self.page]), row % self.page))
+        return [p for p in out if 0 <= p[1] < self.codes[0].shape[0]]
+
+
+BATCHES = {   # new tokens, lengths, heads, page
+    "one": ([1], [1], 1, 16), "streams": ([1] * 9, [1, 16, 17, 300, 5, 64, 63, 2, 33], 4, 16), "ragged": ([0, 5, 130, 1, 0, 64], [7, 5, 200, 90, 0, 64], 3, 32),
+    "many": ([2] * 70, [2 + i % 40 for i in range(70)], 2, 16), "a frame": ([1374], [1500], 5, 256), "more than rows": ([9, 3], [4, 1], 2, 16),
+}
+
+
+def rows_of(n, H, dtype, seed):
+    """Values over the whole range of sizes: blocks of other widths, exact borders between codes, zeros, the smallest and largest."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    x = torch.randn((n, H, D), generator=g, device="cuda") * torch.exp(4.0 * torch.randn((n, H, 1), generator=g, device="cuda"))
+    border = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, -0.25, -2.5, -5.0, 0.0, -0.0, 4.0, 1.0, 3.0], device="cuda")
+    x[::3, 0] = border.repeat(4) * 2.0 ** torch.randint(-9, 9, (x[::3, 0].shape[0], 1), generator=g, device="cuda")
+    x[1::5, -1, :32] = 0.0
+    x[2::7, 0, 32:] = border.repeat(2) * 1.75 / 6.0         # largest: 1.75, the border between two exponents
+    if dtype != torch.float16:
+        x[3::11, 0] = (x[3::11, 0] * 2.0 ** 118).clamp(-3.38e38, 3.38e38)
+        x[4::11, -1] *= 2.0 ** -125
+        x[5::11, 0, 40] = torch.finfo(torch.bfloat16).max
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("batch", BATCHES, ids=lambda s: s.replace(" ", "_"))
+def test_append_writes_the_nearest_codes(batch, dtype):
+    new, lens, H, page = BATCHES[batch]
+    p = Pages(new, lens, H, page, pad_front=2, pad=5)
+    k, v = rows_of(p.n, H, DTYPES[dtype], 1), rows_of(p.n, H, DTYPES[dtype], 2)
+    q = torch.randn(p.n, 2 * H, D, device="cuda").to(DTYPES[dtype])
+    q_out = torch.full((p.n, 2 * H, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    want = [t.clone() for t in (*p.codes, p.scales)]
+    (kc, ke), (vc, ve) = pack(k), pack(v)
+    says = [torch.ones_like(t, dtype=torch.bool) for t in want]         # (the codes of a block that is NaN, as of an fp16 that is infinite, say nothing)
+    for t, pg, row in p.places():
+        want[0][pg, :, row], want[1][pg, :, row], want[2][pg, :, row] = kc[t], vc[t], scales_of(ke[t], ve[t])
+        for i, e in ((0, ke), (1, ve)):
+            says[i][pg, :, row] = (e[t] != 255).repeat_interleave(16, -1)
+    httm.cache_append(httm.NormRope(**PLAIN), q, k, v, None, p.cache, p.offsets, p.seq_lens, q_out)
+    for name, a, b, c in zip(("keys", "values", "scales"), (*p.codes, p.scales), want, says):
+        same(a[c], b[c], name)
+    real = slice(p.off[0], p.off[-1])
+    assert torch.equal(q_out[real], q[real].bfloat16())
+    assert (q_out[:p.off[0]] == 3).all() and (q_out[p.off[-1]:] == 3).all()
+    # and back: every value that the cache holds, zeros where a token has no row, padding as it was
+    got = [torch.full((p.n, H, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    httm.cache_read(p.cache, p.offsets, p.seq_lens, *got)
+    for name, x, c, e in (("keys", got[0], kc, ke), ("values", got[1], vc, ve)):
+        ref = torch.full((p.n, H, D), 7.0, dtype=torch.float64, device="cuda")
+        ref[real] = 0.0
+        for t, _, _ in p.places():
+            ref[t] = unpack(c[t], e[t])
+        same(x.double(), ref, name + " again")
+
+
+def test_blocks_that_are_not_finite_become_nan():
+    p = Pages([6], [6], 2, 16)
+    k, v = rows_of(6, 2, torch.float32, 3), rows_of(6, 2, torch.float32, 4)
+    k[1, 0, 5], k[2, 1, 40], v[3, 0, 63], v[4, 1, 0] = float("inf"), float("nan"), -float("inf"), -float("nan")
+    httm.cache_append(httm.NormRope(**PLAIN), None, k, v, None, p.cache, p.offsets, p.seq_lens, None)
+    got = [torch.empty(6, 2, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    httm.cache_read(p.cache, p.offsets, p.seq_lens, *got)
+    for x, g in zip((k, v), got):
+        ref = unpack(*pack(x))
+        assert torch.equal(torch.isnan(g), torch.isnan(ref)) and int(torch.isnan(g).sum()) == 64
+        assert torch.equal(g.double().nan_to_num(9.0), ref.nan_to_num(9.0))
+
+
+@pytest.mark.parametrize("norm,axes,rot_dim,pairing,base,dtype", [
+    ("layer", 2, 64, "halves", 100.0, "bf16"), ("rms", 1, 48, "neighbours", 500000.0, "fp32"), ("none", 3, 48, "halves", 10000.0, "fp16"),
+    ("rms", 1, 32, "halves", 10000.0, "bf16"), ("layer", 0, 0, "halves", 1.0, "fp32")])
+def test_append_rounds_what_norm_and_rotation_leave(norm, axes, rot_dim, pairing, base, dtype):
+    """Codes are those of a value within what fp32 arithmetic may be off: between the codes of both ends, at the exponent of either."""
+    new, lens, H, page = BATCHES["ragged"]
+    p = Pages(new, lens, H, page)
+    x = (torch.randn(p.n, 2 * H, D, device="cuda") * 1.7 + 0.8).to(DTYPES[dtype])
+    k, v = x[:, :H], x[:, H:]
+    kw = affine(norm, 5)
+    nr = httm.NormRope(norm=norm, eps=1e-5, axes=axes, rot_dim=rot_dim, pairing=pairing, base=base, k_scale=0.18, **kw)
+    pos = positions(p.n, axes, 5000, 9)
+    httm.cache_append(nr, None, k, v, pos, p.cache, p.offsets, p.seq_lens, None)
+    got = [torch.empty(p.n, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    httm.cache_read(p.cache, p.offsets, p.seq_lens, *got)
+    assert torch.equal(got[1].double(), unpack(*pack(v)))
+    scale = float(torch.tensor(0.18, dtype=torch.float32))
+    ref, tol = formula(k, norm, kw.get("k_weight"), kw.get("k_bias"), 1e-5, axes, rot_dim, pairing, base, pos, scale)
+    tol = tol - 2.0 ** -8 * ref.abs() * scale ** 0         # (formula() counts the rounding to bf16, which is not taken here)
+    tol = tol.clamp_min(2.0 ** -20 * ref.abs() + 1e-30)
+    y, t, g = (z.unflatten(-1, (2, 32)) for z in (ref, tol, got[0].double()))
+    lo, hi = exponents((y.abs() - t).clamp_min(0).amax(-1)), exponents((y.abs() + t).amax(-1))
+    fits = torch.zeros_like(g, dtype=torch.bool)
+    for e in (lo, hi):
+        unit = power(e)[..., None]
+        level = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device="cuda")
+        ends = [torch.sign(z) * level[nearest(z, e)] * unit for z in (y - t, y + t)]
+        fits |= ((g >= ends[0]) & (g <= ends[1])).all(-1, keepdim=True)
+    assert fits.all(), f"{int((~fits).sum())} of {fits.numel()}"
+    assert (g - y).abs().max() > 0
+
+
+def test_read_of_a_cache_in_16_bits():
+    b = Batch([3, 1, 130], [3, 40, 200], 0, 3, 3, 16, pad_front=2, pad=3)
+    b.cache.page_table[2, 5] = -1
+    k, v = (torch.full((b.n, 3, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    httm.cache_read(b.cache, b.offsets, b.seq_lens, k, v)
+    for got, own in ((k, b.k), (v, b.v)):
+        assert (got[:2] == 7).all() and (got[b.off[-1]:] == 7).all()
+        for i, (n, L) in enumerate(zip(b.new, b.lens)):
+            ref = own[i][:, L - n:].transpose(0, 1).clone()
+            if i == 2:
+                ref[80 - (L - n):96 - (L - n)] = 0.0
+            assert torch.equal(got[b.off[i]:b.off[i + 1]], ref), i
+
+
+def test_tokens_without_a_page_and_lengths_out_of_range():
+    p = Pages([20, 5, 4], [60, 40, 30], 2, 16)
+    bad = p.cache.page_table
+    bad[0, 3], bad[1, 2] = p.codes[0].shape[0], 2**31 - 1
+    p.table = bad.cpu()
+    p.seq_lens.copy_(torch.tensor([60, 40, 2**31 - 1]))     # counts as all the rows of the table, whose last page is none
+    p.lens[2] = 0
+    k, v = rows_of(p.n, 2, torch.bfloat16, 1), rows_of(p.n, 2, torch.bfloat16, 2)
+    want = p.codes[0].clone()
+    kc, _ = pack(k)
+    for t, pg, row in p.places():
+        if t < 25:
+            want[pg, :, row] = kc[t]
+    httm.cache_append(httm.NormRope(**PLAIN), None, k, v, None, p.cache, p.offsets, p.seq_lens, None)
+    assert torch.equal(p.codes[0], want)
+    got = [torch.full((p.n, 2, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    httm.cache_read(p.cache, p.offsets, p.seq_lens, *got)
+    assert (got[0][8:20] == 0).all() and (got[1][20:] == 0).all() and (got[0][:8] != 0).any()
+
+
+# ---- attention -------------------------------------------------------------------------------------------------
+
+TRIED = ["one token, one row", "prefix alone", "nothing at all", "one token", "long cache", "streams", "streams without prefix",
+         "empty sequences", "drafts", "many streams", "grouped", "pieces of prompts", "a frame", "a prompt", "more tokens than rows",
+         "more streams than lanes", "one long among short", "rows of 64 heads", "a prompt behind another", "together, streams", "together, drafts",
+         "together, pieces", "together, many rows", "together, more rows", "wide, a frame", "wide, frames", "wide, a prompt", "wide, odd groups",
+         "wide, pieces of prompts", "wide, more tokens than rows"]
+
+
+def sums(b, causal, scale=0.125):
+    """lse in 64 bits, [n, H_q], of the batch's real tokens (else 5), and what fp32 may be off by."""
+    ref = torch.full((b.n, b.H_q), 5.0, dtype=torch.float64, device="cuda")
+    tol = torch.zeros_like(ref)
+    G = b.H_q // b.H_kv
+    for i, (n, L) in enumerate(zip(b.new, b.lens)):
+        for h in range(b.H_kv if n else 0):
+            k = torch.cat([b.kp[h], b.k[i][h]]).double()
+            q = b.q[b.off[i]:b.off[i + 1], h * G:(h + 1) * G].double()
+            s = q @ k.T * scale
+            if causal:
+                r, j = torch.arange(n, device="cuda")[:, None], torch.arange(L, device="cuda")[None]
+                s[:, :, b.P:].masked_fill_((j > L - n + r)[:, None], -math.inf)
+            at = slice(b.off[i], b.off[i + 1]), slice(h * G, (h + 1) * G)
+            ref[at] = torch.logsumexp(s, -1) if k.shape[0] else -math.inf
+            size = (q.abs() @ k.abs().T * scale).amax(-1) if k.shape[0] else 0.0
+            # weights of a sum rounded to bf16 (tiles of 256 rows), 2^-9 on either side of 1 at most; scores: sums of 64 products; shift and logarithm
+            tol[at] = 2.0 ** -8 + 2.0 ** -17 * size + 2.0 ** -20 * torch.where(torch.isfinite(ref[at]), ref[at].abs(), 0.0)
+    return ref, tol
+
+
+def check_sums(lse, b, causal):
+    ref, tol = sums(b, causal)
+    none = torch.isinf(ref)
+    assert torch.equal(torch.isinf(lse), none) and (lse[none] < 0).all()
+    off = (lse.double() - ref).abs()[~none]
+    assert (off <= tol[~none]).all(), float((off / tol[~none].clamp_min(1e-30)).max())
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", TRIED, ids=lambda s: s.replace(" ", "_").replace(",", ""))
+def test_attention(shape, causal):
+    b = PackedBatch(*SHAPES[shape], seed=len(shape), pad_front=3, pad=4)
+    got = b.check(causal)
+    lse = torch.full((b.n, b.H_q), 5.0, device="cuda")
+    out = torch.full_like(got, 5.0)
+    httm.attention_cached(b.q, b.kp if b.P else None, b.vp if b.P else None, b.cache, b.offsets, b.seq_lens, out, causal=causal, workspace=b.ws, lse=lse)
+    assert torch.equal(out, got)
+    check_sums(lse, b, causal)
+
+
+@pytest.mark.parametrize("shape", ["one token", "nothing at all", "streams", "drafts", "a prompt", "together, drafts", "wide, frames"],
+                         ids=lambda s: s.replace(" ", "_").replace(",", ""))
+def test_sums_of_a_cache_in_16_bits(shape):
+    b = Batch(*SHAPES[shape], seed=len(shape), pad_front=1, pad=2)
+    want, lse, out = b.run(True), torch.full((b.n, b.H_q), 5.0, device="cuda"), torch.full((b.n, b.H_q * D), 5.0, dtype=torch.bfloat16, device="cuda")
+    httm.attention_cached(b.q, b.kp if b.P else None, b.vp if b.P else None, b.cache, b.offsets, b.seq_lens, out, causal=True, workspace=b.ws, lse=lse)
+    assert torch.equal(out, want)
+    check_sums(lse, b, True)
+
+
+@pytest.mark.parametrize("new,lens,P", [([5, 3], [40, 35], 50), ([200], [200], 100), ([5, 3] * 7, [40, 35] * 7, 17000), ([200], [200], 40000)])
+def test_keys_that_are_not_finite_stay_where_they_are_seen(new, lens, P):
+    b = PackedBatch(new, lens, P, 4, 2, 16)
+    for i, L in enumerate(lens):
+        page, row = int(b.cache.page_table[i, (L - 1) // 16]), (L - 1) % 16
+        b.cache.scales[page, 0, row, 1] = 255      # value, head 0, channels 0 .. 31
+        b.cache.scales[page, 1, row, 2] = 255      # key, head 1
+    got = b.run(True).view(-1, 4, D)
+    ref, tol = (t.view(-1, 4, D) for t in b.reference(True))
+    last = torch.zeros(b.n, dtype=torch.bool, device="cuda")
+    last[torch.tensor([b.off[i + 1] - 1 for i in range(len(new))], device="cuda")] = True
+    err = (got.double() - ref).abs()
+    assert (err[~last] <= tol[~last]).all()
+    assert torch.isnan(got[last][:, :2, :32]).all() and torch.isnan(got[last][:, 2:]).all()
+    assert (err[last][:, :2, 32:] <= tol[last][:, :2, 32:]).all()
+
+
+@pytest.mark.parametrize("new,lens,P", [([2, 1, 90], [100, 50, 200], 33), ([2, 1, 4] * 6, [100, 50, 200] * 6, 16000), ([2, 1, 690], [100, 50, 800], 24033)])
+def test_pages_that_are_none_are_left_out(new, lens, P):
+    b = PackedBatch(new, lens, P, 2, 2, 16)
+    drop = [torch.zeros(n, dtype=torch.bool, device="cuda") for n in b.lens]
+    for i, j, bad in ((0, 2, -1), (0, 6, 2**31 - 1), (1, 0, -5), (2, 3, int(b.cache.k_codes.shape[0])), (2, 12, -1)):
+        b.cache.page_table[i, j] = bad
+        drop[i][16 * j:16 * j + 16] = True
+    b.check(False, drop=drop)
+    b.check(True, drop=drop)
+
+
+def test_queries_of_any_strides_scales_and_runs():
+    for name in ("drafts", "streams", "wide, frames", "together, many rows"):
+        b = PackedBatch(*SHAPES[name], seed=8)
+        want = b.run(True)
+        wide = torch.full((b.n, 2 * b.H_q, 2 * D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        wide[:, ::2, :D] = b.q
+        assert torch.equal(b.run(True, q=wide[:, ::2, :D]), want)
+        for fill in (0, 0x7F):
+            assert torch.equal(b.run(True, ws=torch.full((b.ws.numel(),), fill, dtype=torch.uint8, device="cuda")), want)
+        b.check(False, scale=0.4)
+
+
+def test_peaked_scores():
+    for shape in ("streams", "drafts", "frames", "wide, frames"):
+        PackedBatch(*SHAPES[shape], seed=3, k_scale=30.0).check(True)
+
+
+def test_cache_beyond_32_bit_offsets():
+    """Codes that lie more than 4 GB into their buffer, and scales with them."""
+    page, H = 256, 16
+    n_pages = (5 << 30) // (page * H * 32)
+    b = PackedBatch([1, 40], [500, 300], 50, H, H, page)
+    u8 = dict(dtype=torch.uint8, device="cuda")
+    k, v, s = torch.empty(n_pages, H, page, 32, **u8), torch.empty(n_pages, H, page, 32, **u8), torch.empty(n_pages, H, page, 4, **u8)
+    used = b.cache.k_codes.shape[0]
+    k[-used:], v[-used:], s[-used:] = b.cache.k_codes, b.cache.v_codes, b.cache.scales
+    table = torch.where(b.cache.page_table >= 0, b.cache.page_table + (n_pages - used), -1).to(torch.int32).contiguous()
+    b.cache = httm.PackedCache(k, v, s, table)
+    b.check()
+    x, y = rows_of(41, H, torch.bfloat16, 1), rows_of(41, H, torch.bfloat16, 2)
+    httm.cache_append(httm.NormRope(**PLAIN), None, x, y, None, b.cache, b.offsets, b.seq_lens, None)
+    got = [torch.empty(41, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    httm.cache_read(b.cache, b.offsets, b.seq_lens, *got)
+    assert torch.equal(got[0].double(), unpack(*pack(x))) and torch.equal(got[1].double(), unpack(*pack(y)))
+
+
+@pytest.mark.parametrize("B,n,P", [(4, 1, 700), (2, 100, 300), (2, 200, 19000), (14, 1, 16000)])
+def test_graph_of_append_and_attention_follows_the_lengths(B, n, P):
+    """Captured together; replays serve the sequences as they grow, next to other work."""
+    b = PackedBatch([n] * B, [n + 200] * B, P, 4, 2, 16)
+    nr = httm.NormRope(norm="rms", axes=1, base=10000.0)
+    k, v = (torch.randn(b.n, 2, D, device="cuda").bfloat16() for _ in range(2))
+    out, lse = torch.zeros(b.n, b.H_q * D, dtype=torch.bfloat16, device="cuda"), torch.zeros(b.n, b.H_q, device="cuda")
+
+    def step(out, lse, ws):
+        httm.cache_append(nr, None, k, v, None, b.cache, b.offsets, b.seq_lens, None)
+        httm.attention_cached(b.q, b.kp, b.vp, b.cache, b.offsets, b.seq_lens, out, causal=True, workspace=ws, lse=lse)
+
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(out, lse, b.ws)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            step(out, lse, b.ws)
+    torch.cuda.synchronize()
+    for i in range(4):
+        b.seq_lens.copy_(torch.tensor([n + i * 37 + j for j in range(B)]))
+        for t in (b.q, k, v):
+            t.copy_(torch.randn_like(t))
+        graph.replay()
+        codes = [t.clone() for t in (b.cache.k_codes, b.cache.v_codes, b.cache.scales)]
+        want, want_lse = torch.zeros_like(out), torch.zeros_like(lse)
+        step(want, want_lse, b.ws.clone())
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), i
+        assert all(torch.equal(x, y) for x, y in zip(codes, (b.cache.k_codes, b.cache.v_codes, b.cache.scales)))
+
+
+def test_two_streams_at_once():
+    a, b = PackedBatch(*SHAPES["streams"], seed=1), PackedBatch(*SHAPES["a whole scene"], seed=2)
+    want_a, want_b = a.run(), b.run()
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        with torch.cuda.stream(sa):
+            got.append((a.run(), want_a))
+        with torch.cuda.stream(sb):
+            got.append((b.run(), want_b))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in got)
+
+
+def test_what_the_cache_holds_is_within_half_a_step():
+    """The promise of the format: of a unit 2^(e - 127), a quarter up to 2, a half up to 4, one above."""
+    x = torch.randn(5000, 1, D, device="cuda") * torch.exp(3 * torch.randn(5000, 1, 1, device="cuda"))
+    p = Pages([5000], [5000], 1, 256)
+    httm.cache_append(httm.NormRope(**PLAIN), None, x, x, None, p.cache, p.offsets, p.seq_lens, None)
+    k, v = (torch.empty(5000, 1, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    httm.cache_read(p.cache, p.offsets, p.seq_lens, k, v)
+    assert torch.equal(k, v)
+    top = x.unflatten(-1, (2, 32)).abs().amax(-1, keepdim=True).expand(-1, -1, -1, 32).flatten(-2).double()
+    m, e = torch.frexp(top)
+    unit = power(torch.where(m >= 0.875, e + 1, e) - 3 + 127)
+    a = x.double().abs() / unit
+    step = torch.where(a <= 2, 0.25, torch.where(a <= 4, 0.5, 1.0)) * unit
+    assert ((k.double() - x.double()).abs() <= step).all()
