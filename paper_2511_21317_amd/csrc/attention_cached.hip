@@ -46,6 +46,10 @@ namespace httm {
 
 namespace {
 
+// What a kernel is made for: the cache's rows in 16 bits; the same, with the logarithms of the sums (which cost others registers that they do not
+// have: 2.8 % of the time of tiles of 256 rows); rows in 4 bits, with or without them
+enum { ROWS, ROWS_AND_SUMS, MX4_ROWS };
+
 constexpr int kUnit = 32;                       // keys
 constexpr int kUnitBytes = kUnit * kRowBytes;
 constexpr float kSlack = 10.f;
@@ -375,16 +379,15 @@ __device__ __forceinline__ void put(const LineArgs& a, const Part& part, const P
     *(f32x4*)(part.slot_o + ((int64_t)t.slot * R + r) * kDHead + channel) = o;
   }
 }
-template <int R>
+template <int R, bool LSE>
 __device__ __forceinline__ void put_sums(const LineArgs& a, const Part& part, const Place& p, const Seq& s, const Target& t, int r, float m,
                                          float l) {
-  if (p.tile * R + r >= s.n * a.c.group) return;
-  if (!t.finish) {
-    if ((uint32_t)t.slot < (uint32_t)part.max_slots) part.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
-  } else if (a.c.lse) {
-    const Row row = row_of(a, p, s, p.tile * R + r);
-    a.c.lse[(int64_t)row.token * a.H_q + row.head] = log_sum(m, l);
-  }
+  if constexpr (LSE)
+    if (t.finish && a.c.lse && p.tile * R + r < s.n * a.c.group) {
+      const Row row = row_of(a, p, s, p.tile * R + r);
+      a.c.lse[(int64_t)row.token * a.H_q + row.head] = log_sum(m, l);
+    }
+  if (!t.finish && (uint32_t)t.slot < (uint32_t)part.max_slots && p.tile * R + r < s.n * a.c.group) part.slot_ml[(int64_t)t.slot * R + r] = float2{m, l};
 }
 
 // V^T operands: 16 channels x 32 keys in the order of the weights (see the top)
@@ -471,9 +474,10 @@ __device__ __forceinline__ void add_seen(f32x4 (&o)[4][NQ], const bf16x8 (&av)[4
 
 // Scores, statistics and product of a unit.  row0: its first key; end: keys from there on are masked in all rows (causal
 // own keys: in some); ok: bit per half of 16 keys, whether it has a page; limit_of(qt): own keys that the lane's row sees.
-template <int NQ, bool CAUSAL, bool MX4, typename Limit>
+template <int NQ, bool CAUSAL, int KIND, typename Limit>
 __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, bf16_t* sv, float c, int row0, int end, int ok, bool own,
                                           int lane, Limit limit_of) {
+  constexpr bool MX4 = KIND == MX4_ROWS;
   const int l16 = lane & 15, grp = lane >> 4;
   const bool masked = ok != 3 || row0 + kUnit > end;
   const bool wild = CAUSAL && masked && own && __ballot(not_finite(d.v)) != 0;
@@ -552,9 +556,10 @@ __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, b
 // A share's way along a part of the line: four waves take the units of a piece in turn.  [x, end): positions in the part, `line`:
 // where it starts on the line.
 constexpr int kWaves = 4;
-template <int NQ, bool CAUSAL, bool MX4>
+template <int NQ, bool CAUSAL, int KIND>
 __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const Share& share, const Extent& ex, int64_t line, int64_t x,
                                      int64_t end, Seq window, char* s_mem, float2* s_ml) {
+  constexpr bool MX4 = KIND == MX4_ROWS;
   constexpr int R = 16 * NQ, KS = kWaves;
   constexpr int DEPTH = 1;     // units of a wave on their way besides the one in work
   const CachedAttnArgs& c = a.c;
@@ -675,7 +680,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
           expand(d[0], 0, half[0]);
           expand(d[0], 1, half[1]);
         }
-      unit_step<NQ, CAUSAL, MX4>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane, limit_of);
+      unit_step<NQ, CAUSAL, KIND>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane, limit_of);
 #pragma unroll
       for (int i = 0; i < DEPTH; ++i) {
         d[i] = d[i + 1];
@@ -711,7 +716,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
         sum += ml[k].y * f;
         o += so[(k * 16 + row) * 16 + (chunk ^ row)] * f;
       }
-      if (chunk == 0) put_sums<R>(a, part, p, s, to, 16 * qt + row, top, sum);
+      if (chunk == 0) put_sums<R, KIND != ROWS>(a, part, p, s, to, 16 * qt + row, top, sum);
       put<R>(a, part, p, s, to, 16 * qt + row, 4 * chunk, o, sum);
     }
     __syncthreads();
@@ -725,7 +730,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
 // NA query tiles of 16 rows for the first part of the line, the prefix against all sequences' rows, or 0: there is none;
 // NB for the second.
 constexpr int waves_per_simd(int nq) { return nq == 1 ? 3 : 2; }
-template <int NA, int NB, bool CAUSAL, bool MX4>
+template <int NA, int NB, bool CAUSAL, int KIND>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(waves_per_simd(NA > NB ? NA : NB), waves_per_simd(NA > NB ? NA : NB)))) void
 attention_cached_kernel(const LineArgs a) {
   __shared__ __attribute__((aligned(16))) char s_mem[kWaves * kUnitBytes];
@@ -740,10 +745,10 @@ attention_cached_kernel(const LineArgs a) {
   if (!find_share(a, total_a + total_b, share)) return;
   if constexpr (NA > 0)
     if (share.at < total_a) {
-      walk<NA, false, MX4>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
+      walk<NA, false, KIND>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
     }
   if (share.end > total_a)
-    walk<NB, CAUSAL, MX4>(a, a.part[1], share, eb, total_a, std::max(share.at, total_a) - total_a, share.end - total_a, window_b, s_mem, s_ml);
+    walk<NB, CAUSAL, KIND>(a, a.part[1], share, eb, total_a, std::max(share.at, total_a) - total_a, share.end - total_a, window_b, s_mem, s_ml);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------
@@ -787,8 +792,9 @@ __device__ __forceinline__ void raise_shift(WideState& w, const float (&top)[kWi
   }
 }
 
-template <bool CAUSAL, bool MX4>
+template <bool CAUSAL, int KIND>
 __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_cached_wide_kernel(const LineArgs a) {
+  constexpr bool MX4 = KIND == MX4_ROWS;
   constexpr int NQ = kWideQ, R = kWideRows, UNIT = kWideUnit;
   // K of two units, V of two.  All that reads or writes them goes by offsets that change sides once a unit.
   constexpr int kSide = UNIT * kRowBytes, kHalf = kSide / 2;
@@ -1115,7 +1121,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       for (int i = 0; i < 2; ++i) {
         const int qt = 2 * pair + i;
         l[i] = groups_sum(w.l[qt]);
-        if (grp == 0) put_sums<R>(a, part, p, s, to, wave * 16 * NQ + 16 * qt + l16, -w.m[qt], l[i]);
+        if (grp == 0) put_sums<R, KIND != ROWS>(a, part, p, s, to, wave * 16 * NQ + 16 * qt + l16, -w.m[qt], l[i]);
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct) so[(16 * i + l16) * 16 + ((4 * ct + grp) ^ l16)] = w.o[ct][qt];
       }
@@ -1269,23 +1275,28 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
 }
 int64_t slot_bytes(const Choice& c, int i) { return align256(c.slots[i] * c.rows[i] * 8) + align256(c.slots[i] * c.rows[i] * kDHead * 4); }
 
-template <int NA, int NB, bool MX4>
+template <int NA, int NB, int KIND>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
   if (a.c.causal)
-    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, true, MX4>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, true, KIND>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
   else
-    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, false, MX4>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((attention_cached_kernel<NA, NB, false, KIND>), dim3(shares), dim3(64 * kWaves), 0, stream, a);
 }
 template <int NA, int NB>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
-  a.c.cache.scales ? start<NA, NB, true>(a, shares, stream) : start<NA, NB, false>(a, shares, stream);
+  if (a.c.cache.scales)
+    start<NA, NB, MX4_ROWS>(a, shares, stream);
+  else if (a.c.lse && a.finish)      // (pieces in their slots leave the sums to combine_kernel)
+    start<NA, NB, ROWS_AND_SUMS>(a, shares, stream);
+  else
+    start<NA, NB, ROWS>(a, shares, stream);
 }
-template <bool MX4>
+template <int KIND>
 void start_wide(const LineArgs& a, bool causal, int shares, hipStream_t stream) {
   if (causal)
-    hipLaunchKernelGGL((attention_cached_wide_kernel<true, MX4>), dim3(shares), dim3(64 * kWideWaves), 0, stream, a);
+    hipLaunchKernelGGL((attention_cached_wide_kernel<true, KIND>), dim3(shares), dim3(64 * kWideWaves), 0, stream, a);
   else
-    hipLaunchKernelGGL((attention_cached_wide_kernel<false, MX4>), dim3(shares), dim3(64 * kWideWaves), 0, stream, a);
+    hipLaunchKernelGGL((attention_cached_wide_kernel<false, KIND>), dim3(shares), dim3(64 * kWideWaves), 0, stream, a);
 }
 
 }  // namespace
@@ -1329,7 +1340,12 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
     w.min_length = 2 * kWideUnit;
     // (the part of the prefix has no rows in 4 bits)
     const bool causal = args.causal && i == 1;
-    i == 1 && args.cache.scales ? start_wide<true>(w, causal, ch.shares[i], stream) : start_wide<false>(w, causal, ch.shares[i], stream);
+    if (i == 1 && args.cache.scales)
+      start_wide<MX4_ROWS>(w, causal, ch.shares[i], stream);
+    else if (args.lse && a.finish)
+      start_wide<ROWS_AND_SUMS>(w, causal, ch.shares[i], stream);
+    else
+      start_wide<ROWS>(w, causal, ch.shares[i], stream);
   };
   if (ch.stacked && ch.tiles[0] == 0) wide(0);
   const int na = ch.tiles[0], nb = ch.tiles[1], shares = ch.shares[1];

@@ -20,178 +20,336 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
 
 // ---- weights ---------------------------------------------------------------------------------------------------
 //
-// The rows of a sequence and a key head are those of attention: r / group-th token, query head h * group + r % group.  A wave
-// holds 64 keys as the A operands of S^T = K Q^T (v_mfma_f32_16x16x32_bf16) and goes over rows, 16 at a time: a lane has one row's scores of
-// 4 of 16 keys, and adds what they come to up, key by key; the sum over the 16 lanes is taken once, at the end.
-// Where sequences have few rows a wave goes over all of them; where they have many (SPLIT) the four waves of a
-// workgroup share their 64 keys and take the rows in turn.  No sum depends on how the work falls: results are run-to-run identical.
+// The rows of a sequence and a key head are those of attention: r / group-th token, query head h * group + r % group.  S = Q K^T with
+// v_mfma_f32_16x16x32_bf16, A = 16 rows and B = 16 keys of 32 channels: a lane has one key's scores of 4 of 16 rows, so that a key's sum is one register, and
+// what is left of it at the end two exchanges.  A wave holds 64 keys and goes over rows.  Two kernels: where sequences have few rows
+// every wave has keys of its own and keeps the rows of its head in registers from one item of 64 keys to the next; where
+// they have many, the four waves of a workgroup share 64 keys and take tiles of rows in turn.  No sum depends on how the work falls: results are
+// run-to-run identical.
 //
-// The work of a launch is a line: sequences, their key heads, the head's items of keys, every item as long as it takes to go over the rows.
-// It is cut into equal shares, one per workgroup, which takes the items that begin in its share.
+// The work of a launch is a line: sequences, their key heads, the head's items of 64 keys, every item as long as it takes to go over the rows.
+// It is cut into equal shares, for waves or workgroups, which take the items that begin in their share.
 
 constexpr int kWeighWaves = 4;
-constexpr int kWeighKeys = 64;      // of a wave
-constexpr int kItemFront = 4;       // what an item costs besides its rows, in tiles of 16
+constexpr int kWeighKeys = 64;      // of an item
+constexpr float kLog2e = 1.4426950408889634f;
+
+// over the four lane groups that share a key
+__device__ __forceinline__ float groups_sum(float x) {
+  LanePair p = swap16(x);
+  p = swap32(p.a + p.b);
+  return p.a + p.b;
+}
 
 struct WeighSeq {
   int first, n, len;
   int items;            // of a key head
   int cost;             // of an item
 };
-template <bool SPLIT>
+// FRONT: what an item costs besides its rows, in tiles of 16; TURNS: waves that share the rows
+template <int FRONT, int TURNS>
 __device__ __forceinline__ WeighSeq weigh_seq(const WeighArgs& a, int b) {
-  constexpr int kItem = SPLIT ? kWeighKeys : kWeighKeys * kWeighWaves;
   WeighSeq s = {0, 0, 0, 0, 1};
   if (b >= a.cache.n_seqs) return s;
   const int T = (int)a.n_tokens;
   s.first = std::clamp(a.offsets[b], 0, T);
   s.n = std::clamp(a.offsets[b + 1], s.first, T) - s.first;
   s.len = std::clamp(a.seq_lens[b], 0, a.cache.table_stride << a.cache.page_shift);
-  s.items = (s.len + kItem - 1) / kItem;
-  const int tiles = (s.n * a.group + 15) / 16;
-  s.cost = kItemFront + (SPLIT ? (tiles + kWeighWaves - 1) / kWeighWaves : tiles);
+  s.items = (s.len + kWeighKeys - 1) / kWeighKeys;
+  s.cost = FRONT + ((s.n * a.group + 15) / 16 + TURNS - 1) / TURNS;
   return s;
 }
-
-template <bool MX4, bool SPLIT, bool CAUSAL>
-__global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const WeighArgs a) {
-  constexpr int kItem = SPLIT ? kWeighKeys : kWeighKeys * kWeighWaves;
-  __shared__ float s_sum[kWeighWaves][kWeighKeys];
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
-  const PagedArgs& c = a.cache;
-  const int H = c.H_kv, H_q = H * a.group, n_seqs = c.n_seqs;
-
-  // the share's positions [at, end), and the sequence that it begins in
+// The items of a share: [item, stop) of all key heads of sequence b, then those of the next one
+struct WeighShare {
+  int64_t at, end, begin;      // on the line; where sequence b begins
+  int b;
+};
+template <int FRONT, int TURNS>
+__device__ __forceinline__ bool find_weigh_share(const WeighArgs& a, int id, int shares, int lane, WeighShare& r) {
   auto length = [&](int base) {
-    const WeighSeq s = weigh_seq<SPLIT>(a, base + lane);
-    return (int64_t)s.items * H * s.cost;
+    const WeighSeq s = weigh_seq<FRONT, TURNS>(a, base + lane);
+    return (int64_t)s.items * a.cache.H_kv * s.cost;
   };
   int64_t total = 0;
-  for (int base = 0; base < n_seqs; base += 64) total += length(base);
+  for (int base = 0; base < a.cache.n_seqs; base += 64) total += length(base);
   for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
   total = uniform64(total);
-  const int64_t each = total / gridDim.x, more = total - each * gridDim.x;
-  // (shares next to each other on one XCD: they read the same rows)
-  const int id = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
-  const int64_t at = each * id + std::min<int64_t>(id, more), end = at + each + (id < more ? 1 : 0);
-  if (at >= end) return;
-  int64_t begin = 0;       // of sequence b
-  int b = 0;
-  for (int base = 0; base < n_seqs; base += 64) {
+  const int64_t each = total / shares, more = total - each * shares;
+  r.at = each * id + std::min<int64_t>(id, more);
+  r.end = r.at + each + (id < more ? 1 : 0);
+  if (r.at >= r.end) return false;
+  r.begin = 0;
+  for (int base = 0; base < a.cache.n_seqs; base += 64) {
     int64_t scan = length(base);
     for (int d = 1; d < 64; d <<= 1) {
       const int64_t v = __shfl_up(scan, d);
       scan += lane >= d ? v : 0;
     }
-    const uint64_t in = __ballot(begin + scan > at);
-    if (in == 0) {
-      begin += uniform64(__shfl(scan, 63));
-      continue;
+    const uint64_t in = __ballot(r.begin + scan > r.at);
+    if (in != 0) {
+      const int l = __builtin_ctzll(in);
+      r.b = base + l;
+      r.begin += l ? uniform64(__shfl(scan, l - 1)) : 0;
+      return true;
     }
-    const int l = __builtin_ctzll(in);
-    b = base + l;
-    begin += l ? uniform64(__shfl(scan, l - 1)) : 0;
-    break;
+    r.begin += uniform64(__shfl(scan, 63));
   }
+  return false;
+}
+// r / group, as a product: exact for what rows there can be, 2^20 tokens of 64 heads
+__device__ __forceinline__ int token_of(const WeighArgs& a, int r) { return a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.group_magic); }
 
-  for (; b < n_seqs && begin < end; ++b) {
-    const WeighSeq s = weigh_seq<SPLIT>(a, b);
-    if (s.items == 0) continue;
-    int64_t item = at <= begin ? 0 : (at - begin + s.cost - 1) / s.cost;
-    const int64_t stop = std::min<int64_t>((int64_t)s.items * H, (end - begin + s.cost - 1) / s.cost);
-    begin += (int64_t)s.items * H * s.cost;
-    const int n_rows = s.n * a.group, tiles = (n_rows + 15) / 16, before = s.len - s.n;
-    const int32_t* table = c.table + (int64_t)b * c.table_stride;
-    for (; item < stop; ++item) {
-      const int h = uniform((int)(item / s.items)), j0 = uniform((int)(item - (int64_t)h * s.items) * kItem + (SPLIT ? 0 : wave * kWeighKeys));
-      if (!SPLIT && j0 >= s.len) continue;
-      // keys: 16 channels of a row in a lane, in two operands
-      bf16x8 k[4][2];
-      uint32_t there = 0;
-      {
-        u32x2 codes[4];
-        uint32_t exponents[4];
+// 64 keys of a head on their way: 16 channels of four rows in a lane
+template <bool MX4>
+struct KeysOnTheirWay {
+  u32x4 x[4][MX4 ? 1 : 2];      // codes in two words and the exponent in the third
+  uint32_t there;               // bit per 16 keys, whether they have a page
+  __device__ __forceinline__ void request(const WeighArgs& a, int b, int len, int h, int j0, int l16, int grp) {
+    const PagedArgs& c = a.cache;
+    const auto* table = (const __attribute__((address_space(4))) int32_t*)(c.table + (int64_t)b * c.table_stride);
+    there = 0;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int row = j0 + 16 * t, index = row >> c.page_shift;
-          const int page = row < s.len && index < c.table_stride ? table[index] : -1;
-          const bool ok = page >= 0 && page < c.n_pages;
-          there |= ok ? 1u << t : 0u;
-          const int64_t first = (((int64_t)(ok ? page : 0) * H + h) << c.page_shift) + (row & ((1 << c.page_shift) - 1));
-          const int n = ok ? std::min(s.len - row, 16) : 0;
-          if constexpr (MX4) {
-            codes[t] = __builtin_amdgcn_raw_buffer_load_b64(
-                __builtin_amdgcn_make_buffer_rsrc(c.k_pages + first * kMxRowBytes, 0, n * kMxRowBytes, kRawBufferWord3), l16 * kMxRowBytes + grp * 8, 0, 0);
-            exponents[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(
-                __builtin_amdgcn_make_buffer_rsrc(c.scales + first * kMxScaleBytes, 0, n * kMxScaleBytes, kRawBufferWord3),
-                l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
-          } else {
-            const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(c.k_pages + first * kRowBytes, 0, n * kRowBytes, kRawBufferWord3);
+    for (int t = 0; t < 4; ++t) {
+      const int row = j0 + 16 * t;
+      const int page = row < len ? table[row >> c.page_shift] : -1;     // (no length is beyond the table)
+      const bool ok = page >= 0 && page < c.n_pages;
+      there |= ok ? 1u << t : 0u;
+      const int64_t first = (((int64_t)(ok ? page : 0) * c.H_kv + h) << c.page_shift) + (row & ((1 << c.page_shift) - 1));
+      const int n = ok ? std::min(len - row, 16) : 0;
+      auto rows = [&](const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((char*)p + first * bytes, 0, n * bytes, kRawBufferWord3); };
+      if constexpr (MX4) {
+        const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(rows(c.k_pages, kMxRowBytes), l16 * kMxRowBytes + grp * 8, 0, 0);
+        const uint32_t e = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rows(c.scales, kMxScaleBytes), l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
+        x[t][0] = u32x4{codes[0], codes[1], e, 0};
+      } else {
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              k[t][e] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rows, l16 * kRowBytes + grp * 32 + e * 16, 0, 0));
-          }
-        }
-        if constexpr (MX4)
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) k[t][e] = __builtin_bit_cast(bf16x8, mx4_values(codes[t][e], __uint_as_float(exponents[t] << 23)));
+        for (int e = 0; e < 2; ++e) x[t][e] = __builtin_amdgcn_raw_buffer_load_b128(rows(c.k_pages, kRowBytes), l16 * kRowBytes + grp * 32 + e * 16, 0, 0);
       }
-      f32x4 sum[4] = {};
-      // rows in front of the first that sees one of the keys are left out
-      const int unseen = CAUSAL && j0 > before ? std::min((j0 - before) * a.group, n_rows) / 16 : 0;
-      for (int tile = unseen + (SPLIT ? wave : 0); tile < tiles; tile += SPLIT ? kWeighWaves : 1) {
-        const int r = std::min(16 * tile + l16, n_rows - 1);
-        const int i = r / a.group, head = h * a.group + (r - i * a.group);
-        const int64_t token = s.first + i;
-        const char* q = a.q.data + (token * a.q.token_stride + head * a.q.head_stride) * 2;
-        bf16x8 qf[2];
+    }
+  }
+  __device__ __forceinline__ void take(bf16x8 (&k)[4][2]) const {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) qf[e] = *(const bf16x8*)(q + grp * 32 + e * 16);
-        const float lse = a.lse[token * H_q + head];
-        // keys that the lane's row sees, from j0 on: none behind the last row, and where it saw no key at all
-        int sees = CAUSAL ? std::clamp(before + i + 1, 0, s.len) - j0 : s.len - j0;
-        if (16 * tile + l16 >= n_rows || lse == -__builtin_inff()) sees = 0;
-        const bool masked = __ballot(sees < std::min(kWeighKeys, s.len - j0)) != 0;
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          f32x4 x = mfma16(k[t][0], qf[0], f32x4{0.f, 0.f, 0.f, 0.f});
-          x = mfma16(k[t][1], qf[1], x);
+      for (int e = 0; e < 2; ++e)
+        k[t][e] = __builtin_bit_cast(bf16x8, MX4 ? mx4_values(x[t][0][e], __uint_as_float(x[t][0][2] << 23)) : x[t][e & (MX4 ? 0 : 1)]);
+  }
+};
+// 16 rows of a head: the A operands
+__device__ __forceinline__ void load_queries(bf16x8 (&q)[2], const WeighArgs& a, const WeighSeq& s, int h, int r, int n_rows, int grp) {
+  const int row = std::min(r, n_rows - 1), i = token_of(a, row);
+  const char* at = a.q.data + ((int64_t)(s.first + i) * a.q.token_stride + (h * a.group + row - i * a.group) * a.q.head_stride) * 2;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            // (the difference in one rounding: it is small where the weight counts, and then scaled)
-            float p = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -lse) * 1.4426950408889634f);
-            if (masked && 16 * t + 4 * grp + e >= sees) p = 0.f;
-            sum[t][e] += p;
-          }
+  for (int e = 0; e < 2; ++e) q[e] = *(const bf16x8*)(at + grp * 32 + e * 16);
+}
+// -lse of row r in base 2; minus infinity for a row that adds nothing: behind the last, or one that saw no key
+__device__ __forceinline__ float load_lse(const WeighArgs& a, const WeighSeq& s, int h, int r, int n_rows) {
+  const int row = std::min(r, n_rows - 1), i = token_of(a, row);
+  const float x = a.lse[(int64_t)(s.first + i) * (a.cache.H_kv * a.group) + h * a.group + row - i * a.group];
+  return r >= n_rows || x == -__builtin_inff() ? -__builtin_inff() : -x * kLog2e;
+}
+// What a tile of rows gives 64 keys.  `sees` (MASKED): keys that a row sees, from the first of the 64 on
+template <bool MASKED>
+__device__ __forceinline__ void add_tile(float (&sum)[4], const bf16x8 (&k)[4][2], const bf16x8 (&q)[2], const f32x4& lse, float scale_log2,
+                                         const int (&sees)[4], int l16) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    f32x4 x = mfma16(q[0], k[t][0], f32x4{0.f, 0.f, 0.f, 0.f});
+    x = mfma16(q[1], k[t][1], x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float p = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, lse[e]));
+      if (MASKED && 16 * t + l16 >= sees[e]) p = 0.f;
+      sum[t] += p;
+    }
+  }
+}
+// Sums of 64 keys into the weights: key `lane` of them to lane `lane`
+__device__ __forceinline__ float key_of_lane(const float (&sum)[4], int grp) {
+  float mine = 0.f;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const float x = groups_sum(sum[t]);
+    mine = grp == t ? x : mine;
+  }
+  return mine;
+}
+
+// Few rows: NT tiles of them stay in registers
+template <bool MX4, int NT, bool CAUSAL>
+__global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const WeighArgs a) {
+  constexpr int kFront = 4;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
+  const int H = a.cache.H_kv;
+  // (shares next to each other on one XCD: they read the same rows)
+  const int id = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)) * kWeighWaves + wave;
+  WeighShare share;
+  if (!find_weigh_share<kFront, 1>(a, id, (int)gridDim.x * kWeighWaves, lane, share)) return;
+  const float scale_log2 = a.scale * kLog2e;
+
+  struct Place {
+    WeighSeq s;
+    int64_t left;      // items of the sequence that the share still has, this one among them
+    int b, h, chunk;
+  };
+  // the first item at or behind sequence b that the share has
+  auto start = [&](Place& p) {
+    for (; p.b < a.cache.n_seqs && share.begin < share.end; ++p.b) {
+      p.s = weigh_seq<kFront, 1>(a, p.b);
+      const int64_t all = (int64_t)p.s.items * H, from = share.at <= share.begin ? 0 : (share.at - share.begin + p.s.cost - 1) / p.s.cost;
+      p.left = std::min<int64_t>(all, (share.end - share.begin + p.s.cost - 1) / p.s.cost) - from;
+      share.begin += all * p.s.cost;
+      if (p.left <= 0) continue;
+      p.h = uniform((int)(from / p.s.items));
+      p.chunk = uniform((int)(from - (int64_t)p.h * p.s.items));
+      return true;
+    }
+    return false;
+  };
+  auto next = [&](Place& p) {
+    if (--p.left == 0) {
+      ++p.b;
+      return start(p);
+    }
+    if (++p.chunk == p.s.items) p.chunk = 0, ++p.h;
+    return true;
+  };
+  auto weight_at = [&](const Place& p) { return a.weights + ((int64_t)p.b * H + p.h) * a.columns + p.chunk * kWeighKeys + lane; };
+  auto old_weight = [&](const Place& p) {
+    const int j = p.chunk * kWeighKeys + lane;
+    return j < p.s.len - p.s.n ? *weight_at(p) : 0.f;
+  };
+
+  Place p;
+  p.b = share.b;
+  if (!start(p)) return;
+  KeysOnTheirWay<MX4> keys;
+  keys.request(a, p.b, p.s.len, p.h, p.chunk * kWeighKeys, l16, grp);
+  float old = old_weight(p);
+  bf16x8 q[NT][2];
+  f32x4 lse[NT];
+  int of_b = -1, of_h = -1;      // whose rows q holds
+  while (true) {
+    const Place here = p;
+    const int j0 = here.chunk * kWeighKeys, n_rows = here.s.n * a.group, before = here.s.len - here.s.n;
+    const KeysOnTheirWay<MX4> now = keys;
+    const float was = old;
+    const bool more = next(p);
+    if (more) {
+      keys.request(a, p.b, p.s.len, p.h, p.chunk * kWeighKeys, l16, grp);
+      old = old_weight(p);
+    }
+    bf16x8 k[4][2];
+    now.take(k);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool stays = n_rows <= 16 * NT;
+    for (int r0 = 0; r0 < n_rows; r0 += 16 * NT) {
+      if (!stays || of_b != here.b || of_h != here.h) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          load_queries(q[i], a, here.s, here.h, r0 + 16 * i + l16, n_rows, grp);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) lse[i][e] = load_lse(a, here.s, here.h, r0 + 16 * i + 4 * grp + e, n_rows);
         }
+        of_b = here.b, of_h = here.h;
       }
-      // over the 16 lanes of a group: each is left with one key, 16 * (l16 >> 2) + 4 * grp + (l16 & 3)
-      float mine = 0.f;
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int i = 0; i < NT; ++i) {
+        if (i > 0 && r0 + 16 * i >= n_rows) break;
+        // (rows that add nothing are masked as well: 0 times a key that is not finite would be no number)
+        int sees[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float x = sum[t][e];
-          for (int d = 1; d < 16; d <<= 1) x += __shfl_xor(x, d);
-          if (l16 == 4 * t + e) mine = x;
+          const int t = token_of(a, r0 + 16 * i + 4 * grp + e);
+          sees[e] = lse[i][e] == -__builtin_inff() ? 0 : CAUSAL ? before + t + 1 - j0 : kWeighKeys;
         }
-      const int in = 16 * (l16 >> 2) + 4 * grp + (l16 & 3);
-      if constexpr (SPLIT) {
-        s_sum[wave][in] = mine;
-        __syncthreads();
-        mine = 0.f;
-#pragma unroll
-        for (int i = 0; i < kWeighWaves; ++i) mine += s_sum[i][in];
-        __syncthreads();
-        if (wave != 0) continue;
+        add_tile<true>(sum, k, q[i], lse[i], scale_log2, sees, l16);
       }
-      const int j = j0 + in;
-      if (j >= s.len) continue;
-      if (!((there >> (in >> 4)) & 1)) mine = 0.f;
-      float* w = a.weights + ((int64_t)b * H + h) * a.columns + j;
-      *w = j < before ? fmaf(a.decay, *w, mine) : mine;
+    }
+    float mine = key_of_lane(sum, grp);
+    if (!((now.there >> grp) & 1)) mine = 0.f;
+    if (j0 + lane < here.s.len) *weight_at(here) = j0 + lane < before ? fmaf(a.decay, was, mine) : mine;
+    if (!more) return;
+  }
+}
+
+// Many rows: the waves of a workgroup take tiles of them in turn.  Their lse lie in the LDS, a run of rows at a time.
+template <bool MX4, bool CAUSAL>
+__global__ __launch_bounds__(64 * kWeighWaves) void weigh_many_kernel(const WeighArgs a) {
+  constexpr int kFront = 4, kRun = 1024;
+  __shared__ __attribute__((aligned(16))) float s_lse[kRun];
+  __shared__ float s_sum[kWeighWaves][kWeighKeys];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
+  const int H = a.cache.H_kv;
+  const int id = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
+  WeighShare share;
+  if (!find_weigh_share<kFront, kWeighWaves>(a, id, gridDim.x, lane, share)) return;
+  const float scale_log2 = a.scale * kLog2e;
+  for (int b = share.b; b < a.cache.n_seqs && share.begin < share.end; ++b) {
+    const WeighSeq s = weigh_seq<kFront, kWeighWaves>(a, b);
+    int64_t item = share.at <= share.begin ? 0 : (share.at - share.begin + s.cost - 1) / s.cost;
+    const int64_t stop = std::min<int64_t>((int64_t)s.items * H, (share.end - share.begin + s.cost - 1) / s.cost);
+    share.begin += (int64_t)s.items * H * s.cost;
+    if (item >= stop) continue;
+    const int n_rows = s.n * a.group, before = s.len - s.n;
+    int h = uniform((int)(item / s.items)), chunk = uniform((int)(item - (int64_t)h * s.items));
+    int run_of_h = -1;
+    bool dead = false;      // whether a row of the run adds nothing
+    for (; item < stop; ++item) {
+      const int j0 = chunk * kWeighKeys;
+      KeysOnTheirWay<MX4> keys;
+      keys.request(a, b, s.len, h, j0, l16, grp);
+      float* weight = a.weights + ((int64_t)b * H + h) * a.columns + j0 + lane;
+      const float was = wave == 0 && j0 + lane < before ? *weight : 0.f;
+      bf16x8 k[4][2];
+      keys.take(k);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      // rows in front of the first that sees one of the keys are left out
+      const int unseen = CAUSAL && j0 > before ? std::min((j0 - before) * a.group, n_rows) / 16 : 0;
+      for (int run = unseen * 16 / kRun * kRun; run < n_rows; run += kRun) {
+        if (run_of_h != h || n_rows > kRun) {
+          __syncthreads();
+          bool none = false;
+          for (int i = threadIdx.x; i < kRun && run + i < (n_rows + 15) / 16 * 16; i += 64 * kWeighWaves) {
+            s_lse[i] = load_lse(a, s, h, run + i, n_rows);
+            none |= s_lse[i] == -__builtin_inff() && run + i < n_rows;
+          }
+          dead = __syncthreads_or(none) != 0;
+          run_of_h = h;
+        }
+        const int t1 = (std::min(run + kRun, n_rows) + 15) / 16;
+        int tile = std::max(run / 16, unseen) + wave;
+        if (tile >= t1) continue;
+        bf16x8 q[2];
+        load_queries(q, a, s, h, 16 * tile + l16, n_rows, grp);
+        for (; tile < t1; tile += kWeighWaves) {
+          bf16x8 ahead[2];
+          load_queries(ahead, a, s, h, 16 * (tile + kWeighWaves) + l16, n_rows, grp);
+          const f32x4 lse = *(const f32x4*)(s_lse + 16 * tile - run + 4 * grp);
+          int sees[4] = {0, 0, 0, 0};
+          if (dead || 16 * tile + 16 > n_rows || (CAUSAL && before + token_of(a, 16 * tile) + 1 < std::min(j0 + kWeighKeys, s.len))) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sees[e] = lse[e] == -__builtin_inff() ? 0 : CAUSAL ? before + token_of(a, 16 * tile + 4 * grp + e) + 1 - j0 : kWeighKeys;
+            add_tile<true>(sum, k, q, lse, scale_log2, sees, l16);
+          } else {
+            add_tile<false>(sum, k, q, lse, scale_log2, sees, l16);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) q[e] = ahead[e];
+        }
+      }
+      s_sum[wave][lane] = key_of_lane(sum, grp);
+      __syncthreads();
+      if (wave == 0 && j0 + lane < s.len) {
+        float mine = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWeighWaves; ++i) mine += s_sum[i][lane];
+        if (!((keys.there >> grp) & 1)) mine = 0.f;
+        *weight = j0 + lane < before ? fmaf(a.decay, was, mine) : mine;
+      }
+      __syncthreads();
+      if (++chunk == s.items) chunk = 0, ++h;
     }
   }
 }
@@ -424,12 +582,16 @@ __global__ __launch_bounds__(kMoveThreads) void evict_tail_kernel(const EvictArg
   }
 }
 
-template <bool MX4, bool SPLIT>
-void start_weigh(const WeighArgs& a, int shares, hipStream_t stream) {
-  if (a.causal)
-    hipLaunchKernelGGL((weigh_kernel<MX4, SPLIT, true>), dim3(shares), dim3(64 * kWeighWaves), 0, stream, a);
+template <bool MX4, bool CAUSAL>
+void start_weigh(const WeighArgs& a, hipStream_t stream) {
+  const int64_t mean = a.n_tokens * a.group / a.cache.n_seqs;
+  const dim3 block(64 * kWeighWaves);
+  if (mean > 64)
+    hipLaunchKernelGGL((weigh_many_kernel<MX4, CAUSAL>), dim3(1024), block, 0, stream, a);
+  else if (mean > 16)
+    hipLaunchKernelGGL((weigh_few_kernel<MX4, 4, CAUSAL>), dim3(1024), block, 0, stream, a);
   else
-    hipLaunchKernelGGL((weigh_kernel<MX4, SPLIT, false>), dim3(shares), dim3(64 * kWeighWaves), 0, stream, a);
+    hipLaunchKernelGGL((weigh_few_kernel<MX4, 1, CAUSAL>), dim3(1024), block, 0, stream, a);
 }
 template <bool MX4>
 void start_moves(const EvictArgs& a, hipStream_t stream) {
@@ -441,14 +603,13 @@ void start_moves(const EvictArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_cache_weigh(const WeighArgs& a, hipStream_t stream) {
-  const int64_t rows = a.n_tokens * a.group;
-  const bool split = rows > 64 * (int64_t)a.cache.n_seqs;
-  const int shares = 256 * 6;
+hipError_t launch_cache_weigh(const WeighArgs& args, hipStream_t stream) {
+  WeighArgs a = args;
+  a.group_magic = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
   if (a.cache.scales)
-    split ? start_weigh<true, true>(a, shares, stream) : start_weigh<true, false>(a, shares, stream);
+    a.causal ? start_weigh<true, true>(a, stream) : start_weigh<true, false>(a, stream);
   else
-    split ? start_weigh<false, true>(a, shares, stream) : start_weigh<false, false>(a, shares, stream);
+    a.causal ? start_weigh<false, true>(a, stream) : start_weigh<false, false>(a, stream);
   return hipGetLastError();
 }
 

@@ -276,6 +276,7 @@ struct WeighArgs {
   int32_t causal;
   float scale;
   float decay;
+  uint32_t group_magic;     // (set by the launch) ceil(2^32 / group), for more than 1
   float* weights;           // [n_seqs][H_kv][columns]
   int64_t columns;
 };
