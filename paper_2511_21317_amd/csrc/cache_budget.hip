@@ -18,6 +18,14 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
 }
 
+// floor(x / y) for 0 <= x, 0 < y, both below 2^52, for all lanes alike: the compiler's 64-bit division takes 130 instructions
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  int64_t q = (int64_t)((double)x / (double)y);
+  const int64_t r = x - q * y;
+  q += r < 0 ? -1 : (r >= y ? 1 : 0);
+  return uniform64(q);
+}
+
 // ---- weights ---------------------------------------------------------------------------------------------------
 //
 // The rows of a sequence and a key head are those of attention: r / group-th token, query head h * group + r % group.  S = Q K^T with
@@ -74,7 +82,7 @@ __device__ __forceinline__ bool find_weigh_share(const WeighArgs& a, int id, int
   for (int base = 0; base < a.cache.n_seqs; base += 64) total += length(base);
   for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
   total = uniform64(total);
-  const int64_t each = total / shares, more = total - each * shares;
+  const int64_t each = quotient(total, shares), more = total - each * shares;
   r.at = each * id + std::min<int64_t>(id, more);
   r.end = r.at + each + (id < more ? 1 : 0);
   if (r.at >= r.end) return false;
@@ -104,27 +112,52 @@ template <bool MX4>
 struct KeysOnTheirWay {
   u32x4 x[4][MX4 ? 1 : 2];      // codes in two words and the exponent in the third
   uint32_t there;               // bit per 16 keys, whether they have a page
-  __device__ __forceinline__ void request(const WeighArgs& a, int b, int len, int h, int j0, int l16, int grp) {
+  int pages[4];
+  // the pages of the keys from j0 on, asked for before the rows
+  __device__ __forceinline__ void look_up(const WeighArgs& a, int b, int len, int j0) {
+    const auto* table = (const __attribute__((address_space(4))) int32_t*)(a.cache.table + (int64_t)b * a.cache.table_stride);
+    const int shift = a.cache.page_shift;
+    pages[0] = j0 < len ? table[j0 >> shift] : -1;     // (no length is beyond the table)
+    if (shift < 6)
+#pragma unroll
+      for (int t = 1; t < 4; ++t) pages[t] = j0 + 16 * t < len ? table[(j0 + 16 * t) >> shift] : -1;
+  }
+  // rows [t0, t1) of 16 each, all on one page
+  template <int T0, int T1>
+  __device__ __forceinline__ void request_rows(const WeighArgs& a, int page, int row, int len, int h, int l16, int grp) {
     const PagedArgs& c = a.cache;
-    const auto* table = (const __attribute__((address_space(4))) int32_t*)(c.table + (int64_t)b * c.table_stride);
-    there = 0;
+    const bool ok = page >= 0 && page < c.n_pages;
+    there |= ok ? (1u << T1) - (1u << T0) : 0u;
+    const int64_t first = (((int64_t)(ok ? page : 0) * c.H_kv + h) << c.page_shift) + (row & ((1 << c.page_shift) - 1));
+    const int n = ok ? std::clamp(len - row, 0, 16 * (T1 - T0)) : 0;
+    auto rows = [&](const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((char*)p + first * bytes, 0, n * bytes, kRawBufferWord3); };
+    if constexpr (MX4) {
+      const __amdgpu_buffer_rsrc_t codes = rows(c.k_pages, kMxRowBytes), scales = rows(c.scales, kMxScaleBytes);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int row = j0 + 16 * t;
-      const int page = row < len ? table[row >> c.page_shift] : -1;     // (no length is beyond the table)
-      const bool ok = page >= 0 && page < c.n_pages;
-      there |= ok ? 1u << t : 0u;
-      const int64_t first = (((int64_t)(ok ? page : 0) * c.H_kv + h) << c.page_shift) + (row & ((1 << c.page_shift) - 1));
-      const int n = ok ? std::min(len - row, 16) : 0;
-      auto rows = [&](const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((char*)p + first * bytes, 0, n * bytes, kRawBufferWord3); };
-      if constexpr (MX4) {
-        const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(rows(c.k_pages, kMxRowBytes), l16 * kMxRowBytes + grp * 8, 0, 0);
-        const uint32_t e = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rows(c.scales, kMxScaleBytes), l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
-        x[t][0] = u32x4{codes[0], codes[1], e, 0};
-      } else {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) x[t][e] = __builtin_amdgcn_raw_buffer_load_b128(rows(c.k_pages, kRowBytes), l16 * kRowBytes + grp * 32 + e * 16, 0, 0);
+      for (int t = T0; t < T1; ++t) {
+        const int in = l16 + 16 * (t - T0);
+        const u32x2 k = __builtin_amdgcn_raw_buffer_load_b64(codes, in * kMxRowBytes + grp * 8, 0, 0);
+        x[t][0][0] = k[0];
+        x[t][0][1] = k[1];
+        x[t][0][2] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(scales, in * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
       }
+    } else {
+      const __amdgpu_buffer_rsrc_t keys = rows(c.k_pages, kRowBytes);
+#pragma unroll
+      for (int t = T0; t < T1; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[t][e] = __builtin_amdgcn_raw_buffer_load_b128(keys, (l16 + 16 * (t - T0)) * kRowBytes + grp * 32 + e * 16, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void request(const WeighArgs& a, int len, int h, int j0, int l16, int grp) {
+    there = 0;
+    if (a.cache.page_shift >= 6) {      // (items begin at multiples of 64)
+      request_rows<0, 4>(a, pages[0], j0, len, h, l16, grp);
+    } else {
+      request_rows<0, 1>(a, pages[0], j0, len, h, l16, grp);
+      request_rows<1, 2>(a, pages[1], j0 + 16, len, h, l16, grp);
+      request_rows<2, 3>(a, pages[2], j0 + 32, len, h, l16, grp);
+      request_rows<3, 4>(a, pages[3], j0 + 48, len, h, l16, grp);
     }
   }
   __device__ __forceinline__ void take(bf16x8 (&k)[4][2]) const {
@@ -142,26 +175,59 @@ __device__ __forceinline__ void load_queries(bf16x8 (&q)[2], const WeighArgs& a,
 #pragma unroll
   for (int e = 0; e < 2; ++e) q[e] = *(const bf16x8*)(at + grp * 32 + e * 16);
 }
+// The same of every 64th row from r on, as a walk: an address takes products that are four times as long as sums
+struct QueryWalk {
+  const char* head;          // row 0 of the head, the lane's channels
+  int64_t at, last;          // bytes from there: of the row, and of the last one
+  int64_t step, wrap;        // 64 rows on; a token on and the group's heads back
+  int r, in, n_rows, group, rest;
+  __device__ __forceinline__ QueryWalk(const WeighArgs& a, const WeighSeq& s, int h, int first, int n, int grp) {
+    const int64_t ts = a.q.token_stride * 2, hs = a.q.head_stride * 2;
+    const int i = token_of(a, first), j = token_of(a, n - 1), k = token_of(a, 64);
+    group = a.group, n_rows = n, r = first;
+    head = a.q.data + (int64_t)s.first * ts + (int64_t)h * group * hs + grp * 32;
+    in = first - i * group;
+    at = i * ts + in * hs;
+    last = j * ts + (n - 1 - j * group) * hs;
+    rest = 64 - k * group;
+    step = k * ts + rest * hs;
+    wrap = ts - group * hs;
+  }
+  // the row's operands (behind the last row: of the last one), and on to the next
+  __device__ __forceinline__ void take(bf16x8 (&q)[2]) {
+    const char* row = head + (r < n_rows ? at : last);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) q[e] = *(const bf16x8*)(row + e * 16);
+    r += 64;
+    in += rest;
+    at += step;
+    if (in >= group) in -= group, at += wrap;
+  }
+};
 // -lse of row r in base 2; minus infinity for a row that adds nothing: behind the last, or one that saw no key
 __device__ __forceinline__ float load_lse(const WeighArgs& a, const WeighSeq& s, int h, int r, int n_rows) {
   const int row = std::min(r, n_rows - 1), i = token_of(a, row);
   const float x = a.lse[(int64_t)(s.first + i) * (a.cache.H_kv * a.group) + h * a.group + row - i * a.group];
   return r >= n_rows || x == -__builtin_inff() ? -__builtin_inff() : -x * kLog2e;
 }
-// What a tile of rows gives 64 keys.  `sees` (MASKED): keys that a row sees, from the first of the 64 on
-template <bool MASKED>
-__device__ __forceinline__ void add_tile(float (&sum)[4], const bf16x8 (&k)[4][2], const bf16x8 (&q)[2], const f32x4& lse, float scale_log2,
-                                         const int (&sees)[4], int l16) {
+// A tile of rows against 64 keys: the scores, and what they give.  `sees` (MASKED): keys that a row sees, from the first of the 64 on
+__device__ __forceinline__ void scores_of(f32x4 (&x)[4], const bf16x8 (&k)[4][2], const bf16x8 (&q)[2]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) x[t] = mfma16(q[0], k[t][0], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+  for (int t = 0; t < 4; ++t) x[t] = mfma16(q[1], k[t][1], x[t]);
+}
+template <bool MASKED, bool CAUSAL>
+__device__ __forceinline__ void add_tile(float (&sum)[4], const f32x4 (&x)[4], const f32x4& lse, float scale_log2, const int (&sees)[4], int l16) {
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    f32x4 x = mfma16(q[0], k[t][0], f32x4{0.f, 0.f, 0.f, 0.f});
-    x = mfma16(q[1], k[t][1], x);
+    float p[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float p = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, lse[e]));
-      if (MASKED && 16 * t + l16 >= sees[e]) p = 0.f;
-      sum[t] += p;
+      p[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], scale_log2, lse[e]));
+      if (MASKED && (CAUSAL ? 16 * t + l16 >= sees[e] : sees[e] == 0)) p[e] = 0.f;
     }
+    sum[t] += (p[0] + p[1]) + (p[2] + p[3]);
   }
 }
 // Sums of 64 keys into the weights: key `lane` of them to lane `lane`
@@ -189,19 +255,20 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const Weigh
 
   struct Place {
     WeighSeq s;
+    int64_t begin;     // of the sequence behind b on the line
     int64_t left;      // items of the sequence that the share still has, this one among them
     int b, h, chunk;
   };
   // the first item at or behind sequence b that the share has
   auto start = [&](Place& p) {
-    for (; p.b < a.cache.n_seqs && share.begin < share.end; ++p.b) {
+    for (; p.b < a.cache.n_seqs && p.begin < share.end; ++p.b) {
       p.s = weigh_seq<kFront, 1>(a, p.b);
-      const int64_t all = (int64_t)p.s.items * H, from = share.at <= share.begin ? 0 : (share.at - share.begin + p.s.cost - 1) / p.s.cost;
-      p.left = std::min<int64_t>(all, (share.end - share.begin + p.s.cost - 1) / p.s.cost) - from;
-      share.begin += all * p.s.cost;
+      const int64_t all = (int64_t)p.s.items * H, from = share.at <= p.begin ? 0 : quotient(share.at - p.begin + p.s.cost - 1, p.s.cost);
+      p.left = std::min<int64_t>(all, quotient(share.end - p.begin + p.s.cost - 1, p.s.cost)) - from;
+      p.begin += all * p.s.cost;
       if (p.left <= 0) continue;
-      p.h = uniform((int)(from / p.s.items));
-      p.chunk = uniform((int)(from - (int64_t)p.h * p.s.items));
+      p.h = (int)quotient(from, p.s.items);
+      p.chunk = (int)(from - (int64_t)p.h * p.s.items);
       return true;
     }
     return false;
@@ -215,32 +282,30 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const Weigh
     return true;
   };
   auto weight_at = [&](const Place& p) { return a.weights + ((int64_t)p.b * H + p.h) * a.columns + p.chunk * kWeighKeys + lane; };
-  auto old_weight = [&](const Place& p) {
-    const int j = p.chunk * kWeighKeys + lane;
-    return j < p.s.len - p.s.n ? *weight_at(p) : 0.f;
-  };
 
-  Place p;
-  p.b = share.b;
-  if (!start(p)) return;
-  KeysOnTheirWay<MX4> keys;
-  keys.request(a, p.b, p.s.len, p.h, p.chunk * kWeighKeys, l16, grp);
-  float old = old_weight(p);
+  KeysOnTheirWay<MX4> keys;      // of the item ahead
+  float old;
+  Place here, ahead;
+  ahead.b = share.b, ahead.begin = share.begin;
+  bool more = start(ahead);
   bf16x8 q[NT][2];
   f32x4 lse[NT];
   int of_b = -1, of_h = -1;      // whose rows q holds
-  while (true) {
-    const Place here = p;
+  auto request = [&] {
+    keys.look_up(a, ahead.b, ahead.s.len, ahead.chunk * kWeighKeys);
+    keys.request(a, ahead.s.len, ahead.h, ahead.chunk * kWeighKeys, l16, grp);
+    old = ahead.chunk * kWeighKeys + lane < ahead.s.len - ahead.s.n ? *weight_at(ahead) : 0.f;
+  };
+  if (more) request();
+  while (more) {
+    here = ahead;
     const int j0 = here.chunk * kWeighKeys, n_rows = here.s.n * a.group, before = here.s.len - here.s.n;
-    const KeysOnTheirWay<MX4> now = keys;
     const float was = old;
-    const bool more = next(p);
-    if (more) {
-      keys.request(a, p.b, p.s.len, p.h, p.chunk * kWeighKeys, l16, grp);
-      old = old_weight(p);
-    }
+    const uint32_t there = keys.there;
     bf16x8 k[4][2];
-    now.take(k);
+    keys.take(k);
+    more = next(ahead);
+    if (more) request();
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     const bool stays = n_rows <= 16 * NT;
     for (int r0 = 0; r0 < n_rows; r0 += 16 * NT) {
@@ -263,46 +328,53 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const Weigh
           const int t = token_of(a, r0 + 16 * i + 4 * grp + e);
           sees[e] = lse[i][e] == -__builtin_inff() ? 0 : CAUSAL ? before + t + 1 - j0 : kWeighKeys;
         }
-        add_tile<true>(sum, k, q[i], lse[i], scale_log2, sees, l16);
+        f32x4 x[4];
+        scores_of(x, k, q[i]);
+        add_tile<true, CAUSAL>(sum, x, lse[i], scale_log2, sees, l16);
       }
     }
     float mine = key_of_lane(sum, grp);
-    if (!((now.there >> grp) & 1)) mine = 0.f;
+    if (!((there >> grp) & 1)) mine = 0.f;
     if (j0 + lane < here.s.len) *weight_at(here) = j0 + lane < before ? fmaf(a.decay, was, mine) : mine;
-    if (!more) return;
   }
 }
 
 // Many rows: the waves of a workgroup take tiles of them in turn.  Their lse lie in the LDS, a run of rows at a time.
 template <bool MX4, bool CAUSAL>
-__global__ __launch_bounds__(64 * kWeighWaves) void weigh_many_kernel(const WeighArgs a) {
-  constexpr int kFront = 4, kRun = 1024;
+__global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_eu(4, 4))) void weigh_many_kernel(const WeighArgs a) {
+  constexpr int kFront = 4, kRun = 4096;
+  static_assert(16 * kWeighWaves == 64, "a wave's tiles are 64 rows apart");
   __shared__ __attribute__((aligned(16))) float s_lse[kRun];
   __shared__ float s_sum[kWeighWaves][kWeighKeys];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
   const int H = a.cache.H_kv;
-  const int id = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
+  const int id = blockIdx.x;
   WeighShare share;
   if (!find_weigh_share<kFront, kWeighWaves>(a, id, gridDim.x, lane, share)) return;
   const float scale_log2 = a.scale * kLog2e;
   for (int b = share.b; b < a.cache.n_seqs && share.begin < share.end; ++b) {
     const WeighSeq s = weigh_seq<kFront, kWeighWaves>(a, b);
-    int64_t item = share.at <= share.begin ? 0 : (share.at - share.begin + s.cost - 1) / s.cost;
-    const int64_t stop = std::min<int64_t>((int64_t)s.items * H, (share.end - share.begin + s.cost - 1) / s.cost);
+    int64_t item = share.at <= share.begin ? 0 : quotient(share.at - share.begin + s.cost - 1, s.cost);
+    const int64_t stop = std::min<int64_t>((int64_t)s.items * H, quotient(share.end - share.begin + s.cost - 1, s.cost));
     share.begin += (int64_t)s.items * H * s.cost;
     if (item >= stop) continue;
     const int n_rows = s.n * a.group, before = s.len - s.n;
-    int h = uniform((int)(item / s.items)), chunk = uniform((int)(item - (int64_t)h * s.items));
+    int h = (int)quotient(item, s.items), chunk = (int)(item - (int64_t)h * s.items);
     int run_of_h = -1;
     bool dead = false;      // whether a row of the run adds nothing
+    KeysOnTheirWay<MX4> keys;
+    keys.look_up(a, b, s.len, chunk * kWeighKeys);
+    keys.request(a, s.len, h, chunk * kWeighKeys, l16, grp);
     for (; item < stop; ++item) {
       const int j0 = chunk * kWeighKeys;
-      KeysOnTheirWay<MX4> keys;
-      keys.request(a, b, s.len, h, j0, l16, grp);
       float* weight = a.weights + ((int64_t)b * H + h) * a.columns + j0 + lane;
       const float was = wave == 0 && j0 + lane < before ? *weight : 0.f;
       bf16x8 k[4][2];
       keys.take(k);
+      const uint32_t there = keys.there;
+      int next_chunk = chunk + 1, next_h = h;
+      if (next_chunk == s.items) next_chunk = 0, ++next_h;
+      if (item + 1 < stop) keys.look_up(a, b, s.len, next_chunk * kWeighKeys);
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
       // rows in front of the first that sees one of the keys are left out
       const int unseen = CAUSAL && j0 > before ? std::min((j0 - before) * a.group, n_rows) / 16 : 0;
@@ -310,9 +382,17 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_many_kernel(const Weig
         if (run_of_h != h || n_rows > kRun) {
           __syncthreads();
           bool none = false;
-          for (int i = threadIdx.x; i < kRun && run + i < (n_rows + 15) / 16 * 16; i += 64 * kWeighWaves) {
-            s_lse[i] = load_lse(a, s, h, run + i, n_rows);
-            none |= s_lse[i] == -__builtin_inff() && run + i < n_rows;
+          const int all = std::min(kRun, (n_rows - run + 15) / 16 * 16);
+          for (int i = threadIdx.x; i < all; i += 4 * 64 * kWeighWaves) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = load_lse(a, s, h, run + i + e * 64 * kWeighWaves, n_rows);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int at = i + e * 64 * kWeighWaves;
+              if (at < all) s_lse[at] = x[e];
+              none |= x[e] == -__builtin_inff() && run + at < n_rows;
+            }
           }
           dead = __syncthreads_or(none) != 0;
           run_of_h = h;
@@ -320,43 +400,56 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_many_kernel(const Weig
         const int t1 = (std::min(run + kRun, n_rows) + 15) / 16;
         int tile = std::max(run / 16, unseen) + wave;
         if (tile >= t1) continue;
-        bf16x8 q[2];
-        load_queries(q, a, s, h, 16 * tile + l16, n_rows, grp);
-        for (; tile < t1; tile += kWeighWaves) {
-          bf16x8 ahead[2];
-          load_queries(ahead, a, s, h, 16 * (tile + kWeighWaves) + l16, n_rows, grp);
+        QueryWalk walk(a, s, h, 16 * tile + l16, n_rows, grp);
+        bf16x8 q[2][2];
+        f32x4 x[2][4];
+        // The scores of a tile come while those of the one before are in work, its rows two tiles ahead.  (Behind the last tile: rows that are
+        // there, for nothing.)
+        auto step = [&](int now, int then) {
           const f32x4 lse = *(const f32x4*)(s_lse + 16 * tile - run + 4 * grp);
+          scores_of(x[then], k, q[then]);
+          walk.take(q[now]);
           int sees[4] = {0, 0, 0, 0};
           if (dead || 16 * tile + 16 > n_rows || (CAUSAL && before + token_of(a, 16 * tile) + 1 < std::min(j0 + kWeighKeys, s.len))) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               sees[e] = lse[e] == -__builtin_inff() ? 0 : CAUSAL ? before + token_of(a, 16 * tile + 4 * grp + e) + 1 - j0 : kWeighKeys;
-            add_tile<true>(sum, k, q, lse, scale_log2, sees, l16);
+            add_tile<true, CAUSAL>(sum, x[now], lse, scale_log2, sees, l16);
           } else {
-            add_tile<false>(sum, k, q, lse, scale_log2, sees, l16);
+            add_tile<false, CAUSAL>(sum, x[now], lse, scale_log2, sees, l16);
           }
-#pragma unroll
-          for (int e = 0; e < 2; ++e) q[e] = ahead[e];
+          tile += kWeighWaves;
+        };
+        walk.take(q[0]);
+        walk.take(q[1]);
+        scores_of(x[0], k, q[0]);
+        while (true) {
+          step(0, 1);
+          if (tile >= t1) break;
+          step(1, 0);
+          if (tile >= t1) break;
         }
       }
+      if (item + 1 < stop) keys.request(a, s.len, next_h, next_chunk * kWeighKeys, l16, grp);
       s_sum[wave][lane] = key_of_lane(sum, grp);
       __syncthreads();
       if (wave == 0 && j0 + lane < s.len) {
         float mine = 0.f;
 #pragma unroll
         for (int i = 0; i < kWeighWaves; ++i) mine += s_sum[i][lane];
-        if (!((keys.there >> grp) & 1)) mine = 0.f;
+        if (!((there >> grp) & 1)) mine = 0.f;
         *weight = j0 + lane < before ? fmaf(a.decay, was, mine) : mine;
       }
       __syncthreads();
-      if (++chunk == s.items) chunk = 0, ++h;
+      chunk = next_chunk, h = next_h;
     }
   }
 }
 
 // ---- eviction --------------------------------------------------------------------------------------------------
 
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
+constexpr int kEvictRuns = 32;       // runs of 64 positions that a wave of the selection holds in the LDS
+constexpr int kEvictBins = 2048, kEvictCopies = 2;
 
 // In the order of the weights: NaN is below everything, zeros are alike
 __device__ __forceinline__ uint32_t order_of(float w) {
@@ -364,222 +457,305 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return w != w ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// Moves of a key head of a sequence: how many, where to, where from
+// Moves of a key head of a sequence, in ascending order: how many (-1: none, and nothing else to do), how many of them from in front of row
+// `keep`, where to, where from
 struct Moves {
   int32_t* n;
+  int32_t* near;
   int32_t* to;
   int32_t* from;
 };
 __device__ __forceinline__ Moves moves_of(const EvictArgs& a, int bh) {
-  int32_t* n = (int32_t*)a.workspace + (int64_t)bh * (1 + 2 * (int64_t)a.keep);
-  return {n, n + 1, n + 1 + a.keep};
+  int32_t* n = (int32_t*)a.workspace + (int64_t)bh * (2 + 2 * (int64_t)a.keep);
+  return {n, n + 1, n + 2, n + 2 + a.keep};
 }
 __device__ __forceinline__ int evict_length(const EvictArgs& a, int b) {
   return std::clamp(a.seq_lens[b], 0, a.cache.table_stride << a.cache.page_shift);
 }
-__device__ __forceinline__ int64_t cache_row(const PagedArgs& c, int b, int h, int row) {
-  const int64_t page = c.table[(int64_t)b * c.table_stride + (row >> c.page_shift)];
-  return ((page * c.H_kv + h) << c.page_shift) + (row & ((1 << c.page_shift) - 1));
+
+// Sum over the lanes up to this one, as data-parallel moves: within rows of 16, then what the rows before have
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);      // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // row_bcast:15 into rows 1 and 3, :31 into rows 2 and 3
+  return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
 }
 
-// What stays of a key head of a sequence, and what has to move: one workgroup.  The threshold comes from four passes over 8 bits each of the weights' order,
-// every wave of the workgroup with a part of the positions and counts of its own, so that the places of those alike and of the moves are
-// sums over the waves before.
-__global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const EvictArgs a) {
-  __shared__ uint32_t s_hist[kEvictWaves][256];
-  __shared__ uint32_t s_count[3][kEvictWaves];
-  __shared__ uint32_t s_prefix, s_need, s_hole;
+// What stays of a key head of a sequence, and what has to move: one workgroup, whose waves have a part of the positions each and its weights, as
+// whole numbers in their order, in the LDS.  The threshold comes from counts over 11, 11 and 10 bits of them, as far as it takes until a bin stays or goes
+// as a whole (two copies of the bins, by lane: most weights are within a few powers of two of each other, and counts of one bin wait for each other); the
+// places of those alike with it and of the moves are sums over the waves before.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictArgs a) {
+  constexpr int kWaves = THREADS / 64, kBinsEach = kEvictBins / THREADS;
+  __shared__ uint32_t s_key[kEvictRuns * THREADS];
+  __shared__ __attribute__((aligned(16))) uint32_t s_bins[kEvictBins * kEvictCopies];
+  __shared__ __attribute__((aligned(16))) uint32_t s_count[5][kWaves];
+  __shared__ uint32_t s_prefix, s_need, s_alike;
   const int b = blockIdx.x / a.cache.H_kv, h = blockIdx.x - b * a.cache.H_kv;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int len = evict_length(a, b);
   const Moves mv = moves_of(a, blockIdx.x);
   int32_t* kept = a.kept ? a.kept + (int64_t)blockIdx.x * a.keep : nullptr;
-  if (threadIdx.x == 0) s_hole = 0;
-  __syncthreads();
+  const float* w = a.weights + (int64_t)blockIdx.x * a.columns;
+  const bool over = len > a.keep;
+  const int from = a.first, to = len - a.last, gap = a.keep - a.last;
+  // a wave's part, in runs of 64 positions
+  const int runs = over ? (to - from + THREADS - 1) / THREADS : 0;
+  const int p0 = std::min(from + wave * runs * 64, to), p1 = std::min(p0 + runs * 64, to);
+  uint32_t* keys = s_key + wave * kEvictRuns * 64 + lane;
+#pragma unroll 8
+  for (int i = 0; i < std::min(runs, kEvictRuns); ++i) keys[64 * i] = order_of(w[std::min(p0 + 64 * i + lane, len - 1)]);
   const int32_t* table = a.cache.table + (int64_t)b * a.cache.table_stride;
-  for (int i = threadIdx.x; i < (len + (1 << a.cache.page_shift) - 1) >> a.cache.page_shift; i += kEvictThreads)
-    if (table[i] < 0 || table[i] >= a.cache.n_pages) s_hole = 1;
-  __syncthreads();
-  const bool hole = s_hole != 0;
-  if (hole || len <= a.keep) {
+  bool hole = false;
+  for (int i = threadIdx.x; i < (len + (1 << a.cache.page_shift) - 1) >> a.cache.page_shift; i += THREADS)
+    hole |= table[i] < 0 || table[i] >= a.cache.n_pages;
+  hole = __syncthreads_or(hole) != 0;
+  if (hole || !over) {
     if (threadIdx.x == 0) {
       *mv.n = -1;
       if (h == 0) a.new_lens[b] = len;
     }
     if (kept)
-      for (int d = threadIdx.x; d < a.keep; d += kEvictThreads) kept[d] = !hole && d < len ? d : -1;
+      for (int d = threadIdx.x; d < a.keep; d += THREADS) kept[d] = !hole && d < len ? d : -1;
     return;
   }
-  const float* w = a.weights + (int64_t)blockIdx.x * a.columns;
-  const int from = a.first, to = len - a.last, gap = a.keep - a.last;
-  // a wave's part, in runs of 64 positions
-  const int part = ((to - from + kEvictThreads - 1) / kEvictThreads) * 64;
-  const int p0 = std::min(from + wave * part, to), p1 = std::min(p0 + part, to);
+  // f(position of the run, key of the lane) for the runs of the wave.  (Loops: straight code that is run once is fetched first, 3 us for a thousand
+  // instructions.)
+  auto each_run = [&](auto f) {
+    const int held = std::min(runs, kEvictRuns);
+    uint32_t next = keys[0];
+    for (int i = 0; i < held; ++i) {
+      const uint32_t x = next;
+      next = keys[64 * std::min(i + 1, held - 1)];
+      f(p0 + 64 * i, x);
+    }
+    for (int i = kEvictRuns; i < runs; ++i) f(p0 + 64 * i, order_of(w[std::min(p0 + 64 * i + lane, len - 1)]));
+  };
+  // Sum over the waves before this one, and over all
+  struct Sums {
+    uint32_t before, all;
+  };
+  auto sums_of = [&](int which) {
+    Sums r = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kWaves; i += 4) {
+      const u32x4 x = *(const u32x4*)&s_count[which][i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t n = (uint32_t)uniform((int)x[e]);
+        r.before += i + e < wave ? n : 0;
+        r.all += n;
+      }
+    }
+    return r;
+  };
 
-  uint32_t need = (uint32_t)(a.keep - a.first - a.last), prefix = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < kEvictWaves * 256; i += kEvictThreads) (&s_hist[0][0])[i] = 0;
-    __syncthreads();
-    for (int p = p0 + lane; p < p1; p += 64) {
-      const uint32_t x = order_of(w[p]);
-      if (shift == 24 || (x >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[wave][(x >> shift) & 255], 1u);
-    }
-    __syncthreads();
-    if (threadIdx.x < 256) {
-      uint32_t n = 0;
-      for (int i = 0; i < kEvictWaves; ++i) n += s_hist[i][threadIdx.x];
-      s_hist[0][threadIdx.x] = n;
-    }
-    __syncthreads();
-    if (wave == 0) {
-      // values from above: the bin in which the needed-th lies
-      uint32_t n[4], sum = 0;
+  const bool any = gap > a.first;
+  uint32_t need = (uint32_t)(gap - a.first), prefix = 0, alike_in_all = 0;
+  for (int pass = 0; pass < 3 && any; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, top = pass == 1 ? 21 : 10;      // bits from `top` on are known
+    const uint32_t mask = pass == 2 ? 1023 : 2047;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum += n[i] = s_hist[0][255 - (4 * lane + i)];
-      uint32_t scan = sum;
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t v = __shfl_up(scan, d);
-        scan += lane >= d ? v : 0;
-      }
-      uint32_t above = scan - sum;
+    for (int i = 0; i < kEvictBins * kEvictCopies / THREADS / 4; ++i) *(u32x4*)&s_bins[(i * THREADS + threadIdx.x) * 4] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    each_run([&](int p, uint32_t x) {
+      if (p + lane < p1 && (pass == 0 || (x >> top) == (prefix >> top))) atomicAdd(&s_bins[((x >> shift) & mask) * kEvictCopies + (lane & 1)], 1u);
+    });
+    __syncthreads();
+    // bins from above: the one in which the needed-th lies
+    uint32_t n[kBinsEach], sum = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (above < need && above + n[i] >= need) {
-          s_prefix = prefix | (uint32_t)(255 - (4 * lane + i)) << shift;
-          s_need = need - above;
-        }
-        above += n[i];
-      }
+    for (int i = 0; i < kBinsEach; ++i) {
+      const u32x2 x = *(const u32x2*)&s_bins[(kEvictBins - 1 - i - kBinsEach * (int)threadIdx.x) * kEvictCopies];
+      n[i] = x[0] + x[1];
+      sum += n[i];
     }
-    if (need == 0) break;
+    const uint32_t scan = wave_scan(sum);
+    if (lane == 63) s_count[0][wave] = scan;
+    __syncthreads();
+    uint32_t above = sums_of(0).before + scan - sum;
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) {
+      if (above < need && above + n[i] >= need) {
+        s_prefix = prefix | (uint32_t)(kEvictBins - 1 - i - kBinsEach * (int)threadIdx.x) << shift;
+        s_need = need - above;
+        s_alike = n[i];
+      }
+      above += n[i];
+    }
     __syncthreads();
     prefix = s_prefix;
     need = s_need;
-    __syncthreads();
+    alike_in_all = s_alike;
+    if (alike_in_all == need) break;
   }
-  // stays: above the threshold, or among the first `need` that are alike with it
-  const bool any = a.keep - a.first - a.last > 0;
-  auto ballot_of = [&](int p, uint64_t& above, uint64_t& alike) {
-    const uint32_t x = p < p1 ? order_of(w[p]) : 0u;
-    above = __ballot(p < p1 && any && x > prefix);
-    alike = __ballot(p < p1 && any && x == prefix);
-  };
-  auto before_me = [&](int which, uint32_t mine) {
-    if (lane == 0) s_count[which][wave] = mine;
+  // Stays: above the threshold, or among the first `need` that are alike with it (or all of them: all whose known bits are).  Bit per position of a run.
+  const bool all_alike = alike_in_all == need;
+  uint32_t rank = 0;      // of those alike, in front of the wave
+  if (any && !all_alike) {
+    uint32_t here = 0;
+    each_run([&](int p, uint32_t x) { here += p + lane < p1 && x == prefix ? 1 : 0; });
+    here = wave_scan(here);
+    if (lane == 63) s_count[1][wave] = here;
     __syncthreads();
-    uint32_t n = 0;
-    for (int i = 0; i < wave; ++i) n += s_count[which][i];
-    return (uint32_t)uniform((int)n);
-  };
-  uint32_t alike_here = 0;
-  for (int p = p0; p < p1; p += 64) {
-    uint64_t above, alike;
-    ballot_of(p + lane, above, alike);
-    alike_here += __popcll(alike);
+    rank = sums_of(1).before;
   }
-  const uint32_t alike_before = before_me(0, alike_here);
-  auto stays_of = [&](int p, uint32_t& rank) {      // of a run; rank: of the first that is alike
-    uint64_t above, alike;
-    ballot_of(p + lane, above, alike);
-    const uint32_t mine = rank + __popcll(alike & ((1ull << lane) - 1));
+  const uint32_t alike_before = rank;
+  auto lanes_before = [](uint64_t set) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0)); };
+  // (of the lane; by all lanes of a wave)
+  auto stays_of = [&](int p, uint32_t x) {
+    const bool in = p + lane < p1 && any;
+    if (all_alike) return in && x >= prefix;
+    const uint64_t alike = __ballot(in && x == prefix);
+    const bool stays = in && (x > prefix || (x == prefix && rank + lanes_before(alike) < need));
     rank += __popcll(alike);
-    return above | __ballot(((alike >> lane) & 1) && mine < need);
+    return stays;
   };
-  uint32_t holes = 0, movers = 0, rank = alike_before;
-  for (int p = p0; p < p1; p += 64) {
-    const uint64_t stays = stays_of(p, rank), below = __ballot(p + lane < gap), in = __ballot(p + lane < p1);
-    holes += __popcll(~stays & below & in);
-    movers += __popcll(stays & ~below);
-  }
-  uint32_t hole_at = before_me(1, holes), mover_at = before_me(2, movers);
+  // Counts of the lane: what stays, in front of the gap's end, and between it and row `keep`
+  uint32_t stay = 0, stay_below = 0, stay_near = 0;
+  each_run([&](int p, uint32_t x) {
+    const uint32_t one = stays_of(p, x) ? 1 : 0;
+    stay += one;
+    stay_below += p + lane < gap ? one : 0;
+    stay_near += p + lane < a.keep ? one : 0;
+  });
+  stay = wave_scan(stay), stay_below = wave_scan(stay_below), stay_near = wave_scan(stay_near);
+  if (lane == 63) s_count[2][wave] = std::clamp(gap - p0, 0, p1 - p0) - stay_below, s_count[3][wave] = stay - stay_below, s_count[4][wave] = stay_near - stay_below;
+  __syncthreads();
+  const Sums frees = sums_of(2);
+  uint32_t free_at = frees.before, mover_at = sums_of(3).before;
   rank = alike_before;
-  for (int p = p0; p < p1; p += 64) {
-    const uint64_t stays = stays_of(p, rank), below = __ballot(p + lane < gap), in = __ballot(p + lane < p1);
-    const uint64_t h_set = ~stays & below & in, m_set = stays & ~below, me = 1ull << lane, lower = me - 1;
-    if (h_set & me) mv.to[hole_at + __popcll(h_set & lower)] = p + lane;
-    if (m_set & me) mv.from[mover_at + __popcll(m_set & lower)] = p + lane;
-    if (kept && (stays & below & me)) kept[p + lane] = p + lane;
-    hole_at += __popcll(h_set);
-    mover_at += __popcll(m_set);
+  each_run([&](int p, uint32_t x) {
+    const bool stays = stays_of(p, x), below = p + lane < gap;
+    if (p < gap) {
+      const bool is_free = !stays && below && p + lane < p1;
+      const uint64_t set = __ballot(is_free);
+      if (is_free) mv.to[free_at + lanes_before(set)] = p + lane;
+      if (kept && stays && below) kept[p + lane] = p + lane;
+      free_at += __popcll(set);
+    }
+    if (p + 64 > gap) {
+      const bool moves = stays && !below;
+      const uint64_t set = __ballot(moves);
+      if (moves) mv.from[mover_at + lanes_before(set)] = p + lane;
+      mover_at += __popcll(set);
+    }
+  });
+  if (threadIdx.x == 0) {
+    *mv.n = (int)frees.all;
+    *mv.near = (int)sums_of(4).all;
+    if (h == 0) a.new_lens[b] = a.keep;
   }
-  if (threadIdx.x == kEvictThreads - 1) *mv.n = (int)hole_at;
-  if (h == 0 && threadIdx.x == 0) a.new_lens[b] = a.keep;
   if (kept) {
-    for (int d = threadIdx.x; d < a.keep; d += kEvictThreads)
-      if (d < from || d >= gap) kept[d] = d < from ? d : d + len - a.keep;
+    for (int d = threadIdx.x; d < a.first; d += THREADS) kept[d] = d;
+    for (int d = gap + threadIdx.x; d < a.keep; d += THREADS) kept[d] = d + len - a.keep;
     __threadfence_block();
     __syncthreads();
-    uint32_t n = 0;
-    for (int i = 0; i < kEvictWaves; ++i) n += s_count[1][i];
-    for (int i = threadIdx.x; i < (int)n; i += kEvictThreads) kept[mv.to[i]] = mv.from[i];
+    constexpr int kAtOnce = 8;
+    const int n = (int)frees.all;
+    for (int i = threadIdx.x; i < n; i += kAtOnce * THREADS) {
+      int place[kAtOnce], source[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) place[k] = mv.to[std::min(i + k * THREADS, n - 1)], source[k] = mv.from[std::min(i + k * THREADS, n - 1)];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+        if (i + k * THREADS < n) kept[place[k]] = source[k];
+    }
   }
 }
 
-// A row of keys, one of values and its weight on their way, by 16 lanes
+// Rows move by 16 lanes each: 16 bytes of the key and the value a lane; with 4 bits four lanes have those and one the exponents
+constexpr int kMoveThreads = 512, kMoveRows = kMoveThreads / 16, kMoveAtOnce = 8;
+
 template <bool MX4>
-struct RowInLane {
+struct RowMover {
+  const EvictArgs& a;
+  int b, h, l16;
+  int64_t weights;
   u32x4 x;
   float w;
-  __device__ __forceinline__ void take(const EvictArgs& a, int b, int h, int64_t weights, int row, int l16) {
-    const int64_t at = cache_row(a.cache, b, h, row);
+  __device__ __forceinline__ int64_t at(int row) const {
+    const PagedArgs& c = a.cache;
+    const int64_t page = c.table[(int64_t)b * c.table_stride + (row >> c.page_shift)];
+    return ((page * c.H_kv + h) << c.page_shift) + (row & ((1 << c.page_shift) - 1));
+  }
+  __device__ __forceinline__ void take(int row) {
+    const int64_t r = at(row);
     if constexpr (MX4) {
-      if (l16 < 4) x = *((const u32x4*)((l16 < 2 ? a.cache.k_pages : a.cache.v_pages) + at * kMxRowBytes) + (l16 & 1));
-      if (l16 == 4) x[0] = *(const uint32_t*)(a.cache.scales + at * kMxScaleBytes);
+      if (l16 < 4) x = *((const u32x4*)((l16 < 2 ? a.cache.k_pages : a.cache.v_pages) + r * kMxRowBytes) + (l16 & 1));
+      if (l16 == 4) x[0] = *(const uint32_t*)(a.cache.scales + r * kMxScaleBytes);
     } else {
-      x = *((const u32x4*)((l16 < 8 ? a.cache.k_pages : a.cache.v_pages) + at * kRowBytes) + (l16 & 7));
+      x = *((const u32x4*)((l16 < 8 ? a.cache.k_pages : a.cache.v_pages) + r * kRowBytes) + (l16 & 7));
     }
     if (l16 == 15) w = a.weights[weights + row];
   }
-  __device__ __forceinline__ void put(const EvictArgs& a, int b, int h, int64_t weights, int row, int l16) const {
-    const int64_t at = cache_row(a.cache, b, h, row);
+  __device__ __forceinline__ void put(int row) const {
+    const int64_t r = at(row);
     if constexpr (MX4) {
-      if (l16 < 4) *((u32x4*)((l16 < 2 ? a.cache.k_pages : a.cache.v_pages) + at * kMxRowBytes) + (l16 & 1)) = x;
-      if (l16 == 4) *(uint32_t*)(a.cache.scales + at * kMxScaleBytes) = x[0];
+      if (l16 < 4) *((u32x4*)((l16 < 2 ? a.cache.k_pages : a.cache.v_pages) + r * kMxRowBytes) + (l16 & 1)) = x;
+      if (l16 == 4) *(uint32_t*)(a.cache.scales + r * kMxScaleBytes) = x[0];
     } else {
-      *((u32x4*)((l16 < 8 ? a.cache.k_pages : a.cache.v_pages) + at * kRowBytes) + (l16 & 7)) = x;
+      *((u32x4*)((l16 < 8 ? a.cache.k_pages : a.cache.v_pages) + r * kRowBytes) + (l16 & 7)) = x;
     }
     if (l16 == 15) a.weights[weights + row] = w;
   }
 };
-
-constexpr int kMoveThreads = 256, kMoveRows = kMoveThreads / 16;
-
-// The places that are free are filled; sources lie behind all of them, so moves do not meet
+// The free places are filled, and the last rows go to the end.  Sources of the moves lie behind all places that they fill, so moves do not
+// meet; those in front of row `keep` lie where the last rows go, and move first.  Where the last rows do not go over themselves the workgroups of a head
+// take a part of that region each; else one of them takes all of it, and a batch is read before it is written.
 template <bool MX4>
-__global__ __launch_bounds__(kMoveThreads) void evict_fill_kernel(const EvictArgs a) {
-  const int b = blockIdx.x / a.cache.H_kv, h = blockIdx.x - b * a.cache.H_kv, l16 = threadIdx.x & 15;
-  const Moves mv = moves_of(a, blockIdx.x);
-  const int64_t weights = (int64_t)blockIdx.x * a.columns;
-  const int n = *mv.n;
-  for (int i = blockIdx.y * kMoveRows + (threadIdx.x >> 4); i < n; i += gridDim.y * kMoveRows) {
-    RowInLane<MX4> r;
-    r.take(a, b, h, weights, mv.from[i], l16);
-    r.put(a, b, h, weights, mv.to[i], l16);
-  }
-}
-// The last rows go to the end, in order: towards the front, by one workgroup, which reads a batch before it writes it
-template <bool MX4>
-__global__ __launch_bounds__(kMoveThreads) void evict_tail_kernel(const EvictArgs a) {
-  constexpr int kAtOnce = 8;
-  const int b = blockIdx.x / a.cache.H_kv, h = blockIdx.x - b * a.cache.H_kv, l16 = threadIdx.x & 15;
-  const int64_t weights = (int64_t)blockIdx.x * a.columns;
-  if (*moves_of(a, blockIdx.x).n < 0) return;
-  const int to = a.keep - a.last, from = evict_length(a, b) - a.last;
-  for (int i0 = 0; i0 < a.last; i0 += kAtOnce * kMoveRows) {
-    RowInLane<MX4> r[kAtOnce];
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const EvictArgs a) {
+  const int bh = blockIdx.x, b = bh / a.cache.H_kv, parts = gridDim.y, part = blockIdx.y;
+  const int row0 = threadIdx.x >> 4;
+  const Moves mv = moves_of(a, bh);
+  const int n = *mv.n, near = *mv.near;
+  if (n < 0) return;
+  const RowMover<MX4> r = {a, b, bh - b * a.cache.H_kv, (int)(threadIdx.x & 15), (int64_t)bh * a.columns, {}, 0.f};
+  const int gap = a.keep - a.last, shift = evict_length(a, b) - a.keep;
+  const bool apart = shift >= a.last;
+  const int each = apart ? (a.last + parts - 1) / parts : part == 0 ? a.last : 0;
+  const int d0 = gap + (apart ? std::min(part * each, a.last) : 0), d1 = std::min(d0 + each, a.keep);
+  // moves [i0, i1) whose source is in [lo, hi)
+  auto fill = [&](int i0, int i1, int lo, int hi) {
+    for (int i = i0; i < i1; i += kMoveRows * kMoveAtOnce) {
+      RowMover<MX4> m[kMoveAtOnce] = {r, r, r, r, r, r, r, r};
+      int source[kMoveAtOnce], place[kMoveAtOnce];
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = i0 + k * kMoveRows + (int)(threadIdx.x >> 4);
-      if (i < a.last) r[k].take(a, b, h, weights, from + i, l16);
-    }
-    __syncthreads();
+      for (int k = 0; k < kMoveAtOnce; ++k) {
+        const int at = std::min(i + k * kMoveRows + row0, i1 - 1);
+        source[k] = mv.from[at];
+        place[k] = mv.to[at];
+        if (i + k * kMoveRows + row0 >= i1 || source[k] < lo || source[k] >= hi) source[k] = -1;
+      }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = i0 + k * kMoveRows + (int)(threadIdx.x >> 4);
-      if (i < a.last) r[k].put(a, b, h, weights, to + i, l16);
+      for (int k = 0; k < kMoveAtOnce; ++k)
+        if (source[k] >= 0) m[k].take(source[k]);
+#pragma unroll
+      for (int k = 0; k < kMoveAtOnce; ++k)
+        if (source[k] >= 0) m[k].put(place[k]);
     }
+  };
+  if (d0 < d1) {
+    fill(0, near, d0, d1);
     __syncthreads();
+    for (int d = d0; d < d1; d += kMoveRows * kMoveAtOnce) {
+      RowMover<MX4> m[kMoveAtOnce] = {r, r, r, r, r, r, r, r};
+#pragma unroll
+      for (int k = 0; k < kMoveAtOnce; ++k)
+        if (d + k * kMoveRows + row0 < d1) m[k].take(shift + d + k * kMoveRows + row0);
+      if (!apart) __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kMoveAtOnce; ++k)
+        if (d + k * kMoveRows + row0 < d1) m[k].put(d + k * kMoveRows + row0);
+      if (!apart) __syncthreads();
+    }
   }
+  const int share = ((n - near + parts - 1) / parts + 7) / 8 * 8;
+  const int i0 = std::min(near + part * share, n);
+  fill(i0, std::min(i0 + share, n), 0, INT32_MAX);
 }
 
 template <bool MX4, bool CAUSAL>
@@ -596,9 +772,8 @@ void start_weigh(const WeighArgs& a, hipStream_t stream) {
 template <bool MX4>
 void start_moves(const EvictArgs& a, hipStream_t stream) {
   const unsigned heads = (unsigned)(a.cache.n_seqs * a.cache.H_kv);
-  const unsigned parts = std::max(1u, std::min(64u, 2048u / heads));
-  if (a.keep > a.first + a.last) hipLaunchKernelGGL(evict_fill_kernel<MX4>, dim3(heads, parts), dim3(kMoveThreads), 0, stream, a);
-  if (a.last > 0) hipLaunchKernelGGL(evict_tail_kernel<MX4>, dim3(heads), dim3(kMoveThreads), 0, stream, a);
+  const unsigned parts = std::clamp(1024u / heads, 1u, 32u);
+  hipLaunchKernelGGL(evict_move_kernel<MX4>, dim3(heads, parts), dim3(kMoveThreads), 0, stream, a);
 }
 
 }  // namespace
@@ -614,11 +789,16 @@ hipError_t launch_cache_weigh(const WeighArgs& args, hipStream_t stream) {
 }
 
 int64_t cache_evict_workspace(int n_seqs, int H_kv, int keep) {
-  return ((int64_t)n_seqs * H_kv * (1 + 2 * (int64_t)keep) * 4 + 255) / 256 * 256;
+  return ((int64_t)n_seqs * H_kv * (2 + 2 * (int64_t)keep) * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)(a.cache.n_seqs * a.cache.H_kv)), dim3(kEvictThreads), 0, stream, a);
+  const dim3 heads((unsigned)(a.cache.n_seqs * a.cache.H_kv));
+  // (by what fits the LDS of a workgroup, of the rows that a sequence can have)
+  if ((int64_t)a.cache.table_stride << a.cache.page_shift <= 256 * kEvictRuns)
+    hipLaunchKernelGGL(evict_select_kernel<256>, heads, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL(evict_select_kernel<1024>, heads, dim3(1024), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   a.cache.scales ? start_moves<true>(a, stream) : start_moves<false>(a, stream);
