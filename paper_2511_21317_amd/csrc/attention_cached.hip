@@ -47,8 +47,8 @@ namespace httm {
 namespace {
 
 // What a kernel is made for: the cache's rows in 16 bits; the same, with the logarithms of the sums (which cost others registers that they do not
-// have: 2.8 % of the time of tiles of 256 rows); rows in 4 bits, with or without them
-enum { ROWS, ROWS_AND_SUMS, MX4_ROWS };
+// have: 2.8 % of the time of tiles of 256 rows); rows in 4 bits, with or without them, behind a prefix or alone
+enum { ROWS, ROWS_AND_SUMS, MX4_ROWS, MX4_ALONE };
 
 constexpr int kUnit = 32;                       // keys
 constexpr int kUnitBytes = kUnit * kRowBytes;
@@ -416,23 +416,31 @@ struct UnitData {
   u32x4 k[4];       // [key half * 2 + channel half]: the A operands
   u32x4 v[4];       // 8 rows each; with 4 bits as k
 };
-// The codes of a row's 16 channels, as they lie: {k, k, v, v}, and the block's two exponents
-struct MxHalf {
-  u32x4 codes;
-  uint32_t exponents;
+// A unit of keys in 4 bits: the codes of 16 channels of K and of V of a row of either half, and the block's two exponents
+struct MxUnit {
+  u32x2 k[2], v[2];
+  uint32_t exponents[2];
 };
-__device__ __forceinline__ void expand(UnitData& d, int half, const MxHalf& x) {
-  const float ku = mx4_key_unit(x.exponents), vu = mx4_value_unit(x.exponents);
+__device__ __forceinline__ void expand(UnitData& d, const MxUnit& x) {
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    d.k[2 * half + e] = mx4_values(x.codes[e], ku);
-    d.v[2 * half + e] = mx4_values(x.codes[2 + e], vu);
+  for (int i = 0; i < 2; ++i) {
+    const float ku = mx4_key_unit(x.exponents[i]), vu = mx4_value_unit(x.exponents[i]);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      d.k[2 * i + e] = mx4_values(x.k[i][e], ku);
+      d.v[2 * i + e] = mx4_values(x.v[i][e], vu);
+    }
   }
 }
 
 // Rows of K or V: 16 from `at` on, of which the first `n` are there; the others are read as zeros, wherever they would be
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_rows(const char* at, int n, int row_bytes = kRowBytes) {
-  return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, n * row_bytes, kRawBufferWord3);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_rows(const char* at, int n) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, n * kRowBytes, kRawBufferWord3);
+}
+// The same of `row_bytes` each, where the compiler does not see that all lanes ask for the same rows: it would load for one lane after the other
+// and wait for each
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rows(const char* at, int n, int row_bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)uniform64((int64_t)at), 0, uniform(n * row_bytes), kRawBufferWord3);
 }
 __device__ __forceinline__ u32x4 load_row(__amdgpu_buffer_rsrc_t rows, int offset) {
   return __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 0, 0);
@@ -477,7 +485,7 @@ __device__ __forceinline__ void add_seen(f32x4 (&o)[4][NQ], const bf16x8 (&av)[4
 template <int NQ, bool CAUSAL, int KIND, typename Limit>
 __device__ __forceinline__ void unit_step(WaveState<NQ>& w, const UnitData& d, bf16_t* sv, float c, int row0, int end, int ok, bool own,
                                           int lane, Limit limit_of) {
-  constexpr bool MX4 = KIND == MX4_ROWS;
+  constexpr bool MX4 = KIND == MX4_ROWS || KIND == MX4_ALONE;
   const int l16 = lane & 15, grp = lane >> 4;
   const bool masked = ok != 3 || row0 + kUnit > end;
   const bool wild = CAUSAL && masked && own && __ballot(not_finite(d.v)) != 0;
@@ -559,7 +567,7 @@ constexpr int kWaves = 4;
 template <int NQ, bool CAUSAL, int KIND>
 __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const Share& share, const Extent& ex, int64_t line, int64_t x,
                                      int64_t end, Seq window, char* s_mem, float2* s_ml) {
-  constexpr bool MX4 = KIND == MX4_ROWS;
+  constexpr bool MX4 = KIND == MX4_ROWS || KIND == MX4_ALONE;
   constexpr int R = 16 * NQ, KS = kWaves;
   constexpr int DEPTH = 1;     // units of a wave on their way besides the one in work
   const CachedAttnArgs& c = a.c;
@@ -569,7 +577,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
   Place p;
   if (!find_place<R, CAUSAL, false>(a, part, ex, x, lane, p, window)) return;
   Seq s = of_lane<R, CAUSAL, false>(a, part, window, p.b - p.base);
-  const int P = part.with_prefix ? (int)c.P : 0, prefix_units = (P + kUnit - 1) / kUnit;
+  const int P = KIND != MX4_ALONE && part.with_prefix ? (int)c.P : 0, prefix_units = (P + kUnit - 1) / kUnit;
   const int k_offset = l16 * kRowBytes + grp * (MX4 ? 32 : 16), v_offset = MX4 ? k_offset : lane * 16;
   bool first = true;
 
@@ -597,28 +605,13 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
       }
       return g;
     };
-    // Requests a unit's rows, of own keys in 4 bits the codes in the first half of their place; returns its ok bits
+    // Requests a unit's rows; returns its ok bits
     auto fetch = [&](int unit, const Pages& g, UnitData& d) {
       int ok = 3;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const char *k, *v;
         int n;
-        if (MX4 && unit >= prefix_units) {
-          const int row = (unit - prefix_units) * kUnit + 16 * i;
-          const bool there = g.page[i] >= 0 && g.page[i] < c.cache.n_pages;
-          const int64_t page = there ? g.page[i] : 0;
-          const int64_t at = ((page * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1));
-          n = std::clamp(there ? s.len - row : 0, 0, 16);
-          ok &= there ? 3 : ~(1 << i);
-          const int in = l16 * kMxRowBytes + grp * 8;
-          const u32x2 kc = __builtin_amdgcn_raw_buffer_load_b64(half_rows(c.cache.k_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
-          const u32x2 vc = __builtin_amdgcn_raw_buffer_load_b64(half_rows(c.cache.v_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
-          d.k[2 * i] = u32x4{kc[0], kc[1], vc[0], vc[1]};
-          d.k[2 * i + 1][0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
-              half_rows((const char*)c.cache.scales + at * kMxScaleBytes, n, kMxScaleBytes), l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
-          continue;
-        }
         if (unit < prefix_units) {
           const int row = unit * kUnit + 16 * i;
           const int64_t at = (p.h * c.P + row) * kRowBytes;
@@ -636,7 +629,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
           ok &= there ? 3 : ~(1 << i);
         }
         n = std::clamp(n, 0, 16);
-        const __amdgpu_buffer_rsrc_t kr = half_rows(k, n), vr = half_rows(v, n);
+        const __amdgpu_buffer_rsrc_t kr = MX4 ? uniform_rows(k, n, kRowBytes) : half_rows(k, n), vr = MX4 ? uniform_rows(v, n, kRowBytes) : half_rows(v, n);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) d.k[2 * i + ks] = load_row(kr, k_offset + ks * (MX4 ? 16 : 64));
 #pragma unroll
@@ -661,30 +654,70 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
     // DEPTH units are on their way, the pages of the next one are asked for.  (The data moves through registers: two copies
     // of the step in the loop need more scalar registers than there are.)
     int unit = piece.u0 + wave;
+    const int stop_rows = MX4 ? std::min(stop, prefix_units) : stop;      // of the units in 16 bits
     UnitData d[DEPTH + 1];
     int ok[DEPTH + 1];
     Pages g = look_up(unit);
-#pragma unroll
-    for (int i = 0; i < DEPTH; ++i) {
-      if (unit + i * KS < stop) ok[i] = fetch(unit + i * KS, g, d[i]);
-      g = look_up(unit + (i + 1) * KS);
-    }
-#pragma unroll 1
-    for (; unit < stop; unit += KS) {
-      if (unit + DEPTH * KS < stop) ok[DEPTH] = fetch(unit + DEPTH * KS, g, d[DEPTH]);
-      g = look_up(unit + (DEPTH + 1) * KS);
-      const bool own = unit >= prefix_units;
-      if constexpr (MX4)
-        if (own) {
-          const MxHalf half[2] = {{d[0].k[0], d[0].k[1][0]}, {d[0].k[2], d[0].k[3][0]}};
-          expand(d[0], 0, half[0]);
-          expand(d[0], 1, half[1]);
-        }
-      unit_step<NQ, CAUSAL, KIND>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane, limit_of);
+    if constexpr (KIND != MX4_ALONE) {
 #pragma unroll
       for (int i = 0; i < DEPTH; ++i) {
-        d[i] = d[i + 1];
-        ok[i] = ok[i + 1];
+        if (unit + i * KS < stop_rows) ok[i] = fetch(unit + i * KS, g, d[i]);
+        g = look_up(unit + (i + 1) * KS);
+      }
+#pragma unroll 1
+      for (; unit < stop_rows; unit += KS) {
+        if (unit + DEPTH * KS < stop_rows) ok[DEPTH] = fetch(unit + DEPTH * KS, g, d[DEPTH]);
+        g = look_up(unit + (DEPTH + 1) * KS);
+        const bool own = unit >= prefix_units;
+        unit_step<NQ, CAUSAL, KIND>(w, d[0], sv, c.scale_log2, (own ? unit - prefix_units : unit) * kUnit, own ? least : P, ok[0], own, lane, limit_of);
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+          d[i] = d[i + 1];
+          ok[i] = ok[i + 1];
+        }
+      }
+    }
+    if constexpr (MX4) {
+      // Own keys in 4 bits: a unit's codes are turned into values, and those of a later one requested in their place
+      constexpr int AHEAD = KIND == MX4_ALONE && NQ == 1 ? 3 : 1;
+      MxUnit raw[AHEAD];
+      int ok_raw[AHEAD];
+      auto request = [&](int u, const Pages& p2, MxUnit& r, int& ok) {
+        const int row = (u - prefix_units) * kUnit;
+        ok = 3;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool there = p2.page[i] >= 0 && p2.page[i] < c.cache.n_pages;
+          const int64_t page = there ? p2.page[i] : 0;
+          const int64_t at = ((page * c.cache.H_kv + p.h) << c.cache.page_shift) + ((row + 16 * i) & ((1 << c.cache.page_shift) - 1));
+          const int n = there ? std::clamp(s.len - row - 16 * i, 0, 16) : 0;
+          ok &= there ? 3 : ~(1 << i);
+          const int in = l16 * kMxRowBytes + grp * 8;
+          r.k[i] = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(c.cache.k_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
+          r.v[i] = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(c.cache.v_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
+          r.exponents[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
+              uniform_rows((const char*)c.cache.scales + at * kMxScaleBytes, n, kMxScaleBytes), l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
+        }
+      };
+      if constexpr (KIND != MX4_ALONE) g = look_up(unit);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        if (unit + i * KS < stop) request(unit + i * KS, g, raw[i], ok_raw[i]);
+        g = look_up(unit + (i + 1) * KS);
+      }
+#pragma unroll 1
+      while (unit < stop) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          if (unit >= stop) break;
+          UnitData now;
+          expand(now, raw[i]);
+          const int ok_now = ok_raw[i];
+          if (unit + AHEAD * KS < stop) request(unit + AHEAD * KS, g, raw[i], ok_raw[i]);
+          g = look_up(unit + (AHEAD + 1) * KS);
+          unit_step<NQ, CAUSAL, KIND>(w, now, sv, c.scale_log2, (unit - prefix_units) * kUnit, least, ok_now, true, lane, limit_of);
+          unit += KS;
+        }
       }
     }
 
@@ -745,7 +778,7 @@ attention_cached_kernel(const LineArgs a) {
   if (!find_share(a, total_a + total_b, share)) return;
   if constexpr (NA > 0)
     if (share.at < total_a) {
-      walk<NA, false, KIND>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
+      walk<NA, false, ROWS>(a, a.part[0], share, ea, 0, share.at, std::min(share.end, total_a), window_a, s_mem, s_ml);
     }
   if (share.end > total_a)
     walk<NB, CAUSAL, KIND>(a, a.part[1], share, eb, total_a, std::max(share.at, total_a) - total_a, share.end - total_a, window_b, s_mem, s_ml);
@@ -794,7 +827,7 @@ __device__ __forceinline__ void raise_shift(WideState& w, const float (&top)[kWi
 
 template <bool CAUSAL, int KIND>
 __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_cached_wide_kernel(const LineArgs a) {
-  constexpr bool MX4 = KIND == MX4_ROWS;
+  constexpr bool MX4 = KIND == MX4_ROWS || KIND == MX4_ALONE;
   constexpr int NQ = kWideQ, R = kWideRows, UNIT = kWideUnit;
   // K of two units, V of two.  All that reads or writes them goes by offsets that change sides once a unit.
   constexpr int kSide = UNIT * kRowBytes, kHalf = kSide / 2;
@@ -894,14 +927,15 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
     bool k_own = false, v_own = false;      // what they hold is codes (MX4): two words, and in the second of them an exponent as a unit
     auto request = [&](u32x4 (&in)[2], const RowsAt& r, const char* prefix, const char* pages, int exponent) {
       if (MX4 && r.own) {
-        const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(half_rows(pages + r.offset * kMxRowBytes, r.n, kMxRowBytes), lane * 8, 0, 0);
+        const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(pages + r.offset * kMxRowBytes, r.n, kMxRowBytes), lane * 8, 0, 0);
         in[0][0] = codes[0];
         in[0][1] = codes[1];
-        in[1][0] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(half_rows((const char*)c.cache.scales + r.offset * kMxScaleBytes, r.n, kMxScaleBytes),
+        in[1][0] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(uniform_rows((const char*)c.cache.scales + r.offset * kMxScaleBytes, r.n, kMxScaleBytes),
                                                                 (lane >> 2) * kMxScaleBytes + (lane & 2) + exponent, 0, 0);
         return;
       }
-      const __amdgpu_buffer_rsrc_t rows = half_rows((r.own ? pages : prefix) + r.offset, r.n);
+      const char* at = (r.own ? pages : prefix) + r.offset;
+      const __amdgpu_buffer_rsrc_t rows = MX4 ? uniform_rows(at, r.n, kRowBytes) : half_rows(at, r.n);
 #pragma unroll
       for (int i = 0; i < 2; ++i) in[i] = load_row(rows, MX4 ? lane * 32 + i * 16 : lane * 16 + i * 1024);
     };
@@ -1284,9 +1318,12 @@ void start(const LineArgs& a, int shares, hipStream_t stream) {
 }
 template <int NA, int NB>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
-  if (a.c.cache.scales)
-    start<NA, NB, MX4_ROWS>(a, shares, stream);
-  else if (a.c.lse && a.finish)      // (pieces in their slots leave the sums to combine_kernel)
+  if constexpr (NA > 0) {      // (the sequences' part has no prefix)
+    if (a.c.cache.scales) return start<NA, NB, MX4_ALONE>(a, shares, stream);
+  } else if (a.c.cache.scales) {
+    return a.c.P > 0 && a.part[1].with_prefix ? start<NA, NB, MX4_ROWS>(a, shares, stream) : start<NA, NB, MX4_ALONE>(a, shares, stream);
+  }
+  if (a.c.lse && a.finish)      // (pieces in their slots leave the sums to combine_kernel)
     start<NA, NB, ROWS_AND_SUMS>(a, shares, stream);
   else
     start<NA, NB, ROWS>(a, shares, stream);

@@ -130,7 +130,10 @@ struct KeysOnTheirWay {
     there |= ok ? (1u << T1) - (1u << T0) : 0u;
     const int64_t first = (((int64_t)(ok ? page : 0) * c.H_kv + h) << c.page_shift) + (row & ((1 << c.page_shift) - 1));
     const int n = ok ? std::clamp(len - row, 0, 16 * (T1 - T0)) : 0;
-    auto rows = [&](const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((char*)p + first * bytes, 0, n * bytes, kRawBufferWord3); };
+    // (the compiler does not see that all lanes ask for the same rows: it would load for one lane after the other)
+    auto rows = [&](const void* p, int bytes) {
+      return __builtin_amdgcn_make_buffer_rsrc((void*)uniform64((int64_t)((char*)p + first * bytes)), 0, uniform(n * bytes), kRawBufferWord3);
+    };
     if constexpr (MX4) {
       const __amdgpu_buffer_rsrc_t codes = rows(c.k_pages, kMxRowBytes), scales = rows(c.scales, kMxScaleBytes);
 #pragma unroll
