@@ -36,6 +36,7 @@
 // Tiles of 256 rows: vector issue and power, 4 frames of 1374 tokens behind 28 650 shared keys, 16 heads, 0.90 to 0.95 PFLOP/s in the loop (a bf16
 // product of 8192^3 reaches 1.20).
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_common.hpp"
 #include "dev_common.hpp"
@@ -792,6 +793,7 @@ attention_cached_kernel(const LineArgs a) {
 // own, which depend on neither: the order of issue mixes them.  (V therefore runs a unit behind K.)  Whether a shift has to
 // follow is looked at before the block, on scores that the step before has left.
 
+enum { MIXED_UNITS, PREFIX_UNITS, OWN_UNITS };
 constexpr int kWideUnit = 64;
 constexpr int kWideWaves = 4;
 constexpr int kWideQ = 4;
@@ -843,7 +845,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
   Place p;
   if (!find_place<R, CAUSAL, true>(a, part, ex, share.at, lane, p, window)) return;
   Seq s = of_lane<R, CAUSAL, true>(a, part, window, p.b - p.base);
-  const int P = part.with_prefix ? (int)c.P : 0, prefix_units = (P + UNIT - 1) / UNIT;
+  const int P = KIND != MX4_ALONE && part.with_prefix ? (int)c.P : 0, prefix_units = (P + UNIT - 1) / UNIT;
   int64_t x = share.at;
   bool first = true;
   // lanes' offsets: K operands (channel halves), V operands (channel quarters), the rows that a wave brings (K, V)
@@ -902,77 +904,6 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       return index < c.cache.table_stride ? table[index] : -1;
     };
     auto there = [&](int page) { return page >= 0 && page < (int)c.cache.n_pages; };
-    // A wave brings the unit's rows 16 * wave .. + 15, of K and, a unit later, of V
-    struct RowsAt {
-      int64_t offset;     // from k_prefix or k_pages, and from v_prefix or v_pages, in bytes; of rows in 4 bits in rows
-      int n;
-      bool own;
-    };
-    auto rows_at = [&](int unit) {
-      RowsAt r = {0, 0, unit >= prefix_units};
-      const int row = (r.own ? unit - prefix_units : unit) * UNIT + 16 * wave;
-      if (unit >= stop) {
-      } else if (!r.own) {
-        r.offset = (p.h * c.P + row) * kRowBytes;
-        r.n = std::clamp((int)c.P - row, 0, 16);
-      } else {
-        const int page = page_of(unit, wave);
-        r.n = there(page) ? std::clamp(s.len - row, 0, 16) : 0;
-        r.offset = ((((int64_t)(r.n ? page : 0) * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) *
-                   (MX4 ? 1 : kRowBytes);
-      }
-      return r;
-    };
-    u32x4 in_k[2], in_v[2];
-    bool k_own = false, v_own = false;      // what they hold is codes (MX4): two words, and in the second of them an exponent as a unit
-    auto request = [&](u32x4 (&in)[2], const RowsAt& r, const char* prefix, const char* pages, int exponent) {
-      if (MX4 && r.own) {
-        const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(pages + r.offset * kMxRowBytes, r.n, kMxRowBytes), lane * 8, 0, 0);
-        in[0][0] = codes[0];
-        in[0][1] = codes[1];
-        in[1][0] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(uniform_rows((const char*)c.cache.scales + r.offset * kMxScaleBytes, r.n, kMxScaleBytes),
-                                                                (lane >> 2) * kMxScaleBytes + (lane & 2) + exponent, 0, 0);
-        return;
-      }
-      const char* at = (r.own ? pages : prefix) + r.offset;
-      const __amdgpu_buffer_rsrc_t rows = MX4 ? uniform_rows(at, r.n, kRowBytes) : half_rows(at, r.n);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) in[i] = load_row(rows, MX4 ? lane * 32 + i * 16 : lane * 16 + i * 1024);
-    };
-    auto request_k = [&](u32x4 (&in)[2], const RowsAt& r) { request(in, r, c.k_prefix, c.cache.k_pages, 0); };
-    auto request_v = [&](u32x4 (&in)[2], const RowsAt& r) { request(in, r, c.v_prefix, c.cache.v_pages, 1); };
-    auto expanded = [&](u32x4 (&in)[2], bool own) {
-      if (MX4 && own) {
-        const float unit = __uint_as_float(in[1][0] << 23);
-        const uint32_t c0 = in[0][0], c1 = in[0][1];
-        in[0] = mx4_values(c0, unit);
-        in[1] = mx4_values(c1, unit);
-      }
-    };
-    auto store_k = [&](int to, u32x4 (&in)[2], bool own) {
-      expanded(in, own);
-      *(u32x4*)(s_mem + to) = in[0];
-      if constexpr (MX4)
-        *(u32x4*)(s_mem + (to ^ 16)) = in[1];
-      else
-        *(u32x4*)(s_mem + (to ^ 64) + 8 * kRowBytes) = in[1];      // (k_swizzle() of the row 8 further: 4 more)
-    };
-    auto store_v = [&](int to, u32x4 (&in)[2], bool own) {
-      expanded(in, own);
-      *(u32x4*)(s_mem + to) = in[0];
-      *(u32x4*)(s_mem + (MX4 ? to ^ 16 : to + 8 * kRowBytes)) = in[1];
-    };
-    // 4 bits for a unit, whether its quarters have pages: looked at only where some entry of the tile's is none
-    bool holes = false;
-    auto ok_of = [&](int unit) {
-      uint32_t ok = 15;
-      if (holes && unit >= prefix_units) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ok &= there(page_of(unit, i)) ? 15u : ~(1u << i);
-      }
-      return ok;
-    };
-
     auto load_k = [&](bf16x8 (&ak)[4], int half) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
@@ -1019,7 +950,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
     };
     // A step of 32 keys from row0 on.  half: where the K rows of the step behind it and the V rows of the step before are in their
     // sides; end, ok, own as in unit_step()
-    auto step = [&](int half, int row0, int end, uint32_t ok, bool own) {
+    auto step = [&](int half, int row0, int end, uint32_t ok, bool own) __attribute__((always_inline)) {
       bf16x8 ak[4], av[4];
       load_v(av, half);
       const bool partial = row0 + 32 > end;
@@ -1087,7 +1018,81 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       __builtin_amdgcn_s_setprio(0);
     };
 
-    if (u0 < stop) {
+    // The units [u0, stop) of a piece.  OWN: all of them prefix or all own keys, known to the compiler (rows in 4 bits: one loop for each of the two, without a
+    // choice between two kinds of loads in it: 662 -> TIME us, 4 x 1374 rows to 5516 shared keys in 16 bits and up to 27480 own ones in 4, 16 heads), or by the unit
+    bool holes = false;
+    auto run_units = [&](auto own_units, const int u0, const int stop) __attribute__((always_inline)) {
+      constexpr int OWN = decltype(own_units)::value;
+      auto is_own = [&](int unit) { return OWN == OWN_UNITS || (OWN == MIXED_UNITS && unit >= prefix_units); };
+      // A wave brings the unit's rows 16 * wave .. + 15, of K and, a unit later, of V
+      struct RowsAt {
+        int64_t offset;     // from k_prefix or k_pages, and from v_prefix or v_pages, in bytes; of rows in 4 bits in rows
+        int n;
+        bool own;
+      };
+      auto rows_at = [&](int unit) {
+        RowsAt r = {0, 0, is_own(unit)};
+        const int row = (r.own ? unit - prefix_units : unit) * UNIT + 16 * wave;
+        if (unit >= stop) {
+        } else if (!r.own) {
+          r.offset = (p.h * c.P + row) * kRowBytes;
+          r.n = std::clamp((int)c.P - row, 0, 16);
+        } else {
+          const int page = page_of(unit, wave);
+          r.n = there(page) ? std::clamp(s.len - row, 0, 16) : 0;
+          r.offset = ((((int64_t)(r.n ? page : 0) * c.cache.H_kv + p.h) << c.cache.page_shift) + (row & ((1 << c.cache.page_shift) - 1))) *
+                     (MX4 ? 1 : kRowBytes);
+        }
+        return r;
+      };
+      u32x4 in_k[2], in_v[2];
+      bool k_own = false, v_own = false;      // what they hold is codes (MX4): two words, and in the second of them an exponent as a unit
+      auto request = [&](u32x4 (&in)[2], const RowsAt& r, const char* prefix, const char* pages, int exponent) {
+        if (MX4 && r.own) {
+          const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(pages + r.offset * kMxRowBytes, r.n, kMxRowBytes), lane * 8, 0, 0);
+          in[0][0] = codes[0];
+          in[0][1] = codes[1];
+          in[1][0] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(uniform_rows((const char*)c.cache.scales + r.offset * kMxScaleBytes, r.n, kMxScaleBytes),
+                                                                  (lane >> 2) * kMxScaleBytes + (lane & 2) + exponent, 0, 0);
+          return;
+        }
+        const char* at = (r.own ? pages : prefix) + r.offset;
+        const __amdgpu_buffer_rsrc_t rows = MX4 ? uniform_rows(at, r.n, kRowBytes) : half_rows(at, r.n);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) in[i] = load_row(rows, MX4 ? lane * 32 + i * 16 : lane * 16 + i * 1024);
+      };
+      auto request_k = [&](u32x4 (&in)[2], const RowsAt& r) { request(in, r, c.k_prefix, c.cache.k_pages, 0); };
+      auto request_v = [&](u32x4 (&in)[2], const RowsAt& r) { request(in, r, c.v_prefix, c.cache.v_pages, 1); };
+      auto expanded = [&](u32x4 (&in)[2], bool own) {
+        if (MX4 && own) {
+          const float unit = __uint_as_float(in[1][0] << 23);
+          const uint32_t c0 = in[0][0], c1 = in[0][1];
+          in[0] = mx4_values(c0, unit);
+          in[1] = mx4_values(c1, unit);
+        }
+      };
+      auto store_k = [&](int to, u32x4 (&in)[2], bool own) {
+        expanded(in, own);
+        *(u32x4*)(s_mem + to) = in[0];
+        if constexpr (MX4)
+          *(u32x4*)(s_mem + (to ^ 16)) = in[1];
+        else
+          *(u32x4*)(s_mem + (to ^ 64) + 8 * kRowBytes) = in[1];      // (k_swizzle() of the row 8 further: 4 more)
+      };
+      auto store_v = [&](int to, u32x4 (&in)[2], bool own) {
+        expanded(in, own);
+        *(u32x4*)(s_mem + to) = in[0];
+        *(u32x4*)(s_mem + (MX4 ? to ^ 16 : to + 8 * kRowBytes)) = in[1];
+      };
+      // 4 bits for a unit, whether its quarters have pages: looked at only where some entry of the tile's is none
+      auto ok_of = [&](int unit) {
+        uint32_t ok = 15;
+        if (holes && is_own(unit)) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ok &= there(page_of(unit, i)) ? 15u : ~(1u << i);
+        }
+        return ok;
+      };
       // K units u0 and u0 + 1 and V unit u0 are there before the first step; zeros for the V unit in front of it
       RowsAt v_next = rows_at(u0), k_next = rows_at(u0 + 1);
       {
@@ -1107,7 +1112,8 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
       k_own = k_next.own;
       v_own = v_next.own;
       bool hole = false;
-      for (int i = lane; i < (most + (1 << c.cache.page_shift) - 1) >> c.cache.page_shift; i += 64) hole |= !there(table[i]);
+      if (OWN != PREFIX_UNITS)
+        for (int i = lane; i < (most + (1 << c.cache.page_shift) - 1) >> c.cache.page_shift; i += 64) hole |= !there(table[i]);
       holes = __ballot(hole) != 0;
       barrier();
       if (active) {
@@ -1117,7 +1123,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
         for (int qt = 0; qt < NQ; ++qt) score(ak, qt);
       }
       for (int unit = u0; unit < stop; ++unit) {
-        const bool own = unit >= prefix_units;
+        const bool own = is_own(unit);
         const int row0 = (own ? unit - prefix_units : unit) * UNIT, end = own ? least : P;
         const uint32_t ok = ok_of(unit);
         if (active) step(kHalf, row0, end, ok & 3, own);
@@ -1141,6 +1147,19 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
           for (int ct = 0; ct < 4; ++ct) w.o[ct][qt] = mfma16(av[ct], w.p[qt], w.o[ct][qt]);
       }
+    };
+    if constexpr (KIND == MX4_ROWS) {
+      const int split = std::clamp(prefix_units, u0, std::max(u0, stop));
+      if (u0 < split) run_units(std::integral_constant<int, PREFIX_UNITS>(), u0, split);
+      if (u0 < split && split < stop) {
+        old_row0 = -1;
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) w.p[qt] = bf16x8{};      // (they have been multiplied)
+        barrier();      // everybody is done with the buffers
+      }
+      if (split < stop) run_units(std::integral_constant<int, OWN_UNITS>(), split, stop);
+    } else {
+      if (u0 < stop) run_units(std::integral_constant<int, KIND == MX4_ALONE ? OWN_UNITS : MIXED_UNITS>(), u0, stop);
     }
 
     const Target to = place_piece<R>(a, part, share, p, s, piece, first, x - p.at);
@@ -1378,7 +1397,7 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
     // (the part of the prefix has no rows in 4 bits)
     const bool causal = args.causal && i == 1;
     if (i == 1 && args.cache.scales)
-      start_wide<MX4_ROWS>(w, causal, ch.shares[i], stream);
+      args.P > 0 && a.part[1].with_prefix ? start_wide<MX4_ROWS>(w, causal, ch.shares[i], stream) : start_wide<MX4_ALONE>(w, causal, ch.shares[i], stream);
     else if (args.lse && a.finish)
       start_wide<ROWS_AND_SUMS>(w, causal, ch.shares[i], stream);
     else
