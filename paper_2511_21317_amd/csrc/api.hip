@@ -747,7 +747,7 @@ bool outputs_meet(const NormRopeArgs& a, int dtype, const int64_t (&bytes)[3], c
 }
 
 // `scales`: of a cache in 4 bits, or nullptr
-int check_cache(const httm_paged_t* c, void* scales, int H_q, PagedArgs* out) {
+int check_cache(const httm_paged_t* c, const void* scales, int H_q, PagedArgs* out) {
   if (!c || !c->k_pages || !c->v_pages || !c->page_table || c->n_pages < 1 || c->n_seqs < 1 || c->table_stride < 1 ||
       c->page_size < 1 || c->H_kv < 1 || H_q < 1 || H_q % c->H_kv)
     return HTTM_E_INVALID_ARG;
@@ -762,14 +762,14 @@ int check_cache(const httm_paged_t* c, void* scales, int H_q, PagedArgs* out) {
         meet(scales, rows * 4, c->v_pages, rows * 32))
       return HTTM_E_INVALID_ARG;
   }
-  *out = {(char*)c->k_pages, (char*)c->v_pages, (uint8_t*)scales, c->page_table, c->n_pages, c->n_seqs, c->table_stride, __builtin_ctz(c->page_size), c->H_kv};
+  *out = {(char*)c->k_pages, (char*)c->v_pages, c->page_table, c->n_pages, c->n_seqs, c->table_stride, __builtin_ctz(c->page_size), c->H_kv};
   return HTTM_OK;
 }
 
 // Whether a range lies over the cache's pages
-bool meets_pages(const PagedArgs& c, const void* range, int64_t bytes) {
-  const int64_t rows = (c.n_pages * c.H_kv) << c.page_shift, row = c.scales ? 32 : 128;
-  return meet(c.k_pages, rows * row, range, bytes) || meet(c.v_pages, rows * row, range, bytes) || (c.scales && meet(c.scales, rows * 4, range, bytes));
+bool meets_pages(const PagedArgs& c, const void* scales, const void* range, int64_t bytes) {
+  const int64_t rows = (c.n_pages * c.H_kv) << c.page_shift, row = scales ? 32 : 128;
+  return meet(c.k_pages, rows * row, range, bytes) || meet(c.v_pages, rows * row, range, bytes) || (scales && meet(scales, rows * 4, range, bytes));
 }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -862,6 +862,7 @@ static int append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_r
   a.pos = pos;
   a.first_pos = first_pos;
   a.cache = paged;
+  a.scales = (uint8_t*)scales;
   a.offsets = offsets;
   a.seq_lens = seq_lens;
   a.out[0] = (char*)q_out;
@@ -887,15 +888,16 @@ int httm_cache_read(const httm_paged_t* cache, const void* scales, const int32_t
                     int d_head, void* k_out, void* v_out, void* stream) {
   CacheReadArgs a;
   std::memset(&a, 0, sizeof(a));
-  const int rc = check_cache(cache, const_cast<void*>(scales), cache ? cache->H_kv : 0, &a.cache);
+  const int rc = check_cache(cache, scales, cache ? cache->H_kv : 0, &a.cache);
   if (rc != HTTM_OK) return rc;
   if (n_tokens < 0 || !offsets || !seq_lens || !aligned4(offsets) || !aligned4(seq_lens)) return HTTM_E_INVALID_ARG;
   if (d_head != 64 || n_tokens >= ((int64_t)1 << 25)) return HTTM_E_UNSUPPORTED;
   if (n_tokens == 0) return HTTM_OK;
   const int64_t bytes = n_tokens * cache->H_kv * kOutRow;
-  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || meet(k_out, bytes, v_out, bytes) || meets_pages(a.cache, k_out, bytes) ||
-      meets_pages(a.cache, v_out, bytes))
+  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || meet(k_out, bytes, v_out, bytes) || meets_pages(a.cache, scales, k_out, bytes) ||
+      meets_pages(a.cache, scales, v_out, bytes))
     return HTTM_E_INVALID_ARG;
+  a.scales = (const uint8_t*)scales;
   a.offsets = offsets;
   a.seq_lens = seq_lens;
   a.N = n_tokens;
@@ -916,7 +918,7 @@ int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const 
                               float scale, int causal, void* o, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
   CachedAttnArgs a;
   std::memset(&a, 0, sizeof(a));
-  int rc = check_cache(cache, const_cast<void*>(scales), H_q, &a.cache);
+  int rc = check_cache(cache, scales, H_q, &a.cache);
   if (rc != HTTM_OK) return rc;
   if (n_tokens < 0 || P < 0 || !std::isnormal(scale) || scale < 0.f || !std::isfinite(scale * 1.4426950408889634f)) return HTTM_E_INVALID_ARG;
   if (d_head != 64 || n_tokens >= ((int64_t)1 << 20) || P >= ((int64_t)1 << 24)) return HTTM_E_UNSUPPORTED;
@@ -930,7 +932,7 @@ int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const 
   if (rows_meet(a.q, n_tokens, H_q, 2, o, n_tokens * H_q * kOutRow)) return HTTM_E_INVALID_ARG;
   const int64_t lse_bytes = n_tokens * H_q * (int64_t)sizeof(float);
   if (lse && (!aligned4(lse) || meet(lse, lse_bytes, o, n_tokens * H_q * kOutRow) || rows_meet(a.q, n_tokens, H_q, 2, lse, lse_bytes) ||
-              meet(lse, lse_bytes, workspace, workspace_bytes) || meets_pages(a.cache, lse, lse_bytes)))
+              meet(lse, lse_bytes, workspace, workspace_bytes) || meets_pages(a.cache, scales, lse, lse_bytes)))
     return HTTM_E_INVALID_ARG;
   a.k_prefix = (const char*)k_prefix;
   a.v_prefix = (const char*)v_prefix;
@@ -943,6 +945,7 @@ int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const 
   a.scale_log2 = scale * 1.4426950408889634f;
   a.o = o;
   a.lse = lse;
+  a.scales = (const uint8_t*)scales;
   a.workspace = (char*)workspace;
   HTTM_HIP(launch_cached_attention(a, (hipStream_t)stream));
   return HTTM_OK;
@@ -960,7 +963,7 @@ int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm_paged_t*
                      int64_t columns, void* stream) {
   WeighArgs a;
   std::memset(&a, 0, sizeof(a));
-  int rc = check_cache(cache, const_cast<void*>(scales), H_q, &a.cache);
+  int rc = check_cache(cache, scales, H_q, &a.cache);
   if (rc != HTTM_OK) return rc;
   if (n_tokens < 0 || !std::isnormal(scale) || scale < 0.f || !std::isfinite(scale * 1.4426950408889634f) || !std::isfinite(decay) || decay < 0.f)
     return HTTM_E_INVALID_ARG;
@@ -973,13 +976,14 @@ int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm_paged_t*
   if (n_tokens > 0 && (!a.q.data || !lse || !aligned4(lse) || rows_meet(a.q, n_tokens, H_q, 2, weights, bytes) ||
                        meet(lse, n_tokens * H_q * (int64_t)sizeof(float), weights, bytes)))
     return HTTM_E_INVALID_ARG;
-  if (meets_pages(a.cache, weights, bytes)) return HTTM_E_INVALID_ARG;
+  if (meets_pages(a.cache, scales, weights, bytes)) return HTTM_E_INVALID_ARG;
   a.lse = lse;
   a.offsets = offsets;
   a.seq_lens = seq_lens;
   a.n_tokens = n_tokens;
   a.group = H_q / cache->H_kv;
   a.causal = causal != 0;
+  a.scales = (const uint8_t*)scales;
   a.scale = scale;
   a.decay = decay;
   a.weights = weights;
@@ -1016,10 +1020,11 @@ int httm_cache_evict(const httm_paged_t* cache, void* scales, const int32_t* seq
   const Range r[] = {{new_lens, cache->n_seqs * four}, {weights, heads * columns * four}, {workspace, workspace_bytes}, {kept, kept ? heads * keep * four : 0},
                      {seq_lens, cache->n_seqs * four}, {cache->page_table, (int64_t)cache->n_seqs * cache->table_stride * four}};
   for (int i = 0; i < 6; ++i) {
-    if (r[i].bytes && meets_pages(a.cache, r[i].at, r[i].bytes)) return HTTM_E_INVALID_ARG;
+    if (r[i].bytes && meets_pages(a.cache, scales, r[i].at, r[i].bytes)) return HTTM_E_INVALID_ARG;
     for (int j = 0; j < std::min(i, 4); ++j)
       if (r[i].bytes && r[j].bytes && meet(r[i].at, r[i].bytes, r[j].at, r[j].bytes)) return HTTM_E_INVALID_ARG;
   }
+  a.scales = (uint8_t*)scales;
   a.seq_lens = seq_lens;
   a.weights = weights;
   a.columns = columns;

@@ -697,7 +697,7 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
           r.k[i] = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(c.cache.k_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
           r.v[i] = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(c.cache.v_pages + at * kMxRowBytes, n, kMxRowBytes), in, 0, 0);
           r.exponents[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
-              uniform_rows((const char*)c.cache.scales + at * kMxScaleBytes, n, kMxScaleBytes), l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
+              uniform_rows((const char*)c.scales + at * kMxScaleBytes, n, kMxScaleBytes), l16 * kMxScaleBytes + 2 * (grp >> 1), 0, 0);
         }
       };
       if constexpr (KIND != MX4_ALONE) g = look_up(unit);
@@ -1019,7 +1019,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
     };
 
     // The units [u0, stop) of a piece.  OWN: all of them prefix or all own keys, known to the compiler (rows in 4 bits: one loop for each of the two, without a
-    // choice between two kinds of loads in it: 662 -> TIME us, 4 x 1374 rows to 5516 shared keys in 16 bits and up to 27480 own ones in 4, 16 heads), or by the unit
+    // choice between two kinds of loads in it: 662 -> 574 us, 4 x 1374 rows to 5516 shared keys in 16 bits and up to 27480 own ones in 4, 16 heads), or by the unit
     bool holes = false;
     auto run_units = [&](auto own_units, const int u0, const int stop) __attribute__((always_inline)) {
       constexpr int OWN = decltype(own_units)::value;
@@ -1052,7 +1052,7 @@ __global__ __launch_bounds__(64 * kWideWaves) __attribute__((amdgpu_waves_per_eu
           const u32x2 codes = __builtin_amdgcn_raw_buffer_load_b64(uniform_rows(pages + r.offset * kMxRowBytes, r.n, kMxRowBytes), lane * 8, 0, 0);
           in[0][0] = codes[0];
           in[0][1] = codes[1];
-          in[1][0] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(uniform_rows((const char*)c.cache.scales + r.offset * kMxScaleBytes, r.n, kMxScaleBytes),
+          in[1][0] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(uniform_rows((const char*)c.scales + r.offset * kMxScaleBytes, r.n, kMxScaleBytes),
                                                                   (lane >> 2) * kMxScaleBytes + (lane & 2) + exponent, 0, 0);
           return;
         }
@@ -1338,8 +1338,8 @@ void start(const LineArgs& a, int shares, hipStream_t stream) {
 template <int NA, int NB>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
   if constexpr (NA > 0) {      // (the sequences' part has no prefix)
-    if (a.c.cache.scales) return start<NA, NB, MX4_ALONE>(a, shares, stream);
-  } else if (a.c.cache.scales) {
+    if (a.c.scales) return start<NA, NB, MX4_ALONE>(a, shares, stream);
+  } else if (a.c.scales) {
     return a.c.P > 0 && a.part[1].with_prefix ? start<NA, NB, MX4_ROWS>(a, shares, stream) : start<NA, NB, MX4_ALONE>(a, shares, stream);
   }
   if (a.c.lse && a.finish)      // (pieces in their slots leave the sums to combine_kernel)
@@ -1396,7 +1396,7 @@ hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t strea
     w.min_length = 2 * kWideUnit;
     // (the part of the prefix has no rows in 4 bits)
     const bool causal = args.causal && i == 1;
-    if (i == 1 && args.cache.scales)
+    if (i == 1 && args.scales)
       args.P > 0 && a.part[1].with_prefix ? start_wide<MX4_ROWS>(w, causal, ch.shares[i], stream) : start_wide<MX4_ALONE>(w, causal, ch.shares[i], stream);
     else if (args.lse && a.finish)
       start_wide<ROWS_AND_SUMS>(w, causal, ch.shares[i], stream);

@@ -135,7 +135,7 @@ struct KeysOnTheirWay {
       return __builtin_amdgcn_make_buffer_rsrc((void*)uniform64((int64_t)((char*)p + first * bytes)), 0, uniform(n * bytes), kRawBufferWord3);
     };
     if constexpr (MX4) {
-      const __amdgpu_buffer_rsrc_t codes = rows(c.k_pages, kMxRowBytes), scales = rows(c.scales, kMxScaleBytes);
+      const __amdgpu_buffer_rsrc_t codes = rows(c.k_pages, kMxRowBytes), scales = rows(a.scales, kMxScaleBytes);
 #pragma unroll
       for (int t = T0; t < T1; ++t) {
         const int in = l16 + 16 * (t - T0);
@@ -233,6 +233,17 @@ __device__ __forceinline__ void add_tile(float (&sum)[4], const f32x4 (&x)[4], c
     sum[t] += (p[0] + p[1]) + (p[2] + p[3]);
   }
 }
+// Four rows alone, the first lane group's, against 64 keys: a quarter of the exponents where every group takes 16 of the keys.  Row e of the
+// scores x[t] of lane group 0, for t = 0 .. 3, into lane group t
+__device__ __forceinline__ float groups_apart(const f32x4 (&x)[4], int e) {
+  auto bits = [&](int t) { return __float_as_uint(x[t][e]); };
+  const auto lo = __builtin_amdgcn_permlane16_swap(bits(0), bits(1), false, false);
+  const auto hi = __builtin_amdgcn_permlane16_swap(bits(2), bits(3), false, false);
+  const uint32_t a = lo[0], b = hi[0];
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  const uint32_t y = r[0];
+  return __uint_as_float(y);
+}
 // Sums of 64 keys into the weights: key `lane` of them to lane `lane`
 __device__ __forceinline__ float key_of_lane(const float (&sum)[4], int grp) {
   float mine = 0.f;
@@ -245,8 +256,9 @@ __device__ __forceinline__ float key_of_lane(const float (&sum)[4], int grp) {
 }
 
 // Few rows: NT tiles of them stay in registers
+constexpr int few_waves(int nt) { return nt == 1 ? 4 : 2; }      // on a SIMD
 template <bool MX4, int NT, bool CAUSAL>
-__global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const WeighArgs a) {
+__global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_eu(few_waves(NT), few_waves(NT)))) void weigh_few_kernel(const WeighArgs a) {
   constexpr int kFront = 4;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
   const int H = a.cache.H_kv;
@@ -286,8 +298,10 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const Weigh
   };
   auto weight_at = [&](const Place& p) { return a.weights + ((int64_t)p.b * H + p.h) * a.columns + p.chunk * kWeighKeys + lane; };
 
-  KeysOnTheirWay<MX4> keys;      // of the item ahead
-  float old;
+  // The next item's keys are requested as soon as those of the item in work are turned into operands.  (Two items ahead take registers from the
+  // waves: 64 streams 74 us, so 64.)
+  KeysOnTheirWay<MX4> keys;
+  float old = 0.f;
   Place here, ahead;
   ahead.b = share.b, ahead.begin = share.begin;
   bool more = start(ahead);
@@ -295,11 +309,12 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const Weigh
   f32x4 lse[NT];
   int of_b = -1, of_h = -1;      // whose rows q holds
   auto request = [&] {
+    if (!more) return;
     keys.look_up(a, ahead.b, ahead.s.len, ahead.chunk * kWeighKeys);
     keys.request(a, ahead.s.len, ahead.h, ahead.chunk * kWeighKeys, l16, grp);
     old = ahead.chunk * kWeighKeys + lane < ahead.s.len - ahead.s.n ? *weight_at(ahead) : 0.f;
   };
-  if (more) request();
+  request();
   while (more) {
     here = ahead;
     const int j0 = here.chunk * kWeighKeys, n_rows = here.s.n * a.group, before = here.s.len - here.s.n;
@@ -308,18 +323,29 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const Weigh
     bf16x8 k[4][2];
     keys.take(k);
     more = next(ahead);
-    if (more) request();
+    request();
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    const bool stays = n_rows <= 16 * NT;
+    const bool stays = n_rows <= 16 * NT, four = NT == 1 && n_rows <= 4;
     for (int r0 = 0; r0 < n_rows; r0 += 16 * NT) {
       if (!stays || of_b != here.b || of_h != here.h) {
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
           load_queries(q[i], a, here.s, here.h, r0 + 16 * i + l16, n_rows, grp);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) lse[i][e] = load_lse(a, here.s, here.h, r0 + 16 * i + 4 * grp + e, n_rows);
+          for (int e = 0; e < 4; ++e) lse[i][e] = load_lse(a, here.s, here.h, r0 + 16 * i + (four ? 0 : 4 * grp) + e, n_rows);
         }
         of_b = here.b, of_h = here.h;
+      }
+      if (four) {
+        f32x4 x[4];
+        scores_of(x, k, q[0]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(groups_apart(x, e), scale_log2, lse[0][e]));
+          const int sees = CAUSAL ? before + token_of(a, e) + 1 - j0 : kWeighKeys;
+          sum[0] += lse[0][e] == -__builtin_inff() || lane >= sees ? 0.f : p;
+        }
+        break;
       }
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
@@ -336,7 +362,7 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_few_kernel(const Weigh
         add_tile<true, CAUSAL>(sum, x, lse[i], scale_log2, sees, l16);
       }
     }
-    float mine = key_of_lane(sum, grp);
+    float mine = four ? sum[0] : key_of_lane(sum, grp);
     if (!((there >> grp) & 1)) mine = 0.f;
     if (j0 + lane < here.s.len) *weight_at(here) = j0 + lane < before ? fmaf(a.decay, was, mine) : mine;
   }
@@ -689,7 +715,7 @@ struct RowMover {
     const int64_t r = at(row);
     if constexpr (MX4) {
       if (l16 < 4) x = *((const u32x4*)((l16 < 2 ? a.cache.k_pages : a.cache.v_pages) + r * kMxRowBytes) + (l16 & 1));
-      if (l16 == 4) x[0] = *(const uint32_t*)(a.cache.scales + r * kMxScaleBytes);
+      if (l16 == 4) x[0] = *(const uint32_t*)(a.scales + r * kMxScaleBytes);
     } else {
       x = *((const u32x4*)((l16 < 8 ? a.cache.k_pages : a.cache.v_pages) + r * kRowBytes) + (l16 & 7));
     }
@@ -699,7 +725,7 @@ struct RowMover {
     const int64_t r = at(row);
     if constexpr (MX4) {
       if (l16 < 4) *((u32x4*)((l16 < 2 ? a.cache.k_pages : a.cache.v_pages) + r * kMxRowBytes) + (l16 & 1)) = x;
-      if (l16 == 4) *(uint32_t*)(a.cache.scales + r * kMxScaleBytes) = x[0];
+      if (l16 == 4) *(uint32_t*)(a.scales + r * kMxScaleBytes) = x[0];
     } else {
       *((u32x4*)((l16 < 8 ? a.cache.k_pages : a.cache.v_pages) + r * kRowBytes) + (l16 & 7)) = x;
     }
@@ -768,9 +794,9 @@ void start_weigh(const WeighArgs& a, hipStream_t stream) {
   if (mean > 64)
     hipLaunchKernelGGL((weigh_many_kernel<MX4, CAUSAL>), dim3(1024), block, 0, stream, a);
   else if (mean > 16)
-    hipLaunchKernelGGL((weigh_few_kernel<MX4, 4, CAUSAL>), dim3(1024), block, 0, stream, a);
+    hipLaunchKernelGGL((weigh_few_kernel<MX4, 4, CAUSAL>), dim3(256 * few_waves(4)), block, 0, stream, a);
   else
-    hipLaunchKernelGGL((weigh_few_kernel<MX4, 1, CAUSAL>), dim3(1024), block, 0, stream, a);
+    hipLaunchKernelGGL((weigh_few_kernel<MX4, 1, CAUSAL>), dim3(256 * few_waves(1)), block, 0, stream, a);
 }
 template <bool MX4>
 void start_moves(const EvictArgs& a, hipStream_t stream) {
@@ -784,7 +810,7 @@ void start_moves(const EvictArgs& a, hipStream_t stream) {
 hipError_t launch_cache_weigh(const WeighArgs& args, hipStream_t stream) {
   WeighArgs a = args;
   a.group_magic = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
-  if (a.cache.scales)
+  if (a.scales)
     a.causal ? start_weigh<true, true>(a, stream) : start_weigh<true, false>(a, stream);
   else
     a.causal ? start_weigh<false, true>(a, stream) : start_weigh<false, false>(a, stream);
@@ -804,7 +830,7 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(evict_select_kernel<1024>, heads, dim3(1024), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  a.cache.scales ? start_moves<true>(a, stream) : start_moves<false>(a, stream);
+  a.scales ? start_moves<true>(a, stream) : start_moves<false>(a, stream);
   return hipGetLastError();
 }
 

@@ -202,9 +202,8 @@ struct TokenRows {
   int64_t head_stride;
 };
 struct PagedArgs {
-  char* k_pages;            // bf16 rows, or with `scales` codes of 4 bits (mx4.hpp)
+  char* k_pages;            // bf16 rows, or next to scales codes of 4 bits (mx4.hpp)
   char* v_pages;
-  uint8_t* scales;
   const int32_t* table;
   int64_t n_pages;
   int32_t n_seqs;
@@ -231,12 +230,14 @@ struct NormRopeArgs {
   const int32_t* offsets;
   const int32_t* seq_lens;
   uint64_t turn[kMaxPairs]; // turns per position step of every pair of an axis, as a fraction of 2^64
+  uint8_t* scales;          // of a cache in 4 bits, or nullptr
 };
 // dtype: HTTM_BF16 / _FP16 / _FP32 of the sources; append: into a.cache instead of [H, N, 64] tensors.
 hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, bool append, hipStream_t stream);
 // The rows of a batch's tokens out of the cache, as bf16 [N][H_kv][64]
 struct CacheReadArgs {
   PagedArgs cache;
+  const uint8_t* scales;    // or nullptr
   const int32_t* offsets;
   const int32_t* seq_lens;
   int64_t N;
@@ -258,8 +259,9 @@ struct CachedAttnArgs {
   int32_t causal;
   float scale_log2;         // scale * log2(e)
   void* o;                  // [n_tokens][H_kv * group * 64] bf16
-  float* lse;               // [n_tokens][H_kv * group] or nullptr
   char* workspace;
+  float* lse;               // [n_tokens][H_kv * group] or nullptr
+  const uint8_t* scales;    // of a cache in 4 bits, or nullptr
 };
 int64_t cached_attention_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P);
 hipError_t launch_cached_attention(const CachedAttnArgs& a, hipStream_t stream);
@@ -269,6 +271,7 @@ struct WeighArgs {
   TokenRows q;
   const float* lse;         // [n_tokens][H_kv * group]
   PagedArgs cache;
+  const uint8_t* scales;    // or nullptr
   const int32_t* offsets;
   const int32_t* seq_lens;
   int64_t n_tokens;
@@ -283,6 +286,7 @@ struct WeighArgs {
 hipError_t launch_cache_weigh(const WeighArgs& a, hipStream_t stream);
 struct EvictArgs {
   PagedArgs cache;
+  uint8_t* scales;          // or nullptr
   const int32_t* seq_lens;
   float* weights;
   int64_t columns;

@@ -157,15 +157,15 @@ struct CachePlace {
   int64_t row;        // in its sequence
   int64_t page_row;   // page * H_kv * page_size + row in the page: add head * page_size
 };
-__device__ __forceinline__ CachePlace find_place(const PagedArgs& cache, const int32_t* offsets, const int32_t* seq_lens, int64_t N, int64_t t,
-                                                 int lane) {
+template <typename Args>
+__device__ __forceinline__ CachePlace find_place(const Args& a, int64_t t, int lane) {
   CachePlace c = {false, false, 0, 0};
   // how many offsets are not above t: 64 at a time, one load for the whole wave.  us for 4096 tokens of 32 + 2 x 8 heads in 1 / 64 / 512 / 4096 sequences: 16.4 /
   // 17.0 / 22.8 / 64.9; one token each of 32 / 70 / 1000: 4.6 / 4.9 / 13.6
   int below = 0;
-  const int n_off = cache.n_seqs + 1, mine = lane >> 3;
+  const int n_off = a.cache.n_seqs + 1, mine = lane >> 3;
   for (int i = 0; i < n_off; i += 64) {
-    const int off = i + lane < n_off ? offsets[i + lane] : INT32_MAX;
+    const int off = i + lane < n_off ? a.offsets[i + lane] : INT32_MAX;
 #pragma unroll
     for (int j = 0; j < kTokens; ++j) {
       const int64_t tj = __shfl((int)t, 8 * j);
@@ -174,16 +174,16 @@ __device__ __forceinline__ CachePlace find_place(const PagedArgs& cache, const i
     }
   }
   const int b = below - 1;
-  if (t >= N || b < 0 || b >= cache.n_seqs) return c;
+  if (t >= a.N || b < 0 || b >= a.cache.n_seqs) return c;
   c.real = true;
-  const int64_t most = (int64_t)cache.table_stride << cache.page_shift;
-  const int64_t len = std::clamp<int64_t>(seq_lens[b], 0, most);
-  c.row = len - offsets[b + 1] + t;
+  const int64_t most = (int64_t)a.cache.table_stride << a.cache.page_shift;
+  const int64_t len = std::clamp<int64_t>(a.seq_lens[b], 0, most);
+  c.row = len - a.offsets[b + 1] + t;
   if (c.row < 0 || c.row >= most) return c;
-  const int64_t page = cache.table[(int64_t)b * cache.table_stride + (c.row >> cache.page_shift)];
-  if (page < 0 || page >= cache.n_pages) return c;
+  const int64_t page = a.cache.table[(int64_t)b * a.cache.table_stride + (c.row >> a.cache.page_shift)];
+  if (page < 0 || page >= a.cache.n_pages) return c;
   c.in_cache = true;
-  c.page_row = ((page * cache.H_kv) << cache.page_shift) + (c.row & ((1 << cache.page_shift) - 1));
+  c.page_row = ((page * a.cache.H_kv) << a.cache.page_shift) + (c.row & ((1 << a.cache.page_shift) - 1));
   return c;
 }
 
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
 
   CachePlace place = {true, false, 0, 0};
   constexpr bool APPEND = DEST != TO_DENSE;
-  if constexpr (APPEND) place = find_place(a.cache, a.offsets, a.seq_lens, a.N, t, lane);
+  if constexpr (APPEND) place = find_place(a, t, lane);
   const bool write = t < a.N && place.real && (!APPEND || part == 0 || place.in_cache);
 
   LaneRope rope = {};
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
     out = (part == 1 ? a.cache.k_pages : a.cache.v_pages) + (place.page_row + ((int64_t)head0 << a.cache.page_shift)) * kBytesOut;
     out_bytes = (int64_t)kBytesOut << a.cache.page_shift;
   }
-  uint8_t* scale_out = DEST == TO_MX4 ? a.cache.scales + (place.page_row + ((int64_t)head0 << a.cache.page_shift)) * kMxScaleBytes +
+  uint8_t* scale_out = DEST == TO_MX4 ? a.scales + (place.page_row + ((int64_t)head0 << a.cache.page_shift)) * kMxScaleBytes +
                                             2 * (chunk >> 2) + (part == 2 ? 1 : 0)
                                       : nullptr;
   for (int head = head0; head < head1; head += AHEAD) {
@@ -324,10 +324,10 @@ __global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(const CacheRead
   const int part = wave >= waves ? 1 : 0;
   wave -= part * waves;
   const int head0 = wave * heads_per_wave, head1 = std::min(head0 + heads_per_wave, H);
-  const CachePlace place = find_place(a.cache, a.offsets, a.seq_lens, a.N, t, lane);
+  const CachePlace place = find_place(a, t, lane);
   constexpr int kBytesIn = MX4 ? kMxRowBytes : kRowBytes;
   const char* in = (part ? a.cache.v_pages : a.cache.k_pages) + place.page_row * kBytesIn;
-  const uint8_t* scales = MX4 ? a.cache.scales + place.page_row * kMxScaleBytes + 2 * (chunk >> 2) + part : nullptr;
+  const uint8_t* scales = MX4 ? a.scales + place.page_row * kMxScaleBytes + 2 * (chunk >> 2) + part : nullptr;
   char* out = a.out[part] + t * H * kRowBytes;
   for (int head = head0; head < head1; head += kAtOnce) {
     u32x4 x[kAtOnce];
@@ -368,7 +368,7 @@ void start_norm_rope(const NormRopeArgs& a, int64_t groups, int heads_per_wave, 
 }
 template <int DT>
 void start_norm_rope(const NormRopeArgs& a, bool append, bool nt, int64_t groups, int heads_per_wave, hipStream_t stream) {
-  if (append && a.cache.scales)
+  if (append && a.scales)
     start_norm_rope<DT, TO_MX4, false>(a, groups, heads_per_wave, stream);
   else if (append)
     start_norm_rope<DT, TO_PAGES, false>(a, groups, heads_per_wave, stream);
@@ -404,7 +404,7 @@ hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream) {
   const int H = a.cache.H_kv, per = groups * H < 2048 ? 1 : 4;
   const int waves = 2 * ((H + per - 1) / per);
   const dim3 grid((unsigned)groups, (unsigned)((waves + kWaves - 1) / kWaves)), block(64 * kWaves);
-  if (a.cache.scales)
+  if (a.scales)
     hipLaunchKernelGGL(cache_read_kernel<true>, grid, block, 0, stream, a, per);
   else
     hipLaunchKernelGGL(cache_read_kernel<false>, grid, block, 0, stream, a, per);
