@@ -576,7 +576,7 @@ HTTM_API int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefi
  * yet and get the sum alone.  Called after attention with the same arguments and its lse.  With `causal` a token sees the rows up to its own.
  * A row whose lse is minus infinity adds nothing, and a row of the cache without a page gets nothing.
  * weights: [n_seqs, H_kv, columns] fp32, columns at least table_stride * page_size; entries from the sequence's length on are
- * left as they were.  decay: finite, not negative.  n_tokens < 2^20.  Results are run-to-run identical. */
+ * left as they were.  decay: finite, not negative; 0 forgets what a key had.  n_tokens < 2^20; with 0 tokens the weights decay.  Results are run-to-run identical. */
 HTTM_API int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm_paged_t* cache, const void* scales, const int32_t* offsets,
                               const int32_t* seq_lens, int64_t n_tokens, int H_q, int d_head, float scale, int causal, float decay,
                               float* weights, int64_t columns, void* stream);
@@ -588,7 +588,7 @@ HTTM_API int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm
  * What lies behind row `keep` is left as it was.
  * new_lens: [n_seqs] int32 out, the lengths behind it (not over seq_lens, which is not written).
  * kept: [n_seqs, H_kv, keep] int32 out or NULL: where the row now at d was, -1 behind the sequence's end.
- * The rows from `first` on are written: their pages may belong to no other sequence.  A sequence one of whose rows has no page is left as it is, its kept
+ * The rows from `first` on are written: their pages may belong to no other sequence, and stand in the table once.  A sequence one of whose rows has no page is left as it is, its kept
  * all -1.
  * workspace: device, 256-byte aligned, httm_cache_evict_workspace(...) bytes. */
 HTTM_API int64_t httm_cache_evict_workspace(int n_seqs, int H_kv, int64_t keep);

@@ -255,6 +255,11 @@ __device__ __forceinline__ float key_of_lane(const float (&sum)[4], int grp) {
   return mine;
 }
 
+// A weight with what came: of a key that was there before (else it has none; decay 0 forgets it, also where it is no number)
+__device__ __forceinline__ float weight_with(const WeighArgs& a, bool before, float was, float mine) {
+  return before && a.decay != 0.f ? fmaf(a.decay, was, mine) : mine;
+}
+
 // Few rows: NT tiles of them stay in registers
 constexpr int few_waves(int nt) { return nt == 1 ? 4 : 2; }      // on a SIMD
 template <bool MX4, int NT, bool CAUSAL>
@@ -364,7 +369,7 @@ __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_e
     }
     float mine = four ? sum[0] : key_of_lane(sum, grp);
     if (!((there >> grp) & 1)) mine = 0.f;
-    if (j0 + lane < here.s.len) *weight_at(here) = j0 + lane < before ? fmaf(a.decay, was, mine) : mine;
+    if (j0 + lane < here.s.len) *weight_at(here) = weight_with(a, j0 + lane < before, was, mine);
   }
 }
 
@@ -430,28 +435,25 @@ __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_e
         int tile = std::max(run / 16, unseen) + wave;
         if (tile >= t1) continue;
         QueryWalk walk(a, s, h, 16 * tile + l16, n_rows, grp);
+        // the rows of a tile are on their way while the one before is in work (behind the last: rows that are there)
         bf16x8 q[2][2];
-        f32x4 x[2][4];
-        // The scores of a tile come while those of the one before are in work, its rows two tiles ahead.  (Behind the last tile: rows that are
-        // there, for nothing.)
         auto step = [&](int now, int then) {
           const f32x4 lse = *(const f32x4*)(s_lse + 16 * tile - run + 4 * grp);
-          scores_of(x[then], k, q[then]);
-          walk.take(q[now]);
+          walk.take(q[then]);
+          f32x4 x[4];
+          scores_of(x, k, q[now]);
           int sees[4] = {0, 0, 0, 0};
           if (dead || 16 * tile + 16 > n_rows || (CAUSAL && before + token_of(a, 16 * tile) + 1 < std::min(j0 + kWeighKeys, s.len))) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               sees[e] = lse[e] == -__builtin_inff() ? 0 : CAUSAL ? before + token_of(a, 16 * tile + 4 * grp + e) + 1 - j0 : kWeighKeys;
-            add_tile<true, CAUSAL>(sum, x[now], lse, scale_log2, sees, l16);
+            add_tile<true, CAUSAL>(sum, x, lse, scale_log2, sees, l16);
           } else {
-            add_tile<false, CAUSAL>(sum, x[now], lse, scale_log2, sees, l16);
+            add_tile<false, CAUSAL>(sum, x, lse, scale_log2, sees, l16);
           }
           tile += kWeighWaves;
         };
         walk.take(q[0]);
-        walk.take(q[1]);
-        scores_of(x[0], k, q[0]);
         while (true) {
           step(0, 1);
           if (tile >= t1) break;
@@ -467,7 +469,7 @@ __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
         for (int i = 0; i < kWeighWaves; ++i) mine += s_sum[i][lane];
         if (!((there >> grp) & 1)) mine = 0.f;
-        *weight = j0 + lane < before ? fmaf(a.decay, was, mine) : mine;
+        *weight = weight_with(a, j0 + lane < before, was, mine);
       }
       __syncthreads();
       chunk = next_chunk, h = next_h;

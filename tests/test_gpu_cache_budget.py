@@ -189,6 +189,39 @@ def test_weights_are_the_same_every_time_and_shared_pages_are_read(store):
     w.check(False)
 
 
+@pytest.mark.parametrize("store", STORES)
+def test_steps_without_tokens_let_the_weights_decay(store):
+    w = Weighed(store, [0, 0, 0], [100, 0, 33], 0, 4, 2, 16, seed=8)
+    got = w.check(True, decay=0.5)
+    assert torch.equal(got[0, :, :100], 0.5 * w.before[0, :, :100])
+    w.before[0, 0, 3], w.before[0, 0, 4] = math.inf, math.nan
+    got = w.run(True, decay=0.0)
+    assert not got[0, :, :100].any() and torch.equal(got[0, :, 100:], w.before[0, :, 100:])
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("new", [[1, 1, 1], [90, 100, 3], [20, 9, 30]])
+def test_graph_of_weights_follows_the_lengths(store, new):
+    w = Weighed(store, new, [300, 200, 150], 0, 4, 2, 16, seed=9)
+    w.attend(True)
+    b, weights = w.b, w.before.clone()
+    call = lambda t: httm.cache_weigh(b.q, w.lse, b.cache, b.offsets, b.seq_lens, t, causal=True, decay=0.5)  # noqa: E731
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(weights)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            call(weights)
+    for lens in ([300, 200, 150], [120, 130, 31], [299, 100, 150], [91, 101, 31]):
+        b.seq_lens.copy_(torch.tensor(lens))
+        weights.copy_(w.before)
+        graph.replay()
+        want = call(w.before.clone())
+        torch.cuda.synchronize()
+        assert torch.equal(weights, want), lens
+
+
 # ---- eviction --------------------------------------------------------------------------------------------------
 
 def expected(w, L, keep, first, last):

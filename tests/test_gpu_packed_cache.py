@@ -263,13 +263,17 @@ def test_keys_that_are_not_finite_stay_where_they_are_seen(new, lens, P):
     assert (err[last][:, :2, 32:] <= tol[last][:, :2, 32:]).all()
 
 
-@pytest.mark.parametrize("new,lens,P", [([2, 1, 90], [100, 50, 200], 33), ([2, 1, 4] * 6, [100, 50, 200] * 6, 16000), ([2, 1, 690], [100, 50, 800], 24033)])
-def test_pages_that_are_none_are_left_out(new, lens, P):
-    b = PackedBatch(new, lens, P, 2, 2, 16)
+@pytest.mark.parametrize("page", [16, 32, 128])
+@pytest.mark.parametrize("new,lens,P", [([2, 1, 90], [100, 50, 200], 33), ([2, 1, 4] * 6, [100, 50, 200] * 6, 16000), ([2, 1, 690], [100, 50, 800], 24033),
+                                        ([2, 1, 3000], [100, 50, 3300], 0), ([2, 1, 40], [300, 50, 200], 0)])
+def test_pages_that_are_none_are_left_out(new, lens, P, page):
+    b = PackedBatch(new, lens, P, 2, 2, page)
     drop = [torch.zeros(n, dtype=torch.bool, device="cuda") for n in b.lens]
     for i, j, bad in ((0, 2, -1), (0, 6, 2**31 - 1), (1, 0, -5), (2, 3, int(b.cache.k_codes.shape[0])), (2, 12, -1)):
+        if j >= b.cache.page_table.shape[1]:
+            continue
         b.cache.page_table[i, j] = bad
-        drop[i][16 * j:16 * j + 16] = True
+        drop[i][page * j:page * j + page] = True
     b.check(False, drop=drop)
     b.check(True, drop=drop)
 
