@@ -33,6 +33,9 @@
 //
 // Measured, and what bounds it.  Tiles of few rows: memory, 64 streams of 100 to 5496 rows behind 28 700 shared keys, 16 heads, 160 us, 5.3 TB/s of
 // what has to be read (a sum over 2 GiB reaches 6.16); one token to 5516 keys, 16 heads, is a chain of latencies, 10.7 us for 3.9 us of reading.
+// The same from a cache in 4 bits: 64 streams of 100 to 21 984 rows, 32 heads on 8, 86 us, 4.5 TB/s of the 375 MB that come (32 of a
+// unit's 116 vector instructions turn codes into values).  Tiles of 256 rows from it: 551 to 574 us where the same rows in 16 bits take 592, 4 x 1374 tokens to 5516 shared
+// and up to 27 480 own keys, 16 heads.
 // Tiles of 256 rows: vector issue and power, 4 frames of 1374 tokens behind 28 650 shared keys, 16 heads, 0.90 to 0.95 PFLOP/s in the loop (a bf16
 // product of 8192^3 reaches 1.20).
 #include <algorithm>
@@ -679,7 +682,8 @@ __device__ __forceinline__ void walk(const LineArgs& a, const Part& part, const 
       }
     }
     if constexpr (MX4) {
-      // Own keys in 4 bits: a unit's codes are turned into values, and those of a later one requested in their place
+      // Own keys in 4 bits: a unit's codes are turned into values, and those of a later one requested in their place.  (64 streams: 104 us with one unit ahead
+      // and loads that wait for each other, 86 with three.  Next to a prefix's loop there are no registers for more than one.)
       constexpr int AHEAD = KIND == MX4_ALONE && NQ == 1 ? 3 : 1;
       MxUnit raw[AHEAD];
       int ok_raw[AHEAD];

@@ -6,6 +6,7 @@
 //
 // The kernel moves 128 bytes in and 128 out per row (256 in from fp32) and does some ten operations per element: it is bound
 // by memory, or by one launch where there are few rows.
+// Into a cache in 4 bits: 10 992 tokens of 2 x 16 heads, 57 MB, 17.6 us, 3.3 TB/s, the codes' rounding by instructions for it.
 // Measured: 137 400 tokens of 3 x 16 heads, 1.7 GB, 310 us, 5.4 TB/s (a copy of 2 GiB reaches 4.96); 10 992 tokens 26 us; 522 tokens 5.9 us, of
 // which 2.4 are a launch.
 //
@@ -311,8 +312,8 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(const NormRopeAr
   }
 }
 
-// Rows of the cache to [N][H_kv][64], as values: heads [head0, head1) of eight tokens' keys or values, eight lanes a row.  Bound by memory: 
-// 68 or 256 bytes in and 256 out for a token and head.
+// Rows of the cache to [N][H_kv][64], as values: heads [head0, head1) of eight tokens' keys or values, eight lanes a row.  Bound by memory,
+// 68 or 256 bytes in and 256 out for a token and head: 10 992 tokens of 16 heads in 4 bits, 57 MB, 11.4 us, 5.0 TB/s.
 template <bool MX4>
 __global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(const CacheReadArgs a, int heads_per_wave) {
   constexpr int kAtOnce = 4;
