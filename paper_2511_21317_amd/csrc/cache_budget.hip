@@ -747,8 +747,8 @@ struct RowMover {
 // The free places are filled, and the last rows go to the end.  Sources of the moves lie behind all places that they fill, so moves do not
 // meet; those in front of row `keep` lie where the last rows go, and move first.  Where the last rows do not go over themselves the workgroups of a head
 // take a part of that region each; else one of them takes all of it, and a batch is read before it is written.
-// (Measured: 512 heads that move 256 + up to 256 rows each in 16 bits, 15 us, 4.6 TB/s; 32 heads of 1374 + up to 4000 rows in 4 bits 22 to 26 us, for which a chain
-// of four dependent loads a batch counts.)
+// (Measured: 512 heads, a quarter of which move 256 + up to 256 rows in 16 bits, 25 MB, 15 us; 32 heads of 1374 + up to 4000 rows in 4 bits 22 to 26 us: chains of
+// counts, places, pages and rows, each known when the one before has come.)
 template <bool MX4>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const EvictArgs a) {
   const int bh = blockIdx.x, b = bh / a.cache.H_kv, parts = gridDim.y, part = blockIdx.y;
