@@ -190,6 +190,24 @@ def test_weights_are_the_same_every_time_and_shared_pages_are_read(store):
 
 
 @pytest.mark.parametrize("store", STORES)
+def test_weights_of_lengths_out_of_range(store):
+    """More rows than the table has count as its rows, fewer than none as none; columns behind them stay."""
+    w = Weighed(store, [2, 1, 1], [48, 48, 48], 0, 2, 2, 16, seed=10, more=7)
+    b, c = w.b, w.b.cache
+    table = c.page_table[:, :3].contiguous()
+    b.cache = httm.PackedCache(c.k_codes, c.v_codes, c.scales, table) if store == "mx4" else httm.PagedCache(c.k_pages, c.v_pages, table)
+    w.attend(True)
+    b.seq_lens.copy_(torch.tensor([2**31 - 1, 48, -7]))
+    b.lens[2], b.k[2], b.v[2] = 0, b.k[2][:, :0], b.v[2][:, :0]
+    w.check(True, decay=0.5)
+    with pytest.raises(httm.HttmError):
+        httm.cache_weigh(b.q, w.lse, b.cache, b.offsets, b.seq_lens, w.before[:, :, :47].contiguous())
+    for bad in ((None, w.lse, w.before), (b.q, None, w.before), (b.q, w.lse, None), (b.q, w.lse[:-1], w.before), (b.q, w.lse, w.before.double())):
+        with pytest.raises(httm.HttmError):
+            httm.cache_weigh(bad[0], bad[1], b.cache, b.offsets, b.seq_lens, bad[2])
+
+
+@pytest.mark.parametrize("store", STORES)
 def test_steps_without_tokens_let_the_weights_decay(store):
     w = Weighed(store, [0, 0, 0], [100, 0, 33], 0, 4, 2, 16, seed=8)
     got = w.check(True, decay=0.5)
@@ -371,6 +389,32 @@ def test_eviction_beyond_32_bit_offsets():
     httm.cache_evict(small, e.b.seq_lens, e.weights, 256, new, first=3, last=30, workspace=ws)
     assert torch.equal(k[-used:].view(torch.int16), small.k_pages.view(torch.int16)) and torch.equal(v[-used:].view(torch.int16), small.v_pages.view(torch.int16))
     assert torch.equal(w, e.weights) and not k[:-used].any()
+
+
+def test_evictions_on_two_streams_and_with_any_workspace():
+    """Two caches at once, a workspace each, whatever is in it."""
+    pairs = [Evicted("mx4", [900, 300, 70], 4, 16, seed=11), Evicted("bf16", [5000, 2000], 2, 64, seed=12)]
+    results = []
+    for fill in (0, 0xFF):
+        streams = [torch.cuda.Stream() for _ in pairs]
+        kept = []
+        copies = [[t.clone() for t in (*e.tensors(), e.weights)] for e in pairs]
+        torch.cuda.synchronize()
+        for e, s in zip(pairs, streams):
+            n, H = len(e.b.lens), e.b.H_kv
+            with torch.cuda.stream(s):
+                new, k = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, H, 250, dtype=torch.int32, device="cuda")
+                ws = torch.full((httm.cache_evict_workspace(n, H, 250),), fill, dtype=torch.uint8, device="cuda")
+                httm.cache_evict(e.b.cache, e.b.seq_lens, e.weights, 250, new, first=3, last=40, kept=k, workspace=ws)
+                kept += [k, new, ws]
+        torch.cuda.synchronize()
+        results.append([t.clone() for e in pairs for t in (*e.tensors(), e.weights)] + [t for t in kept if t.dtype is torch.int32])
+        for e, old in zip(pairs, copies):
+            for t, o in zip((*e.tensors(), e.weights), old):
+                t.copy_(o)
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(*results))
+    for e in pairs:
+        e.check(250, 3, 40)
 
 
 def test_graph_follows_the_lengths():

@@ -278,6 +278,41 @@ def test_pages_that_are_none_are_left_out(new, lens, P, page):
     b.check(True, drop=drop)
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("new,lens,P", [([1, 1, 3], [40, 300, 50], 0), ([1, 3], [40, 50], 700), ([1] * 30, [20 + i for i in range(30)], 3607),
+                                        ([300, 280], [340, 800], 16001), ([2900], [3300], 0)])
+def test_a_query_that_is_not_finite_has_its_own_row_alone(new, lens, P, value):
+    b = PackedBatch(new, lens, P, 4, 2, 16, seed=5)
+    ref, tol = (t.view(-1, 4, D) for t in b.reference(True))
+    b.q[b.n // 2, 1, 7], b.q[0, 3, 60] = value, -value
+    got = b.run(True).view(-1, 4, D)
+    off = ~((got.double() - ref).abs() <= tol)
+    own = torch.zeros_like(off)
+    own[b.n // 2, 1], own[0, 3] = True, True
+    assert not (off & ~own).any() and torch.isnan(got[own]).all()
+
+
+def test_tensors_that_are_missing_or_of_another_kind():
+    b = PackedBatch([3], [20], 0, 2, 2, 16)
+    c, x = b.cache, torch.zeros(3, 2, D, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(3, 2, device="cuda")
+    out = torch.zeros(3, 2 * D, dtype=torch.bfloat16, device="cuda")
+    call = lambda **kw: httm.attention_cached(b.q, None, None, c, b.offsets, b.seq_lens, out, workspace=b.ws, **kw)  # noqa: E731
+    for bad in (lse.double(), lse[:2], lse.t().contiguous().t(), lse.cpu()):
+        with pytest.raises(httm.HttmError):
+            call(lse=bad)
+    for bad in ((c.k_codes, c.v_codes, c.scales[..., :2].contiguous(), c.page_table), (c.k_codes, c.v_codes.view(torch.int8), c.scales, c.page_table),
+                (c.k_codes, None, c.scales, c.page_table), (c.k_codes, c.v_codes, None, c.page_table), (c.k_codes, c.k_codes, c.scales, c.page_table)):
+        with pytest.raises(httm.HttmError):
+            cache = httm.PackedCache(*bad)
+            httm.cache_read(cache, b.offsets, b.seq_lens, x, x.clone())
+    for bad in ((None, b.seq_lens, x, x.clone()), (b.offsets, None, x, x.clone()), (b.offsets, b.seq_lens, x, x), (b.offsets, b.seq_lens, x, x.float()),
+                (b.offsets, b.seq_lens, x[:, :1], x.clone()), (b.offsets, b.seq_lens, x, None)):
+        with pytest.raises(httm.HttmError):
+            httm.cache_read(c, *bad)
+    assert httm.cache_read(c, torch.zeros_like(b.offsets), b.seq_lens, x[:0], x[:0].clone())[0].numel() == 0
+
+
 def test_queries_of_any_strides_scales_and_runs():
     for name in ("drafts", "streams", "wide, frames", "together, many rows"):
         b = PackedBatch(*SHAPES[name], seed=8)
