@@ -1293,9 +1293,15 @@ struct Choice {
   int64_t row_pieces;       // bytes of the RowPieces of a part
 };
 
+// Own rows in 4 bits behind a prefix that is taken with the rows of all sequences: from so many on (of all sequences and key heads, by the room in the page table, which
+// is what the host knows of lengths) the prefix has a launch of its own, in tiles of 256 rows, and the own keys one of three waves a SIMD instead of
+// two.  In one launch / apart, us, 32 heads on 8, prefixes of 3000 and 20 000: 64 sequences with room for 0.56 M 33.1 / 34.7 and 49.9 / 49.0, 1.6 M 47.8 / 41.1 and
+// 62.8 / 56.1, 11.3 M 172.9 / 114.3 and 209.1 / 134.1; 24 x 4 tokens 0.29 M 29.2 / 37.3 and 54.8 / 55.8, 0.95 M 38.6 / 42.8 and 61.8 / 62.0, 3.7 M 83.5 / 66.2 and
+// 107.8 / 83.8; 40 sequences 1.3 M 41.6 / 38.0 and 55.4 / 51.9.
+constexpr int64_t kApartKeys = 1000000;
 constexpr int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 
-Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
+Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P, bool apart) {
   Choice c = {};
   const int64_t rows = n_tokens * (H_q / H_kv), mean = rows / n_seqs;
   // Rows of all sequences together against the prefix spare walks along it (`spared` keys of a head, 256 bytes each, in part from caches) and cost every row
@@ -1307,8 +1313,8 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
   const int64_t spared = (n_seqs - (rows + 63) / 64) * P * H_kv;
   c.stacked = mean <= 32 && spared > 250000 + 20 * rows * H_kv;
   // Up to 1024 rows of all sequences go with the own keys in one launch (drafts of 48 streams 62.3, with the prefix in 256-row tiles 71.3; 256 streams
-  // 93.6, 104).
-  c.tiles[0] = !c.stacked ? 0 : rows <= 16 ? 1 : rows <= 1024 ? 4 : 0;
+  // 93.6, 104), unless many own keys in 4 bits need one of their own (kApartKeys).
+  c.tiles[0] = !c.stacked ? 0 : rows <= 16 ? 1 : rows <= 1024 && !apart ? 4 : 0;
   // Tiles as small as hold a sequence's rows, on average: 100 random batches, time with the smaller tile / with the larger, geometric mean: 16 or 32 rows
   // at 9 to 16 rows a sequence 0.95, 32 or 64 at 25 to 32 0.87, at 33 to 48 0.96, but up to 1.3 where the second tile's walk counts; the
   // other way round 16 against 32 at 17 to 24 1.15.  Together with the prefix's 64-row tiles the registers are theirs, and 32 rows are quicker from 9 on: 62.3,
@@ -1362,16 +1368,21 @@ void start_wide(const LineArgs& a, bool causal, int shares, hipStream_t stream) 
 }  // namespace
 
 int64_t cached_attention_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
-  const Choice c = choose(n_tokens, n_seqs, H_q, H_kv, P);
-  int64_t bytes = 0;
-  for (int i = c.stacked ? 0 : 1; i < 2; ++i) bytes += c.row_pieces + slot_bytes(c, i);
-  return bytes;
+  int64_t most = 0;
+  for (bool apart : {false, true}) {
+    const Choice c = choose(n_tokens, n_seqs, H_q, H_kv, P, apart);
+    int64_t bytes = 0;
+    for (int i = c.stacked ? 0 : 1; i < 2; ++i) bytes += c.row_pieces + slot_bytes(c, i);
+    most = std::max(most, bytes);
+  }
+  return most;
 }
 
 hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t stream) {
   if (args.n_tokens == 0) return hipSuccess;
   const int H_kv = args.cache.H_kv, H_q = H_kv * args.group;
-  const Choice ch = choose(args.n_tokens, args.cache.n_seqs, H_q, H_kv, args.P);
+  const bool apart = args.scales && ((int64_t)args.cache.n_seqs * args.cache.table_stride << args.cache.page_shift) * H_kv > kApartKeys;
+  const Choice ch = choose(args.n_tokens, args.cache.n_seqs, H_q, H_kv, args.P, apart);
   LineArgs a = {};
   a.c = args;
   a.H_q = H_q;

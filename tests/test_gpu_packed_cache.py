@@ -236,6 +236,19 @@ def test_attention(shape, causal):
     check_sums(lse, b, causal)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("new,lens,P,heads", [([1] * 30, spread(0, 9000, 30), 3607, 4), ([3, 1, 5, 2, 4] * 4, spread(5, 20000, 20), 6201, 4),
+                                              ([2, 0, 30] * 8, spread(0, 12000, 24), 9001, 4)])
+def test_attention_with_the_prefix_in_a_launch_of_its_own(new, lens, P, heads, causal):
+    """The rows of all sequences against the prefix apart from long own rows: room for a million rows and more."""
+    b = PackedBatch(new, lens, P, 2 * heads, heads, 64, seed=len(new), pad_front=1, pad=2)
+    assert b.cache.page_table.numel() * 64 * heads > 1000000
+    got = b.check(causal)
+    lse = torch.full((b.n, b.H_q), 5.0, device="cuda")
+    httm.attention_cached(b.q, b.kp, b.vp, b.cache, b.offsets, b.seq_lens, got.clone(), causal=causal, workspace=b.ws, lse=lse)
+    check_sums(lse, b, causal)
+
+
 @pytest.mark.parametrize("shape", ["one token", "nothing at all", "streams", "drafts", "a prompt", "together, drafts", "wide, frames"],
                          ids=lambda s: s.replace(" ", "_").replace(",", ""))
 def test_sums_of_a_cache_in_16_bits(shape):
