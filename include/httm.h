@@ -525,7 +525,8 @@ HTTM_API int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q,
  * scale: positive, finite, also times log2(e) (1/8 = 1/sqrt(d_head); ln 2 for keys with log2(e) / 8 in them: HTTM_FLAG_LOG2_KEYS).
  * o: [n_tokens, H_q * d_head] bf16.  n_tokens < 2^20; 0 tokens are no error.
  * workspace: device, 256-byte aligned, httm_attention_cached_workspace(...) bytes; its contents before and after the call are
- * meaningless.  Results do not depend on it and are run-to-run identical. */
+ * meaningless.  Results do not depend on it and are run-to-run identical.  (That many are enough next to a cache in 4 bits as well, see below, which may
+ * need three times as many where the page table has much room; a call is refused only for fewer than its own launches take.) */
 HTTM_API int64_t httm_attention_cached_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P);
 HTTM_API int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P,
                                    const httm_paged_t* cache, const int32_t* offsets, const int32_t* seq_lens, int64_t n_tokens,

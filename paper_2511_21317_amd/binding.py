@@ -723,7 +723,7 @@ def cache_read(cache: PagedCache, offsets, seq_lens, k_out, v_out):
 
 
 def attention_cached_workspace(n_tokens: int, n_seqs: int, H_q: int, H_kv: int, P: int) -> int:
-    """Bytes of workspace of attention_cached()."""
+    """Bytes of workspace of attention_cached(), enough for a cache of either kind (a call refuses only fewer than its launches take)."""
     sizes = n_tokens, n_seqs, H_q, H_kv, P
     if min(sizes) < 0 or max(sizes) >= 1 << 31:      # (ctypes would take them modulo 2^32 or 2^64)
         raise HttmError(f"sizes must be from 0 to 2^31 - 1, got {sizes}")

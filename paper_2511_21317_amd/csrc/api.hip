@@ -928,7 +928,7 @@ int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const 
   if (!q || !q->data || !o || !aligned16(o) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HTTM_E_INVALID_ARG;
   rc = check_rows(q, &a.q);
   if (rc != HTTM_OK) return rc;
-  if (workspace_bytes < cached_attention_workspace(n_tokens, cache->n_seqs, H_q, cache->H_kv, P)) return HTTM_E_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < cached_attention_needs(a.cache, scales != nullptr, n_tokens, H_q, P)) return HTTM_E_WORKSPACE_TOO_SMALL;
   if (rows_meet(a.q, n_tokens, H_q, 2, o, n_tokens * H_q * kOutRow)) return HTTM_E_INVALID_ARG;
   const int64_t lse_bytes = n_tokens * H_q * (int64_t)sizeof(float);
   if (lse && (!aligned4(lse) || meet(lse, lse_bytes, o, n_tokens * H_q * kOutRow) || rows_meet(a.q, n_tokens, H_q, 2, lse, lse_bytes) ||

@@ -1299,6 +1299,9 @@ struct Choice {
 // 62.8 / 56.1, 11.3 M 172.9 / 114.3 and 209.1 / 134.1; 24 x 4 tokens 0.29 M 29.2 / 37.3 and 54.8 / 55.8, 0.95 M 38.6 / 42.8 and 61.8 / 62.0, 3.7 M 83.5 / 66.2 and
 // 107.8 / 83.8; 40 sequences 1.3 M 41.6 / 38.0 and 55.4 / 51.9.
 constexpr int64_t kApartKeys = 1000000;
+bool prefix_apart(const PagedArgs& cache, bool mx4) {
+  return mx4 && ((int64_t)cache.n_seqs * cache.table_stride << cache.page_shift) * cache.H_kv > kApartKeys;
+}
 constexpr int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 
 Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P, bool apart) {
@@ -1337,6 +1340,11 @@ Choice choose(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P, bool a
   return c;
 }
 int64_t slot_bytes(const Choice& c, int i) { return align256(c.slots[i] * c.rows[i] * 8) + align256(c.slots[i] * c.rows[i] * kDHead * 4); }
+int64_t plan_bytes(const Choice& c) {
+  int64_t bytes = 0;
+  for (int i = c.stacked ? 0 : 1; i < 2; ++i) bytes += c.row_pieces + slot_bytes(c, i);
+  return bytes;
+}
 
 template <int NA, int NB, int KIND>
 void start(const LineArgs& a, int shares, hipStream_t stream) {
@@ -1368,21 +1376,16 @@ void start_wide(const LineArgs& a, bool causal, int shares, hipStream_t stream) 
 }  // namespace
 
 int64_t cached_attention_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P) {
-  int64_t most = 0;
-  for (bool apart : {false, true}) {
-    const Choice c = choose(n_tokens, n_seqs, H_q, H_kv, P, apart);
-    int64_t bytes = 0;
-    for (int i = c.stacked ? 0 : 1; i < 2; ++i) bytes += c.row_pieces + slot_bytes(c, i);
-    most = std::max(most, bytes);
-  }
-  return most;
+  return std::max(plan_bytes(choose(n_tokens, n_seqs, H_q, H_kv, P, false)), plan_bytes(choose(n_tokens, n_seqs, H_q, H_kv, P, true)));
+}
+int64_t cached_attention_needs(const PagedArgs& cache, bool mx4, int64_t n_tokens, int H_q, int64_t P) {
+  return plan_bytes(choose(n_tokens, cache.n_seqs, H_q, cache.H_kv, P, prefix_apart(cache, mx4)));
 }
 
 hipError_t launch_cached_attention(const CachedAttnArgs& args, hipStream_t stream) {
   if (args.n_tokens == 0) return hipSuccess;
   const int H_kv = args.cache.H_kv, H_q = H_kv * args.group;
-  const bool apart = args.scales && ((int64_t)args.cache.n_seqs * args.cache.table_stride << args.cache.page_shift) * H_kv > kApartKeys;
-  const Choice ch = choose(args.n_tokens, args.cache.n_seqs, H_q, H_kv, args.P, apart);
+  const Choice ch = choose(args.n_tokens, args.cache.n_seqs, H_q, H_kv, args.P, prefix_apart(args.cache, args.scales != nullptr));
   LineArgs a = {};
   a.c = args;
   a.H_q = H_q;

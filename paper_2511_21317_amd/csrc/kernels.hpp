@@ -263,7 +263,9 @@ struct CachedAttnArgs {
   float* lse;               // [n_tokens][H_kv * group] or nullptr
   const uint8_t* scales;    // of a cache in 4 bits, or nullptr
 };
+// Bytes that are enough next to a cache of either kind, and what the launches next to this one take
 int64_t cached_attention_workspace(int64_t n_tokens, int n_seqs, int H_q, int H_kv, int64_t P);
+int64_t cached_attention_needs(const PagedArgs& cache, bool mx4, int64_t n_tokens, int H_q, int64_t P);
 hipError_t launch_cached_attention(const CachedAttnArgs& a, hipStream_t stream);
 
 // ---- accumulated attention weights, eviction ----------------------------------------------------------
