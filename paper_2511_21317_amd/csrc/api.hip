@@ -771,6 +771,12 @@ bool meets_pages(const PagedArgs& c, const void* scales, const void* range, int6
   const int64_t rows = (c.n_pages * c.H_kv) << c.page_shift, row = scales ? 32 : 128;
   return meet(c.k_pages, rows * row, range, bytes) || meet(c.v_pages, rows * row, range, bytes) || (scales && meet(scales, rows * 4, range, bytes));
 }
+// Whether a range lies over what all waves of a launch read to find their work: offsets (or nullptr), lengths, page table
+bool meets_batch(const PagedArgs& c, const int32_t* offsets, const int32_t* seq_lens, const void* range, int64_t bytes) {
+  const int64_t n = c.n_seqs, four = sizeof(int32_t);
+  return (offsets && meet(offsets, (n + 1) * four, range, bytes)) || meet(seq_lens, n * four, range, bytes) ||
+         meet(c.table, n * c.table_stride * four, range, bytes);
+}
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Norm, rotation and sources of a launch
@@ -894,9 +900,9 @@ int httm_cache_read(const httm_paged_t* cache, const void* scales, const int32_t
   if (d_head != 64 || n_tokens >= ((int64_t)1 << 25)) return HTTM_E_UNSUPPORTED;
   if (n_tokens == 0) return HTTM_OK;
   const int64_t bytes = n_tokens * cache->H_kv * kOutRow;
-  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || meet(k_out, bytes, v_out, bytes) || meets_pages(a.cache, scales, k_out, bytes) ||
-      meets_pages(a.cache, scales, v_out, bytes))
-    return HTTM_E_INVALID_ARG;
+  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || meet(k_out, bytes, v_out, bytes)) return HTTM_E_INVALID_ARG;
+  for (const void* out : {k_out, v_out})
+    if (meets_pages(a.cache, scales, out, bytes) || meets_batch(a.cache, offsets, seq_lens, out, bytes)) return HTTM_E_INVALID_ARG;
   a.scales = (const uint8_t*)scales;
   a.offsets = offsets;
   a.seq_lens = seq_lens;
@@ -929,10 +935,15 @@ int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const 
   rc = check_rows(q, &a.q);
   if (rc != HTTM_OK) return rc;
   if (workspace_bytes < cached_attention_needs(a.cache, scales != nullptr, n_tokens, H_q, P)) return HTTM_E_WORKSPACE_TOO_SMALL;
-  if (rows_meet(a.q, n_tokens, H_q, 2, o, n_tokens * H_q * kOutRow)) return HTTM_E_INVALID_ARG;
-  const int64_t lse_bytes = n_tokens * H_q * (int64_t)sizeof(float);
-  if (lse && (!aligned4(lse) || meet(lse, lse_bytes, o, n_tokens * H_q * kOutRow) || rows_meet(a.q, n_tokens, H_q, 2, lse, lse_bytes) ||
-              meet(lse, lse_bytes, workspace, workspace_bytes) || meets_pages(a.cache, scales, lse, lse_bytes)))
+  // nothing that is written lies over what is read for rows of other tokens
+  const int64_t o_bytes = n_tokens * H_q * kOutRow, lse_bytes = n_tokens * H_q * (int64_t)sizeof(float), prefix_bytes = P * cache->H_kv * kOutRow;
+  auto meets_sources = [&](const void* out, int64_t bytes) {
+    return rows_meet(a.q, n_tokens, H_q, 2, out, bytes) || meets_batch(a.cache, offsets, seq_lens, out, bytes) ||
+           (P > 0 && (meet(k_prefix, prefix_bytes, out, bytes) || meet(v_prefix, prefix_bytes, out, bytes)));
+  };
+  if (meets_sources(o, o_bytes)) return HTTM_E_INVALID_ARG;
+  if (lse && (!aligned4(lse) || meet(lse, lse_bytes, o, o_bytes) || meets_sources(lse, lse_bytes) || meet(lse, lse_bytes, workspace, workspace_bytes) ||
+              meets_pages(a.cache, scales, lse, lse_bytes)))
     return HTTM_E_INVALID_ARG;
   a.k_prefix = (const char*)k_prefix;
   a.v_prefix = (const char*)v_prefix;
@@ -976,7 +987,7 @@ int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm_paged_t*
   if (n_tokens > 0 && (!a.q.data || !lse || !aligned4(lse) || rows_meet(a.q, n_tokens, H_q, 2, weights, bytes) ||
                        meet(lse, n_tokens * H_q * (int64_t)sizeof(float), weights, bytes)))
     return HTTM_E_INVALID_ARG;
-  if (meets_pages(a.cache, scales, weights, bytes)) return HTTM_E_INVALID_ARG;
+  if (meets_pages(a.cache, scales, weights, bytes) || meets_batch(a.cache, offsets, seq_lens, weights, bytes)) return HTTM_E_INVALID_ARG;
   a.lse = lse;
   a.offsets = offsets;
   a.seq_lens = seq_lens;
