@@ -565,8 +565,8 @@ HTTM_API int httm_cache_read(const httm_paged_t* cache, const void* scales, cons
 
 /* httm_attention_cached, over either kind of cache, with the logarithms of the sums (or lse NULL):
  *   lse[t][h] = ln sum_j e^(scale * q.k_j), minus infinity for a token that sees no key.  lse: [n_tokens, H_q] fp32.
- * Keys and values in 4 bits enter as the values they stand for (exact in bf16).  In tiles of 256 rows the sum is one of weights rounded to bf16: a logarithm is
- * off by 2^-9 at most, by random 2^-9 / sqrt(3 n) of n keys that count alike. */
+ * Keys and values in 4 bits enter as the values they stand for (exact in bf16).  In tiles of 256 rows the sum is one of weights rounded to bf16, each off by half
+ * a step: a logarithm is off by 2^-8 at most, as that of a row that sees one key, by random about 2^-9 / sqrt(n) of n keys that count alike. */
 HTTM_API int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefix, const void* v_prefix, int64_t P,
                                        const httm_paged_t* cache, const void* scales, const int32_t* offsets, const int32_t* seq_lens,
                                        int64_t n_tokens, int H_q, int d_head, float scale, int causal, void* o, float* lse, void* workspace,
@@ -577,6 +577,7 @@ HTTM_API int httm_attention_cached_lse(const httm_rows_t* q, const void* k_prefi
  * over the tokens of sequence b and the query heads of key head h, for the rows j of the sequence; the batch's own tokens, its last rows, have no weight
  * yet and get the sum alone.  Called after attention with the same arguments and its lse.  With `causal` a token sees the rows up to its own.
  * A row whose lse is minus infinity adds nothing, and a row of the cache without a page gets nothing.
+ * What an lse is off by, all weights of its row are (from tiles of 256 rows up to 2^-8 of them, see above).
  * weights: [n_seqs, H_kv, columns] fp32, columns at least table_stride * page_size; entries from the sequence's length on are
  * left as they were.  decay: finite, not negative; 0 forgets what a key had.  n_tokens < 2^20; with 0 tokens the weights decay.  Results are run-to-run identical. */
 HTTM_API int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm_paged_t* cache, const void* scales, const int32_t* offsets,
