@@ -541,8 +541,8 @@ HTTM_API int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, c
  * Rows in 4 bits (the open MX format with e2m1 elements).  The 64 channels of a row are two blocks of 32.  A block has an exponent
  * byte e, and a channel a code of 4 bits, a sign (8) and the index of one of 0, 0.5, 1, 1.5, 2, 3, 4, 6: the value is that times 2^(e - 127); e = 255
  * makes the block NaN.  Rows are rounded as follows: e - 127 is the exponent of the block's largest |x|, rounded to two significant bits, less 2,
- * within -126 and 125; each channel becomes the nearest value, the even code of two that are as near.  So none is off by more than half a step (one
- * quarter of its value above the unit 2^(e - 127), 1/7 of the largest), but for |x| above 7 * 2^125, which are held as 6 * 2^125.  A block with an infinity or NaN becomes NaN.
+ * within -126 and 125; each channel becomes the nearest value, the even code of two that are as near.  So none is off by more than half a step (above
+ * the unit 2^(e - 127) one fifth of its value, the largest among them: 5 units become 4), but for |x| above 7 * 2^125, which are held as 6 * 2^125.  A block with an infinity or NaN becomes NaN.
  *
  * A cache in 4 bits is an httm_paged_t whose k_pages and v_pages are [n_pages, H_kv, page_size, d_head / 2] bytes, channel 2 i in the low
  * half of byte i, with `scales` beside it: [n_pages, H_kv, page_size, 4] bytes, the exponents of a row: key and value of channels 0 .. 31, key and
