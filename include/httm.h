@@ -505,7 +505,8 @@ typedef struct httm_paged {
  * front of offsets[0] and from offsets[n_seqs] on are padding, for which nothing is written.  A token whose row
  * would be negative is not written to the cache.
  * q: n_tokens x H_q rows, k, v: n_tokens x H_kv rows of type `dtype`.  q may have data NULL, and q_out be NULL then.
- * pos: [n_tokens][axes] int32 (device), or NULL with one axis: then a token's position is first_pos + its row.
+ * pos: [n_tokens][axes] int32 (device), or NULL with one axis: then a token's position is first_pos + its row (not for sequences
+ * that httm_cache_evict has cut, whose rows no longer count what came).
  * q_out: [n_tokens, H_q, d_head] bf16.  n_tokens < 2^25; 0 tokens are no error. */
 HTTM_API int httm_cache_append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v,
                                int dtype, const int32_t* pos, int64_t first_pos, int64_t n_tokens, int H_q, int d_head,
@@ -589,6 +590,9 @@ HTTM_API int httm_cache_weigh(const httm_rows_t* q, const float* lse, const httm
  * Rows move as little as they can: those that stay in front of row keep - last stay where they are; the rows that become free there are filled, in
  * ascending order, by those that stay behind it, in ascending order; the last rows move to the end, in order.  Weights move with their rows.
  * What lies behind row `keep` is left as it was.
+ * Rows keep the rotation that they were appended with, and a sequence that was cut is shorter than its tokens were many: with rotation the
+ * caller counts those, and gives httm_cache_append every later token's position in `pos`.  Without it a token would get one that an older row
+ * already has, and a single first_pos does not mend that, since sequences lose rows in different numbers.
  * new_lens: [n_seqs] int32 out, the lengths behind it (not over seq_lens, which is not written).
  * kept: [n_seqs, H_kv, keep] int32 out or NULL: where the row now at d was, -1 behind the sequence's end.
  * The rows from `first` on are written: their pages may belong to no other sequence, and stand in the table once.  A sequence one of whose rows has no page is left as it is, its kept

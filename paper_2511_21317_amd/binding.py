@@ -679,7 +679,8 @@ def qk_norm_rope(nr: NormRope, q, k, v, pos, q_out, k_out, v_out):
 def cache_append(nr: NormRope, q, k, v, pos, cache: PagedCache, offsets, seq_lens, q_out, first_pos: int = 0):
     """New tokens of the sequences of a batch into the cache (a PackedCache takes them in 4 bits): q [n, H_q, 64] (or None, with q_out), k, v [n, H_kv, 64]; offsets
     [n_seqs + 1], seq_lens [n_seqs] (with the new tokens) int32 on the GPU; q_out [n, H_q, 64] bf16.
-    pos: [n, axes] int32, or None with one axis: first_pos + a token's row in its sequence."""
+    pos: [n, axes] int32, or None with one axis: first_pos + a token's row in its sequence, which is not its position any more once
+    cache_evict() has cut the sequence: tokens that come later need `pos`."""
     code, dtype, here = _rows_type(k), k.dtype, _here(k)
     n, H_kv = k.shape[0] if k.dim() == 3 else 0, cache.H_kv
     H_q = q.shape[1] if q is not None and q.dim() == 3 else H_kv
@@ -805,6 +806,7 @@ def cache_evict_workspace(n_seqs: int, H_kv: int, keep: int) -> int:
 def cache_evict(cache: PagedCache, seq_lens, weights, keep: int, new_lens, first: int = 0, last: int = 0, kept=None, workspace=None):
     """Cuts every sequence of more than `keep` rows to `keep`, each key head by itself: the `first` first and the `last` last rows stay,
     and of the others those of highest weight (weights as for cache_weigh(); they move with their rows).  Places that become free are filled from behind.
+    Rows keep their rotation; as lengths no longer count the tokens that came, cache_append() has to be given `pos` from then on.
     seq_lens [n_seqs] int32 are the lengths, new_lens [n_seqs] those behind it; kept [n_seqs, H_kv, keep] int32 or None: where every row
     was.  workspace: a uint8 tensor of at least cache_evict_workspace(...) bytes."""
     i32 = torch.int32
