@@ -1297,7 +1297,9 @@ struct Choice {
 // is what the host knows of lengths) the prefix has a launch of its own, in tiles of 256 rows, and the own keys one of three waves a SIMD instead of
 // two.  In one launch / apart, us, 32 heads on 8, prefixes of 3000 and 20 000: 64 sequences with room for 0.56 M 33.1 / 34.7 and 49.9 / 49.0, 1.6 M 47.8 / 41.1 and
 // 62.8 / 56.1, 11.3 M 172.9 / 114.3 and 209.1 / 134.1; 24 x 4 tokens 0.29 M 29.2 / 37.3 and 54.8 / 55.8, 0.95 M 38.6 / 42.8 and 61.8 / 62.0, 3.7 M 83.5 / 66.2 and
-// 107.8 / 83.8; 40 sequences 1.3 M 41.6 / 38.0 and 55.4 / 51.9.
+// 107.8 / 83.8; 40 sequences 1.3 M 41.6 / 38.0 and 55.4 / 51.9.  (Tables half full, or full.)  Less full: 64 sequences, 11.3 M, at a tenth 54.8 / 44.1 and 70.2 / 58.2, at a
+// hundredth 26.9 / 30.5 and 45.1 / 45.7; 24 x 4 tokens, 4.2 M, at a quarter 55.8 / 52.5 and 77.6 / 66.2, at a tenth 37.0 / 44.6 and 60.1 / 57.6; 40 sequences on 4
+// heads, 1.3 M, at a tenth 23.5 / 28.7 and 30.4 / 41.9: a table with far more room than its sequences take costs up to 12 us.
 constexpr int64_t kApartKeys = 1000000;
 bool prefix_apart(const PagedArgs& cache, bool mx4) {
   return mx4 && ((int64_t)cache.n_seqs * cache.table_stride << cache.page_shift) * cache.H_kv > kApartKeys;

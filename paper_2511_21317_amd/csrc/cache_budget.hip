@@ -42,9 +42,10 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 //
 // Measured, and what bounds it.  Few rows: a token each of 64 streams of 100 to 21 984 keys in 4 bits, 32 heads on 8, 63 us, 3.7 TB/s of what has to be moved:
 // one item of 2.2 KB on its way for each of four waves a SIMD, half of whose time is waiting.  Many rows: 2 x 1374 tokens to 5496 to 13 740 keys in 16 bits, 16
-// heads, 132 us, 0.45 PFLOP/s: 466 million pairs, for 1024 of which a SIMD issues 16 exp2 of 16 cycles, some 50 vector instructions of 4 and 8 products
-// of 16, none of which hides behind the others (580 cycles in all, 16 waves a CU); loading scores a tile earlier changes nothing, staging the lse of a run of
-// rows in the LDS instead of asking for every row's took 150 to 133.
+// heads, 132 us, 0.45 PFLOP/s: 466 million pairs. By the counters a SIMD takes 656 clocks for 1024 of them. In 411 a vector instruction is in work: 78, of which 16 are
+// exp2 of 8 clocks (8.6 measured alone, 24 us of all pairs'), 16 fma, 16 additions and 30 the walk over the rows, its addresses and choices. In 128 a product is (8 of 16). Waves
+// wait for 57 % of their time: what bounds it is that rows, lse and addresses are taken anew for every 64 keys, and waiting for them. Loading scores a
+// tile earlier changes nothing, staging the lse of a run of rows in the LDS instead of asking for every row's took 150 to 133.
 
 constexpr int kWeighWaves = 4;
 constexpr int kWeighKeys = 64;      // of an item
@@ -838,7 +839,10 @@ int64_t cache_evict_workspace(int n_seqs, int H_kv, int keep) {
 
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t stream) {
   const dim3 heads((unsigned)(a.cache.n_seqs * a.cache.H_kv));
-  // (by what fits the LDS of a workgroup, of the rows that a sequence can have)
+  // By what fits the LDS of a workgroup, of the rows that a sequence can have: the host knows the room in the page table alone.  256 / 1024 threads, selection and
+  // moves, us: 64 sequences of 8 heads 4352 -> 4096 rows 35.6 / 42.8 (the workgroup with the larger LDS is alone on its CU), 1100 -> 1024 19.9 / 28.0, 8300 -> 8192 47.4 / 49.1,
+  // 16 700 -> 16 384 103 / 80; 2 of 16 heads 4352 -> 4096 23.3 / 20.8, 27 480 -> 13 740 119 / 46.  So many short heads in a table with room for long ones lose
+  // 7 or 8 us, and few heads of 8000 rows in a table with no more room 9 (33.4 / 24.4).
   if ((int64_t)a.cache.table_stride << a.cache.page_shift <= 256 * kEvictRuns)
     hipLaunchKernelGGL(evict_select_kernel<256>, heads, dim3(256), 0, stream, a);
   else

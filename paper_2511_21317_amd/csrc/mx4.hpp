@@ -15,7 +15,7 @@ constexpr int kMxRowBytes = kDHead / 2;
 constexpr int kMxScaleBytes = 4;
 
 // The exponent byte of a block from the bits of its largest |x|: that of x rounded to two bits of significand, less two, so that
-// x lies at 4 to 6 units and nothing in the block is more than half a step off.  The smallest unit is 2^-126, below which codes lose
+// x, held as 4 or 6 units, lies at 3.5 to 7 of them, and nothing in the block is more than half a step off.  The smallest unit is 2^-126, below which codes lose
 // bits; the largest 2^125, at which the last quarter below 2^128 is held as 6 units: 2^126 would make it infinite.
 // Infinities and NaN make the block NaN.
 __device__ __forceinline__ uint32_t mx4_exponent(uint32_t top) {
