@@ -549,8 +549,9 @@ HTTM_API int httm_attention_cached(const httm_rows_t* q, const void* k_prefix, c
  * half of byte i, with `scales` beside it: [n_pages, H_kv, page_size, 4] bytes, the exponents of a row: key and value of channels 0 .. 31, key and
  * value of channels 32 .. 63.  All three 16-byte aligned, none over another.
  * The calls below take `scales` NULL for a cache of bf16 rows.  What the section above says of offsets, lengths, tables and pages holds
- * for them as well.  An output of attention, read, weights or eviction that lies over offsets, lengths, the page table or the shared prefix is
- * refused (HTTM_E_INVALID_ARG), and so are sums, rows that are read, weights and lengths over the cache's pages: other waves still read those. */
+ * for them as well.  An output of these calls that lies over offsets, lengths, the page table, positions or the shared prefix is
+ * refused (HTTM_E_INVALID_ARG), and so are sums, rows that are read, weights and lengths over the cache's pages, and queries and sources of an append over pages in
+ * 4 bits: other waves still read what would be written. */
 
 /* httm_cache_append to a cache in 4 bits: keys and values are rounded once, from what norm, rotation and k_scale leave in fp32. */
 HTTM_API int httm_cache_append_mx4(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_rows_t* k, const httm_rows_t* v,

@@ -872,7 +872,18 @@ static int append(const httm_norm_rope_t* nr, const httm_rows_t* q, const httm_r
   a.offsets = offsets;
   a.seq_lens = seq_lens;
   a.out[0] = (char*)q_out;
-  if (outputs_meet(a, dtype, {n_tokens * a.H[0] * kOutRow, 0, 0}, {64 * a.H[0], 0, 0}, {64, 0, 0})) return HTTM_E_INVALID_ARG;
+  const int64_t q_bytes = n_tokens * a.H[0] * kOutRow;
+  if (outputs_meet(a, dtype, {q_bytes, 0, 0}, {64 * a.H[0], 0, 0}, {64, 0, 0})) return HTTM_E_INVALID_ARG;
+  if (q_out && (meets_batch(paged, offsets, seq_lens, q_out, q_bytes) ||
+                (pos && a.axes > 0 && meet(pos, n_tokens * a.axes * (int64_t)sizeof(int32_t), q_out, q_bytes))))
+    return HTTM_E_INVALID_ARG;
+  if (scales) {
+    if (q_out && meets_pages(paged, scales, q_out, q_bytes)) return HTTM_E_INVALID_ARG;
+    const int64_t rows = (paged.n_pages * paged.H_kv) << paged.page_shift;
+    for (int i = 0; i < 3; ++i)
+      for (const void* to : {(const void*)paged.k_pages, (const void*)paged.v_pages, (const void*)scales})
+        if (a.src[i].data && rows_meet(a.src[i], n_tokens, a.H[i], dtype == HTTM_FP32 ? 4 : 2, to, rows * (to == scales ? 4 : 32))) return HTTM_E_INVALID_ARG;
+  }
   HTTM_HIP(launch_norm_rope(a, dtype, true, (hipStream_t)stream));
   return HTTM_OK;
 }
